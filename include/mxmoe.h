@@ -190,6 +190,37 @@ MXMOE_API mxmoe_status mxmoe_router_topk(const float* logits, int32_t T, int32_t
                                int32_t* topk_ids, float* topk_w, float* shared_w,
                                hipStream_t stream);
 
+/* Workspace bytes of mxmoe_balance_loss (0 for invalid sizes).               */
+MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
+
+/* Balance loss of the router, with the experts' counts and the gradient of the
+ * logits.  Over the n tokens that token_mask keeps (all without a mask):
+ *   counts[e] = (token, slot) pairs of kept tokens whose id is e
+ *   probs[e]  = 1/n sum_t p[t,e],  p[t] = softmax of the token's logits
+ *   loss      = alpha E sum_e counts[e] / (k n) * probs[e]
+ *   grad[t,e] = dloss / dlogits[t,e]
+ *             = alpha E / n * p[t,e] (f_e - sum_j f_j p[t,j]), f_e = counts[e] / (k n)
+ *               (the counts are constants of the gradient), 0 for other tokens.
+ * alpha also takes the factor of a gradient from above.
+ *   logits    : fp32 [T, E]; -inf is a probability of 0, a token with nothing but
+ *               -inf has probabilities 0 throughout (it counts in n); a NaN or
+ *               +inf of a kept token makes loss and probs NaN
+ *   topk_ids  : int32 [T, k]; ids outside [0, E) are not counted, an id that a
+ *               token holds twice counts twice
+ *   token_mask: uint8 [T], 0 = not kept (padding: its logits and ids are not
+ *               used, whatever they hold), or NULL
+ *   counts: int32 [E], probs: fp32 [E], loss: fp32 [1]
+ *   grad  : fp32 [T, E], or NULL if not wanted; may be `logits` itself
+ * With no kept token everything is 0.  Sums over tokens are formed in a fixed
+ * order.  Limits: 1 <= k <= E <= 1024, T >= 0, T*k < 2^31.  4-byte aligned,
+ * workspace 256-byte.  Outputs share no bytes with inputs (but grad) or each
+ * other.  Errors: INVALID_ARG, WORKSPACE, HIP.                               */
+MXMOE_API mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids,
+                                const uint8_t* token_mask, int32_t T, int32_t E, int32_t k,
+                                float alpha, int32_t* counts, float* probs, float* loss,
+                                float* grad, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream);
+
 /* ------------------------------------------------------ activation quant */
 
 /* Per-row symmetric quantization of a [rows, cols] activation matrix (row
@@ -199,6 +230,33 @@ MXMOE_API mxmoe_status mxmoe_router_topk(const float* logits, int32_t T, int32_t
 MXMOE_API mxmoe_status mxmoe_act_quant(const void* a, mxmoe_dtype act, int32_t rows, int32_t cols,
                              int64_t ld, int32_t qmax, int8_t* codes, float* scales,
                              hipStream_t stream);
+
+/* Residual addition, RMS norm and per-row 8-bit encoding, one launch:
+ *   z = round(x + residual)                       (to `act`; x without residual)
+ *   r = fl32(1 / sqrt(mean over the row of z^2 + eps)), mean, root and quotient
+ *       in 64 bits (the same bits whatever the order of the sum)
+ *   y = round(fl32(fl32(z * r) * weight))         (to `act`)
+ *   codes, scales: of the rounded y, with the recipe and formats of
+ *       mxmoe_act_quant for qmax = 127 (int8) or 448 (FP8 e4m3); the codes that
+ *       mxmoe_linear_decode takes.  A row whose y is not finite throughout gets
+ *       scale NaN (and codes 0), a row whose largest |y| is below 2^-118 counts as
+ *       zero (scale 0, codes 0).
+ *   x       : `act` [rows, cols], row stride ldx elements
+ *   residual: `act` [rows, cols], row stride ldr, or NULL
+ *   weight  : `act` [cols]
+ *   sum     : z, row stride lds, or NULL (NULL without residual)
+ *   y       : row stride ldy, or NULL if only the codes are wanted
+ *   qmax    : 0 (codes and scales NULL), 127 or 448 (UNSUPPORTED otherwise)
+ *   codes   : int8 [rows, cols] dense, scales: fp32 [rows]
+ * 16-bit pointers 2-byte, scales 4-byte aligned; rows whose pointers and strides
+ * are multiples of 16 bytes take the wide path, others the same results.  sum and
+ * y may each be x or residual itself (same pointer and stride), but not share
+ * bytes with them otherwise, nor with each other, weight, codes or scales.
+ * eps > 0, cols <= 2^24.  Errors: INVALID_ARG, UNSUPPORTED, HIP.             */
+MXMOE_API mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                                const void* weight, mxmoe_dtype act, int32_t rows, int32_t cols,
+                                double eps, void* sum, int64_t lds, void* y, int64_t ldy,
+                                int32_t qmax, int8_t* codes, float* scales, hipStream_t stream);
 
 /* --------------------------------------------------------- one linear */
 
@@ -221,6 +279,27 @@ MXMOE_API size_t mxmoe_linear_workspace_bytes(const mxmoe_linear* L, int32_t m);
 MXMOE_API mxmoe_status mxmoe_linear_forward(const mxmoe_linear* L, mxmoe_dtype act, const void* packed,
                                   int32_t m, const void* a, void* out, void* workspace,
                                   size_t workspace_bytes, hipStream_t stream);
+
+/* Most rows of mxmoe_linear_decode.                                         */
+#define MXMOE_DECODE_ROWS 64
+
+/* One packed linear on the few rows of a decode step, one launch without plan or
+ * workspace: out = a W^T + bias, rounded once to `act`.
+ *   wNg128 with N = 4: a `act` [m, k], a_scales NULL; per group the exact sum of
+ *       a * (q - z) in fp32, times the group's scale, added over the groups;
+ *   w8a8: a int8 [m, k] codes, a_scales fp32 [m] (mxmoe_act_quant with qmax 127
+ *       or mxmoe_add_rms_norm): exact int32 sums times a_scales[m] * s_w[n];
+ *   fp8:  a e4m3 bytes [m, k], a_scales fp32 [m] (qmax 448): products
+ *       accumulated in fp32 by the FP8 MFMA, times a_scales[m] * s_w[n];
+ *   other schemes: UNSUPPORTED (mxmoe_linear_forward takes them, and more rows).
+ *   lda : row stride of a in elements; rows 16-byte aligned (a and the stride)
+ *   bias: `act` [n] or NULL, added in fp32 before the rounding
+ *   out : `act` [m, n], row stride ldo elements; shares no byte with the inputs
+ * Limits: 0 <= m <= MXMOE_DECODE_ROWS (UNSUPPORTED beyond), n and k as for every
+ * linear.  Errors: INVALID_ARG, UNSUPPORTED, HIP.                            */
+MXMOE_API mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const void* packed,
+                                 int32_t m, const void* a, int64_t lda, const float* a_scales,
+                                 const void* bias, void* out, int64_t ldo, hipStream_t stream);
 
 /* ---------------------------------------------------------- MoE block */
 

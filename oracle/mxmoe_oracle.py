@@ -50,7 +50,7 @@ import numpy as np
 __all__ = [
     "bf16_bits_to_f64", "round_to_act", "act_values", "route", "router_topk", "shared_gate", "dequant",
     "act_quant", "fp8_quant", "e4m3_values", "e4m3_code", "linear", "moe_forward", "lpt_makespan", "optimal_makespan",
-    "silu", "tile_plan", "scheme_index", "xcd_queues", "xcd_tiles",
+    "silu", "add_rms_norm", "balance_loss", "tile_plan", "scheme_index", "xcd_queues", "xcd_tiles",
 ]
 
 # ----------------------------------------------------------------------------
@@ -323,6 +323,61 @@ def act_quant_groups(a: np.ndarray, qmax: int, group: int) -> Tuple[np.ndarray, 
 
 def _qmax(a_bits: int) -> int:
     return (1 << (a_bits - 1)) - 1
+
+
+# ----------------------------------------------------------------------------
+# Residual addition and RMS norm (the rows in front of a block or a linear)
+# ----------------------------------------------------------------------------
+
+
+def add_rms_norm(x: np.ndarray, residual: Optional[np.ndarray], weight: np.ndarray, act: str, eps: float):
+    """(y, z, y64) for activation-dtype values x, residual [rows, cols], weight
+    [cols] given as fp64: z = x + residual rounded to the dtype, r = fl32(1 /
+    sqrt(mean z^2 + eps)), y = fl32(fl32(z r) weight) rounded to the dtype, and
+    y64 = z weight / sqrt(mean z^2 + eps) without any rounding.  The products of
+    two fp32 values are exact in fp64, so the casts below round them once."""
+    def f32(v):
+        return v.astype(np.float32).astype(np.float64)
+    z = x if residual is None else round_to_act(f32(x + residual), act)
+    r64 = 1.0 / np.sqrt((z * z).mean(axis=1) + eps)
+    y = round_to_act(f32(f32(z * f32(r64)[:, None]) * weight), act)
+    return y, z, z * r64[:, None] * weight
+
+
+# ----------------------------------------------------------------------------
+# Balance loss of the router
+# ----------------------------------------------------------------------------
+
+
+def balance_loss(logits: np.ndarray, topk_ids: np.ndarray, mask: Optional[np.ndarray] = None, alpha: float = 1.0,
+                 counts: Optional[np.ndarray] = None):
+    """(loss, counts, mean probabilities, gradient of the logits) in fp64:
+    L = alpha E sum_e f_e P_e over the n kept tokens, f_e = counts[e] / (k n),
+    P_e the mean softmax probability; the counts (given or counted) are constants
+    of the gradient.  Token by token, as the definition reads."""
+    T, E = logits.shape
+    k = topk_ids.shape[1]
+    kept = [t for t in range(T) if mask is None or mask[t]]
+    n = len(kept)
+    if counts is None:
+        counts = np.zeros(E, np.int64)
+        for t in kept:
+            for e in topk_ids[t]:
+                if 0 <= e < E:
+                    counts[e] += 1
+    P, grad = np.zeros(E), np.zeros((T, E))
+    if n == 0:
+        return 0.0, counts, P, grad
+    f = counts / (k * n)
+    for t in kept:
+        l = np.asarray(logits[t], np.float64)
+        if np.all(l == -np.inf):
+            continue
+        p = np.exp(l - l.max())
+        p /= p.sum()
+        P += p / n
+        grad[t] = alpha * E / n * p * (f - (f * p).sum())
+    return alpha * E * float((f * P).sum()), counts, P, grad
 
 
 # ----------------------------------------------------------------------------

@@ -412,6 +412,74 @@ mxmoe_status mxmoe_act_quant(const void* a, mxmoe_dtype act, int32_t rows, int32
   return hip_status(launch_act_quant(a, act, rows, cols, ld, qmax, codes, scales, stream));
 }
 
+// ------------------------------------------------------------ RMS norm
+namespace {
+// Rows of a buffer as a call uses it: `bytes` of each `pitch`.
+struct Rows {
+  const void* p;
+  int64_t pitch, bytes, rows;
+  uintptr_t lo() const { return (uintptr_t)p; }
+  uintptr_t hi() const { return lo() + (uintptr_t)((rows - 1) * pitch + bytes); }
+};
+// Whether two buffers share a byte.  Rows of one pitch may lie beside each other
+// in wider rows (slices of one tensor).
+bool overlap(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.hi() <= b.lo() || b.hi() <= a.lo()) return false;
+  if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
+  const int64_t d = a.lo() <= b.lo() ? (int64_t)((b.lo() - a.lo()) % a.pitch)
+                                     : (int64_t)((a.pitch - (int64_t)((a.lo() - b.lo()) % a.pitch)) % a.pitch);
+  return d < a.bytes || a.pitch - d < b.bytes;
+}
+bool same_rows(const Rows& a, const Rows& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
+constexpr int64_t kMaxPitch = (int64_t)1 << 38;  // bytes; more than the device's memory is a mistake
+constexpr int32_t kMaxNormCols = 1 << 24;
+}  // namespace
+
+mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                                mxmoe_dtype act, int32_t rows, int32_t cols, double eps, void* sum, int64_t lds,
+                                void* y, int64_t ldy, int32_t qmax, int8_t* codes, float* scales,
+                                hipStream_t stream) {
+  if (!valid_dtype(act) || rows < 0 || cols <= 0 || !(eps > 0.0) || !(eps < 1e300)) return MXMOE_ERR_INVALID_ARG;
+  if (qmax != 0 && qmax != 127 && qmax != kQmaxF8) return MXMOE_ERR_UNSUPPORTED;
+  if (cols > kMaxNormCols) return MXMOE_ERR_UNSUPPORTED;
+  if (rows == 0) return MXMOE_OK;
+  if (!x || !weight || (!y && !qmax) || (sum && !residual)) return MXMOE_ERR_INVALID_ARG;
+  if (qmax ? (!codes || !scales) : (codes || scales)) return MXMOE_ERR_INVALID_ARG;
+  const int64_t most = kMaxPitch / 2;
+  if (ldx < cols || ldx > most || (residual && (ldr < cols || ldr > most)) || (sum && (lds < cols || lds > most)) ||
+      (y && (ldy < cols || ldy > most)))
+    return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(weight, 2) || !aligned(sum, 2) || !aligned(y, 2) ||
+      !aligned(scales, 4))
+    return MXMOE_ERR_INVALID_ARG;
+  const int64_t b = 2 * (int64_t)cols;
+  const Rows in[3] = {{x, 2 * ldx, b, rows}, {residual, 2 * ldr, b, rows}, {weight, b, b, 1}};
+  const Rows out[4] = {{sum, 2 * lds, b, rows}, {y, 2 * ldy, b, rows}, {codes, cols, cols, rows}, {scales, 4, 4, rows}};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 3; ++i)  // a row of sum or y may take the place of the row it is made from
+      if (overlap(out[o], in[i]) && !(o < 2 && i < 2 && same_rows(out[o], in[i]))) return MXMOE_ERR_INVALID_ARG;
+    for (int i = 0; i < o; ++i)
+      if (overlap(out[o], out[i])) return MXMOE_ERR_INVALID_ARG;
+  }
+  NormArgs a;
+  a.x = x;
+  a.res = residual;
+  a.weight = weight;
+  a.sum = sum;
+  a.y = y;
+  a.codes = codes;
+  a.scales = scales;
+  a.ldx = ldx;
+  a.ldr = ldr;
+  a.lds = lds;
+  a.ldy = ldy;
+  a.eps = eps;
+  a.rows = rows;
+  a.cols = cols;
+  a.qmax = qmax;
+  return hip_status(launch_add_rms_norm(a, act, stream));
+}
+
 // -------------------------------------------------------- single linear
 namespace {
 struct LinWs { size_t plan, partial, aq, as, rsa, total; int qcap, fcap; int64_t pfloats; };
@@ -559,6 +627,103 @@ mxmoe_status mxmoe_linear_forward(const mxmoe_linear* L, mxmoe_dtype act, const 
                              nullptr, grid, narrow, xp, stream);
   if (e != hipSuccess) return MXMOE_ERR_HIP;
   return hip_status(launch_group_gemm(ga, 2, grid, narrow, stream));
+}
+
+mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const void* packed, int32_t m, const void* a,
+                                 int64_t lda, const float* a_scales, const void* bias, void* out, int64_t ldo,
+                                 hipStream_t stream) {
+  int kd;
+  mxmoe_status st = check_linear(L, &kd);
+  if (st != MXMOE_OK) return st;
+  if (!valid_dtype(act) || m < 0) return MXMOE_ERR_INVALID_ARG;
+  if (!decode_kind(kd) || m > MXMOE_DECODE_ROWS) return MXMOE_ERR_UNSUPPORTED;
+  if (m == 0) return MXMOE_OK;
+  const int es = kind_is_int(kd) ? 1 : 2;
+  if (!packed || !a || !out || (es == 1) != (a_scales != nullptr)) return MXMOE_ERR_INVALID_ARG;
+  if (lda < L->k || lda > kMaxPitch / es || ldo < L->n || ldo > kMaxPitch / 2) return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(packed, 256) || !aligned(a, 16) || (m > 1 && lda * es % 16) || !aligned(a_scales, 4) || !aligned(bias, 2) ||
+      !aligned(out, 2))
+    return MXMOE_ERR_INVALID_ARG;
+  const int64_t pb = (int64_t)packed_bytes_kind(kd, L->n, L->k);
+  const Rows o{out, 2 * ldo, 2 * (int64_t)L->n, m};
+  const Rows in[4] = {{packed, pb, pb, 1}, {a, es * lda, es * (int64_t)L->k, m}, {a_scales, 4, 4, m},
+                      {bias, 2 * (int64_t)L->n, 2 * (int64_t)L->n, 1}};
+  for (const Rows& i : in)
+    if (overlap(o, i)) return MXMOE_ERR_INVALID_ARG;
+  DecodeArgs p;
+  p.packed = reinterpret_cast<const uint8_t*>(packed);
+  p.wscale = kind_is_int(kd) ? reinterpret_cast<const float*>(p.packed + codes_bytes(kd, L->n, L->k)) : nullptr;
+  p.a = a;
+  p.a_scales = a_scales;
+  p.bias = bias;
+  p.out = out;
+  p.lda = lda;
+  p.ldo = ldo;
+  p.m = m;
+  p.n = L->n;
+  p.k = L->k;
+  return hip_status(launch_linear_decode(p, kd, act, stream));
+}
+
+// ------------------------------------------------------- balance loss
+namespace {
+struct BalWs { size_t counts, probs, total; int n_count, n_part; };
+BalWs bal_layout(int32_t T, int32_t E) {
+  BalWs w;
+  w.n_count = std::max(1, std::min(32, T / 512));
+  w.n_part = std::max(1, std::min(512, T / 16));
+  size_t o = 0;
+  w.counts = o; o = align256(o + 4 * (size_t)w.n_count * (E + 1));
+  w.probs = o; o = align256(o + 4 * (size_t)w.n_part * E);
+  w.total = o;
+  return w;
+}
+}  // namespace
+
+size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E) {
+  if (T < 0 || E <= 0 || E > kMaxE) return 0;
+  return bal_layout(T, E).total;
+}
+
+mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids, const uint8_t* token_mask, int32_t T,
+                                int32_t E, int32_t k, float alpha, int32_t* counts, float* probs, float* loss,
+                                float* grad, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (T < 0 || E <= 0 || E > kMaxE || k <= 0 || k > E || !(alpha - alpha == 0.f)) return MXMOE_ERR_INVALID_ARG;
+  if ((int64_t)T * k >= (1LL << 31)) return MXMOE_ERR_INVALID_ARG;
+  if (!counts || !probs || !loss || !workspace) return MXMOE_ERR_INVALID_ARG;
+  if (T > 0 && (!logits || !topk_ids)) return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(logits, 4) || !aligned(topk_ids, 4) || !aligned(counts, 4) || !aligned(probs, 4) || !aligned(loss, 4) ||
+      !aligned(grad, 4) || !aligned(workspace, 256))
+    return MXMOE_ERR_INVALID_ARG;
+  const BalWs w = bal_layout(T, E);
+  if (workspace_bytes < w.total) return MXMOE_ERR_WORKSPACE;
+  const int64_t lb = 4 * (int64_t)T * E, ib = 4 * (int64_t)T * k, eb = 4 * (int64_t)E, wb = (int64_t)w.total;
+  const int64_t some = T > 0 ? 1 : 0;
+  const Rows in[3] = {{logits, lb, lb, some}, {topk_ids, ib, ib, some}, {token_mask, T, T, some}};
+  const Rows out[5] = {{counts, eb, eb, 1}, {probs, eb, eb, 1}, {loss, 4, 4, 1}, {grad, lb, lb, some}, {workspace, wb, wb, 1}};
+  for (int o = 0; o < 5; ++o) {
+    for (int i = 0; i < 3; ++i)  // the gradient may take the logits' place
+      if (overlap(out[o], in[i]) && !(o == 3 && i == 0 && grad == logits)) return MXMOE_ERR_INVALID_ARG;
+    for (int i = 0; i < o; ++i)
+      if (overlap(out[o], out[i])) return MXMOE_ERR_INVALID_ARG;
+  }
+  BalanceArgs a;
+  a.logits = logits;
+  a.ids = topk_ids;
+  a.mask = token_mask;
+  a.counts = counts;
+  a.probs = probs;
+  a.loss = loss;
+  a.grad = grad;
+  a.part_counts = at<int32_t>(workspace, w.counts);
+  a.part_probs = at<float>(workspace, w.probs);
+  a.T = T;
+  a.E = E;
+  a.k = k;
+  a.n_count = w.n_count;
+  a.n_part = w.n_part;
+  a.alpha = alpha;
+  return hip_status(launch_balance_loss(a, stream));
 }
 
 // -------------------------------------------------------- MoE block

@@ -539,4 +539,47 @@ int group_gemm_grid(int device);
 hipError_t launch_combine(const void* slots, int slot16, const int32_t* ids, int T, int k, int E, int n_sh,
                           int H, int act, void* y, hipStream_t s);
 
+// Residual addition, RMS norm and 8-bit rows (norm.hip).  Rows of 16-bit values
+// with strides in elements; res, sum, y and codes / scales (qmax 0) may be null.
+struct NormArgs {
+  const void *x, *res, *weight;
+  void *sum, *y;
+  int8_t* codes;
+  float* scales;
+  int64_t ldx, ldr, lds, ldy;
+  double eps;
+  int32_t rows, cols, qmax;
+};
+hipError_t launch_add_rms_norm(const NormArgs& a, int act, hipStream_t s);
+
+// One packed linear on the few rows of a decode step (decode.hip): w4g128 on
+// 16-bit rows, w8a8 and fp8 on rows of codes with a scale each (lda in elements).
+struct DecodeArgs {
+  const uint8_t* packed;
+  const float* wscale;  // per-channel scales (w8a8, fp8)
+  const void* a;
+  const float* a_scales;
+  const void* bias;
+  void* out;
+  int64_t lda, ldo;
+  int32_t m, n, k;
+};
+bool decode_kind(int kind);
+hipError_t launch_linear_decode(const DecodeArgs& p, int kind, int act, hipStream_t s);
+
+// Balance loss of the router (balance.hip).  n_count workgroups count, n_part
+// take the tokens' softmax.
+struct BalanceArgs {
+  const float* logits;
+  const int32_t* ids;
+  const uint8_t* mask;
+  int32_t* counts;
+  float *probs, *loss, *grad;
+  int32_t* part_counts;  // [n_count][E + 1]: the share's counts and kept tokens
+  float* part_probs;     // [n_part][E]
+  int32_t T, E, k, n_count, n_part;
+  float alpha;
+};
+hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s);
+
 }  // namespace mxmoe

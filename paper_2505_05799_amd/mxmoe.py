@@ -64,9 +64,11 @@ EXPORTS = [
     "mxmoe_block_table_bytes", "mxmoe_block_table_fill", "mxmoe_workspace_bytes", "mxmoe_moe_forward",
     "mxmoe_moe_forward_ex", "mxmoe_workspace_layout", "mxmoe_status_string", "mxmoe_version",
     "mxmoe_moe_forward_noalloc", "mxmoe_set_tile_costs", "mxmoe_get_tile_costs",
+    "mxmoe_add_rms_norm", "mxmoe_linear_decode", "mxmoe_balance_workspace_bytes", "mxmoe_balance_loss",
 ]
 TILE_COST_SHAPE = (2, 11, 4, 4)     # [phase][scheme][configuration][a, bs, bu, h], MXMOE_TILE_COST_ENTRIES
 NOALLOC_SCRATCH_BYTES = 128 << 20   # MXMOE_NOALLOC_SCRATCH_BYTES
+DECODE_ROWS = 64                    # MXMOE_DECODE_ROWS
 
 _lib = None
 
@@ -103,6 +105,11 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "mxmoe_version": (i32, []),
         "mxmoe_set_tile_costs": (C.c_int, [vp, i32]),
         "mxmoe_get_tile_costs": (C.c_int, [vp, i32]),
+        "mxmoe_add_rms_norm": (C.c_int, [vp, i64, vp, i64, vp, C.c_int, i32, i32, C.c_double, vp, i64, vp, i64, i32, vp, vp,
+                                         vp]),
+        "mxmoe_linear_decode": (C.c_int, [PL, C.c_int, vp, i32, vp, i64, vp, vp, vp, i64, vp]),
+        "mxmoe_balance_workspace_bytes": (sz, [i32, i32]),
+        "mxmoe_balance_loss": (C.c_int, [vp, vp, vp, i32, i32, i32, C.c_float, vp, vp, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -313,6 +320,176 @@ def linear_forward(pl: PackedLinear, a, stream=None, return_ws: bool = False):
     _check(lib.mxmoe_linear_forward(C.byref(pl.L), act_code(pl.act), _ptr(pl.buf), m, _ptr(a.contiguous()),
                                     _ptr(out), _ptr(ws), wsb, _stream_ptr(stream)), "mxmoe_linear_forward")
     return (out, ws) if return_ws else out
+
+
+# ------------------------------------------------- operators around the block
+def _run_on(device, stream, body, used):
+    """body(stream handle) with `device` current, on `stream` (default: the
+    device's current one); what body allocates belongs to that stream, and the
+    tensors `used` are kept until its work on them is done."""
+    torch = _torch()
+    if stream is None:
+        if device.index == torch.cuda.current_device():
+            return body(torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(device):
+            return body(torch.cuda.current_stream().cuda_stream)
+    if stream.device != device:
+        raise ValueError(f"a stream of {stream.device} for tensors on {device}")
+    with torch.cuda.stream(stream):
+        out = body(stream.cuda_stream)
+    for t in used:
+        if t is not None:
+            t.record_stream(stream)
+    return out
+
+
+def _want(t, name, dtype, shape, device, strided: bool = False):
+    """Raise ValueError unless t is a tensor of the dtype(s), shape and device;
+    strided: rows of any stride (elements of a row side by side), else dense."""
+    if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
+        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    if strided:
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the elements of a row have to be side by side")
+        if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+            raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+
+
+def _cuda_rows(t, name):
+    """Device of a [rows, cols] tensor on a GPU."""
+    if t.dim() != 2 or t.device.type != "cuda":
+        raise ValueError(f"{name}: a [rows, columns] tensor on a GPU is expected, got {tuple(t.shape)} on {t.device}")
+    return t.device
+
+
+def _ld(t) -> int:
+    """Row stride of a [rows, cols] tensor (a single row's own length)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, want_y: bool = True, sum_out=None,
+                 stream=None):
+    """z = x + residual, y = RMS norm of z times weight, and y's 8-bit rows
+    (mxmoe_add_rms_norm): returns (y, z, codes, scales).
+
+    x, residual [rows, cols] fp16 or bf16, rows of any stride; weight [cols].
+    z is None without a residual, else a new tensor or sum_out (which may be
+    residual or x themselves); y is None with want_y=False.  qmax 127: int8 codes,
+    448: FP8 e4m3 bytes in an int8 tensor, with fp32 scales per row (linear_decode
+    takes them); 0: neither."""
+    torch = _torch()
+    lib = load_library()
+    dev = _cuda_rows(x, "x")
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"x: {x.dtype}, expected bfloat16 or float16")
+    rows, cols = x.shape
+    _want(x, "x", x.dtype, x.shape, dev, strided=True)
+    _want(weight, "weight", x.dtype, (cols,), dev)
+    if residual is not None:
+        _want(residual, "residual", x.dtype, x.shape, dev, strided=True)
+    if sum_out is not None:
+        if residual is None:
+            raise ValueError("sum_out: there is no sum without a residual")
+        _want(sum_out, "sum_out", x.dtype, x.shape, dev, strided=True)
+
+    def body(s):
+        z = sum_out
+        if residual is not None and z is None:
+            z = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+        y = torch.empty((rows, cols), dtype=x.dtype, device=dev) if want_y else None
+        codes = scales = None
+        if qmax:
+            codes = torch.empty((rows, cols), dtype=torch.int8, device=dev)
+            scales = torch.empty(rows, dtype=torch.float32, device=dev)
+        _check(lib.mxmoe_add_rms_norm(
+            x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(), 0 if residual is None else _ld(residual),
+            weight.data_ptr(), BF16 if x.dtype == torch.bfloat16 else F16, rows, cols, eps,
+            None if z is None else z.data_ptr(), 0 if z is None else _ld(z), None if y is None else y.data_ptr(), cols, qmax,
+            None if codes is None else codes.data_ptr(), None if scales is None else scales.data_ptr(), s),
+            "mxmoe_add_rms_norm")
+        return y, z, codes, scales
+
+    return _run_on(dev, stream, body, (x, residual, weight, sum_out))
+
+
+def linear_decode(pl: PackedLinear, a, scales=None, bias=None, out=None, stream=None):
+    """out = a W^T + bias for at most DECODE_ROWS rows, in the activation dtype
+    (mxmoe_linear_decode).  w4g128: a fp16 / bf16 [m, k]; w8a8 and fp8: a the
+    codes [m, k] and scales [m] of act_quant or add_rms_norm.  Rows of any stride
+    (copied if not 16-byte aligned)."""
+    torch = _torch()
+    lib = load_library()
+    dev = _cuda_rows(a, "a")
+    q = pl.q
+    m = a.shape[0]
+    act = torch.bfloat16 if pl.act == "bf16" else torch.float16
+    coded = q.scheme.a_bits < 16
+    _want(a, "a", (torch.int8, torch.uint8) if coded else act, (m, q.k), dev, strided=True)
+    if pl.buf.device != dev:
+        raise ValueError(f"a: on {dev}, the packed weights on {pl.buf.device}")
+    if coded != (scales is not None):
+        raise ValueError(f"{q.scheme.name}: scales are the rows' of 8-bit codes")
+    if scales is not None:
+        _want(scales, "scales", torch.float32, (m,), dev)
+    if bias is not None:
+        _want(bias, "bias", act, (q.n,), dev)
+    if out is not None:
+        _want(out, "out", act, (m, q.n), dev, strided=True)
+
+    def body(s):
+        rows = a
+        if rows.data_ptr() % 16 or (m > 1 and rows.stride(0) * rows.element_size() % 16):
+            rows = rows.clone(memory_format=torch.contiguous_format)
+        o = torch.empty((m, q.n), dtype=act, device=dev) if out is None else out
+        _check(lib.mxmoe_linear_decode(
+            C.byref(pl.L), BF16 if pl.act == "bf16" else F16, pl.buf.data_ptr(), m, rows.data_ptr(), _ld(rows),
+            None if scales is None else scales.data_ptr(), None if bias is None else bias.data_ptr(), o.data_ptr(), _ld(o), s),
+            "mxmoe_linear_decode")
+        return o
+
+    return _run_on(dev, stream, body, (a, scales, bias, out, pl.buf))
+
+
+def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_grad: bool = True, stream=None):
+    """Balance loss of the router (mxmoe_balance_loss): (loss [], counts int32
+    [E], mean probabilities [E], gradient of the logits [T, E] or None).
+
+    logits fp32 [T, E]; topk_ids int32 [T, k]; token_mask bool or uint8 [T], False
+    for padding.  The gradient enters a backward pass as
+    ``torch.autograd.backward([out, logits], [None, grad])``; alpha takes its
+    factor."""
+    torch = _torch()
+    lib = load_library()
+    dev = _cuda_rows(logits, "logits")
+    T, E = logits.shape
+    _want(logits, "logits", torch.float32, logits.shape, dev)
+    if topk_ids.dim() != 2:
+        raise ValueError(f"topk_ids: shape {tuple(topk_ids.shape)}, expected [T, k]")
+    k = topk_ids.shape[1]
+    _want(topk_ids, "topk_ids", torch.int32, (T, k), dev)
+    if token_mask is not None:
+        _want(token_mask, "token_mask", (torch.bool, torch.uint8), (T,), dev)
+
+    def body(s):
+        counts = torch.empty(E, dtype=torch.int32, device=dev)
+        probs = torch.empty(E, dtype=torch.float32, device=dev)
+        loss = torch.empty((), dtype=torch.float32, device=dev)
+        grad = torch.empty((T, E), dtype=torch.float32, device=dev) if want_grad else None
+        wsb = lib.mxmoe_balance_workspace_bytes(T, E)
+        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+        _check(lib.mxmoe_balance_loss(
+            logits.data_ptr(), topk_ids.data_ptr(), None if token_mask is None else token_mask.data_ptr(), T, E, k, alpha,
+            counts.data_ptr(), probs.data_ptr(), loss.data_ptr(), None if grad is None else grad.data_ptr(), ws.data_ptr(),
+            wsb, s), "mxmoe_balance_loss")
+        return loss, counts, probs, grad
+
+    return _run_on(dev, stream, body, (logits, topk_ids, token_mask))
 
 
 # --------------------------------------------------------------- routing
