@@ -252,7 +252,8 @@ MXMOE_API mxmoe_status mxmoe_act_quant(const void* a, mxmoe_dtype act, int32_t r
  * are multiples of 16 bytes take the wide path, others the same results.  sum and
  * y may each be x or residual itself (same pointer and stride), but not share
  * bytes with them otherwise, nor with each other, weight, codes or scales.
- * eps > 0, cols <= 2^24.  Errors: INVALID_ARG, UNSUPPORTED, HIP.             */
+ * 1e-30 <= eps <= 1e30 (the factor is finite), cols <= 2^24.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                     */
 MXMOE_API mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr,
                                 const void* weight, mxmoe_dtype act, int32_t rows, int32_t cols,
                                 double eps, void* sum, int64_t lds, void* y, int64_t ldy,

@@ -65,7 +65,7 @@ def check_norm(x, res, w, act, qmax, got, eps=1e-6):
 
 NORM_SHAPES = [(1, 1), (3, 2), (2, 7), (1, 8), (5, 64), (4, 127), (7, 128), (1, 513), (9, 1024), (1, 2048), (33, 2056),
                (2, 3584), (130, 4096), (3, 4104), (5, 7168), (2, 16384), (1, 16392), (1, 32768), (2, 33000), (1, 70001),
-               (700, 72), (1500, 256), (4100, 128)]
+               (700, 72), (1500, 256), (4100, 128), (4097, 1000), (4096, 1600), (4099, 2056), (513, 5000), (512, 16000)]
 
 
 @pytest.mark.parametrize("act", ["bf16", "fp16"])

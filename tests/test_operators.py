@@ -129,7 +129,7 @@ def norm_call(lib, x=at(1), ldx=64, res=at(2), ldr=64, w=at(3), act=M.BF16, rows
 
 @pytest.mark.parametrize("bad", [
     dict(x=None), dict(w=None), dict(act=2), dict(rows=-1), dict(cols=0), dict(eps=0.0), dict(eps=-1.0),
-    dict(eps=float("nan")), dict(eps=float("inf")), dict(ldx=63), dict(ldr=63), dict(lds=63), dict(ldy=63),
+    dict(eps=float("nan")), dict(eps=1e-31), dict(eps=float("inf")), dict(ldx=63), dict(ldr=63), dict(lds=63), dict(ldy=63),
     dict(ldx=1 << 40), dict(ldy=1 << 62), dict(res=None), dict(qmax=127, codes=None), dict(qmax=127, scales=None),
     dict(qmax=0), dict(qmax=0, codes=None), dict(qmax=0, codes=None, scales=None, y=None), dict(x=at(1, 1)),
     dict(w=at(3, 1)), dict(scales=at(7, 2)),
