@@ -9,6 +9,10 @@
 //           against ones; fp16: 1024 + q, from which a packed subtraction of
 //           1024 + z leaves q - z.  Both are exact in their dtype.
 //   w8a8    int8 MFMA, int32 sums; fp8  FP8 MFMA, fp32 sums; times s_a s_w at the end.
+//
+// A workgroup takes 16 channels; its wavefronts take the k blocks in turn and meet
+// once, through LDS, in wavefront order.  Rows past the last one repeat it (their sums
+// are dropped).
 #include "mxmoe_internal.h"
 
 namespace mxmoe {
@@ -22,90 +26,279 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-template <int ACT> __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+#define DEC_INL __device__ __attribute__((always_inline)) inline
+
+template <int ACT> DEC_INL f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (ACT == MXMOE_BF16)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-template <int ACT> __device__ inline float act_load(const uint16_t* p) {
+template <int ACT> DEC_INL float act_load(const uint16_t* p) {
   if constexpr (ACT == MXMOE_BF16) return __uint_as_float((uint32_t)*p << 16);
   else return (float)__builtin_bit_cast(_Float16, *p);
 }
-template <int ACT> __device__ inline uint16_t act_round(float f) {
+template <int ACT> DEC_INL uint16_t act_round(float f) {
   asm("" : "+v"(f));  // the fp32 value is rounded, not the expression it came from
   if constexpr (ACT == MXMOE_BF16) return __builtin_bit_cast(uint16_t, (__bf16)f);
   else return __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
-// One wavefront per 16 channels and 16 rows.
-template <int KD, int ACT>
-__global__ void __launch_bounds__(64) decode_kernel(DecodeArgs p) {
-  const int lane = threadIdx.x, li = lane & 15, qd = lane >> 4;
-  const int kb_n = p.k / 128;
-  const int row = min((int)blockIdx.y * 16 + li, p.m - 1);  // rows past the last repeat it: their sums are dropped
-  const uint8_t* wb = p.packed + (int64_t)blockIdx.x * kb_n * block_bytes(KD);
-  f32x4 tot = {0.f, 0.f, 0.f, 0.f};
-  i32x4 itot = {0, 0, 0, 0};
-  for (int kb = 0; kb < kb_n; ++kb, wb += block_bytes(KD)) {
-    const u32x4* wl = reinterpret_cast<const u32x4*>(wb + lane * lane_bytes(KD));
-    if constexpr (KD == K_W4G) {
-      const u32x4 d = wl[0];
-      const uint32_t sz = reinterpret_cast<const uint32_t*>(wb + 64 * lane_bytes(KD))[li];
-      const float s = (float)__builtin_bit_cast(_Float16, (uint16_t)sz);
-      const _Float16 z = __builtin_bit_cast(_Float16, (uint16_t)(sz >> 16));
-      const u32x4* ar = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(p.a) + row * p.lda + kb * 128);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f}, rs = {0.f, 0.f, 0.f, 0.f};
+// What a lane holds of one k block: its weights (and the group's scale and zero point),
+// and the rows of a fragment (16-byte pieces: four of 16-bit rows, two of codes).
+template <int KD> struct Wgt {
+  static constexpr int N = lane_bytes(KD) / 16;
+  u32x4 w[N];
+  uint32_t sz;
+  // block: the fragment block of the lane's channels and this k block
+  DEC_INL void load(const uint8_t* block, int lane) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x4 a = ar[4 * j + qd];
-        u32x4 b;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t v = (d[j] >> (4 * i)) & 0x000F000Fu;
-          if constexpr (ACT == MXMOE_BF16) {
-            v |= 0x43004300u;
-          } else {
-            const _Float16 off = (_Float16)1024.f + z;
-            v = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v | 0x64006400u) - f16x2{off, off});
-          }
-          b[i] = v;
-        }
-        acc = mfma16<ACT>(a, b, acc);
-        if constexpr (ACT == MXMOE_BF16) rs = mfma16<ACT>(a, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, rs);
-      }
-      if constexpr (ACT == MXMOE_BF16) acc -= (128.f + (float)z) * rs;
-      tot += s * acc;
-    } else {
-      const u32x4* ar = reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(p.a) + row * p.lda + kb * 128);
-      const u32x4 a0 = ar[qd], a1 = ar[4 + qd], w0 = wl[0], w1 = wl[1];
-      if constexpr (KD == K_W8A8) {
-        itot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a0), __builtin_bit_cast(i32x4, w0), itot, 0, 0, 0);
-        itot = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a1), __builtin_bit_cast(i32x4, w1), itot, 0, 0, 0);
-      } else {
-        const i32x8 A = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-        const i32x8 B = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
-        tot = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, tot, 0, 0, 0, 127, 0, 127);
-      }
-    }
+    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const u32x4*>(block + lane * lane_bytes(KD))[i];
+    if constexpr (KD == K_W4G) sz = reinterpret_cast<const uint32_t*>(block + 64 * lane_bytes(KD))[lane & 15];
   }
-  const int ch = blockIdx.x * 16 + li;
-  const float bias = p.bias ? act_load<ACT>(reinterpret_cast<const uint16_t*>(p.bias) + ch) : 0.f;
+};
+template <int KD> constexpr int kPieces = KD == K_W4G ? 4 : 2;
+template <int KD, int MF> using Rows = u32x4[MF][kPieces<KD>];
+template <int KD> struct AccT { using type = f32x4; };
+template <> struct AccT<K_W8A8> { using type = i32x4; };
+template <int KD> using Acc = typename AccT<KD>::type;
+
+// Row sums of a k block over the group (bf16 rows of w4g128), in the accumulators' layout.
+template <int KD, int ACT, int MF> DEC_INL void row_sums(const Rows<KD, MF>& a, f32x4 (&rs)[MF]) {
+  if constexpr (KD == K_W4G && ACT == MXMOE_BF16) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = blockIdx.y * 16 + 4 * qd + i;
-    if (r >= p.m) continue;
-    float v = KD == K_W8A8 ? (float)itot[i] : tot[i];
-    if constexpr (KD != K_W4G) v = v * p.a_scales[r] * p.wscale[ch];
-    reinterpret_cast<uint16_t*>(p.out)[r * p.ldo + ch] = act_round<ACT>(v + bias);
+    for (int f = 0; f < MF; ++f) {
+      rs[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        rs[f] = mfma16<ACT>(a[f][j], u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, rs[f]);
+    }
   }
 }
 
-template <int KD> hipError_t launch_kind(const DecodeArgs& p, int act, hipStream_t s) {
-  const dim3 grid(p.n / 16, (p.m + 15) / 16);
-  if (act == MXMOE_BF16) hipLaunchKernelGGL((decode_kernel<KD, MXMOE_BF16>), grid, dim3(64), 0, s, p);
-  else hipLaunchKernelGGL((decode_kernel<KD, MXMOE_F16>), grid, dim3(64), 0, s, p);
+template <int KD, int ACT, int MF>
+DEC_INL void use_block(const Wgt<KD>& s, const Rows<KD, MF>& a, const f32x4 (&rs)[MF], Acc<KD> (&tot)[MF]) {
+  if constexpr (KD == K_W4G) {
+    const float sc = (float)__builtin_bit_cast(_Float16, (uint16_t)s.sz);
+    const _Float16 z = __builtin_bit_cast(_Float16, (uint16_t)(s.sz >> 16));
+    f32x4 acc[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u32x4 b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t v = (s.w[0][j] >> (4 * i)) & 0x000F000Fu;
+        if constexpr (ACT == MXMOE_BF16) {
+          v |= 0x43004300u;
+        } else {
+          const _Float16 off = (_Float16)1024.f + z;
+          v = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v | 0x64006400u) - f16x2{off, off});
+        }
+        b[i] = v;
+      }
+#pragma unroll
+      for (int f = 0; f < MF; ++f) acc[f] = mfma16<ACT>(a[f][j], b, acc[f]);
+    }
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+      if constexpr (ACT == MXMOE_BF16) acc[f] -= (128.f + (float)z) * rs[f];
+      tot[f] += sc * acc[f];
+    }
+  } else if constexpr (KD == K_W8A8) {
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        tot[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a[f][j]), __builtin_bit_cast(i32x4, s.w[j]), tot[f], 0, 0, 0);
+  } else {
+    auto wide = [](u32x4 l, u32x4 h) { return i32x8{(int)l[0], (int)l[1], (int)l[2], (int)l[3], (int)h[0], (int)h[1], (int)h[2], (int)h[3]}; };
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+      tot[f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(a[f][0], a[f][1]), wide(s.w[0], s.w[1]), tot[f], 0, 0, 0, 127, 0, 127);
+  }
+}
+
+// The wavefronts' sums of one block of channels, added in wavefront order, to the
+// output.  red: [NW][MF][64] accumulators in LDS.  Output o = 64 (4 f + i) + l:
+// fragment f, row 4 (l / 16) + i of it, channel l % 16.
+template <int KD, int ACT, int MF, int NW>
+DEC_INL void write_out(const DecodeArgs& p, const Acc<KD>* red, int nb, int t, int threads) {
+  for (int o = t; o < MF * 256; o += threads) {
+    const int l = o & 63, i = (o >> 6) & 3, f = o >> 8, r = 16 * f + 4 * (l >> 4) + i;
+    if (r >= p.m) continue;
+    auto v = red[f * 64 + l][i];
+#pragma unroll
+    for (int j = 1; j < NW; ++j) v += red[(j * MF + f) * 64 + l][i];
+    const int c = nb * 16 + (l & 15);
+    float x = (float)v;
+    if constexpr (KD != K_W4G) x = x * p.a_scales[r] * p.wscale[c];
+    if (p.bias) x += act_load<ACT>(reinterpret_cast<const uint16_t*>(p.bias) + c);
+    reinterpret_cast<uint16_t*>(p.out)[(int64_t)r * p.ldo + c] = act_round<ACT>(x);
+  }
+}
+
+// ---- At most 16 rows, straight from memory.  NW wavefronts share 16 channels; a
+// wavefront's next k block is asked for before this one is used.  One token through
+// 4096 x 4096 w4g128 3.8 us a launch in a graph, one wavefront for all k blocks 10.7; 20480 x
+// 3584 9.8 us, 4.0 TB/s with the weights in the Infinity Cache.
+template <int KD, int ACT, int NW>
+__global__ void __launch_bounds__(64 * NW) decode_kernel(DecodeArgs p) {
+  __shared__ Acc<KD> red[NW * 64];
+  constexpr int ES = KD == K_W4G ? 2 : 1;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, qd = lane >> 4;
+  const int kbs = p.k / 128;
+  const uint8_t* wb = p.packed + (int64_t)blockIdx.x * kbs * block_bytes(KD);
+  const uint8_t* ar = reinterpret_cast<const uint8_t*>(p.a) + (int64_t)min(li, p.m - 1) * p.lda * ES + 16 * qd;
+  Acc<KD> tot[1] = {Acc<KD>{0, 0, 0, 0}};
+  struct Step { Wgt<KD> w; Rows<KD, 1> a; } cur, nxt;
+  auto load = [&](Step& s, int kb) {
+    s.w.load(wb + (int64_t)kb * block_bytes(KD), lane);
+#pragma unroll
+    for (int j = 0; j < kPieces<KD>; ++j)
+      s.a[0][j] = *reinterpret_cast<const u32x4*>(ar + (int64_t)kb * (64 * kPieces<KD>) + 64 * j);
+  };
+  if (w < kbs) load(cur, w);
+  for (int kb = w; kb < kbs; kb += NW) {
+    if (kb + NW < kbs) load(nxt, kb + NW);
+    f32x4 rs[1];
+    row_sums<KD, ACT, 1>(cur.a, rs);
+    use_block<KD, ACT, 1>(cur.w, cur.a, rs, tot);
+    cur = nxt;
+  }
+  red[w * 64 + lane] = tot[0];
+  __syncthreads();
+  write_out<KD, ACT, 1, NW>(p, red, blockIdx.x, tid, 64 * NW);
+}
+
+// ---- Rows through LDS.  Fragments of many rows straight from memory are 64-byte
+// pieces of as many rows, which the cache serves at a quarter of its rate (64 rows of
+// fp8, 4096 x 14336: 28.7 us whatever n).  Here 8 wavefronts bring KC k blocks of all rows into
+// LDS, row by row in whole lines, and share them: WN groups of wavefronts take NB blocks of
+// 16 channels each, the WK wavefronts of a group one k block each.  Piece q of
+// row r lies at q ^ (r % 16), so that both the writes along a row and the fragment reads
+// across rows are free of bank conflicts.  The next k blocks' rows and weights are on
+// their way in registers meanwhile.  Workgroups start at different k blocks: all at the
+// same lines, they waited for the same few channels of the L2 (that fp8 case 26.7 -> 22.6 us).
+// What it is bound by then: the rows' way from the L2, 13 TB/s over all CUs.
+template <int KD, int ACT, int MF, int WN, int NB>
+__global__ void __launch_bounds__(512) decode_rows_kernel(DecodeArgs p) {
+  constexpr int NW = 8, WK = NW / WN, KC = WK, PP = 4 * kPieces<KD>, RP = KC * PP, RS = 512 / RP, NPT = 16 * MF / RS;
+  constexpr int ES = KD == K_W4G ? 2 : 1;
+  constexpr int kStage = 16 * MF * RP, kRed = NW * MF * 64;
+  static_assert(512 % RP == 0 && NPT >= 1 && (16 * MF) % RS == 0, "staging covers the rows");
+  __shared__ u32x4 buf[kStage > kRed ? kStage : kRed];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, qd = lane >> 4;
+  const int wn = w / WK, wk = w % WK;
+  const int kbs = p.k / 128, nbs = p.n / 16, chunks = (kbs + KC - 1) / KC;
+  const int nb0 = (int)blockIdx.x * (WN * NB) + wn * NB;
+  const uint8_t* wb[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) wb[b] = p.packed + (int64_t)min(nb0 + b, nbs - 1) * kbs * block_bytes(KD);
+  const int sq = tid % RP, sr = tid / RP;
+  const uint8_t* src = reinterpret_cast<const uint8_t*>(p.a) + sr * p.lda * ES + 16 * sq;
+  u32x4 st[NPT];
+  auto stage_load = [&](int c) {
+    const bool in = c * RP + sq < kbs * PP;
+#pragma unroll
+    for (int i = 0; i < NPT; ++i)
+      if (in && sr + RS * i < p.m) st[i] = *reinterpret_cast<const u32x4*>(src + (int64_t)(RS * i) * p.lda * ES + (int64_t)c * (16 * RP));
+  };
+  Wgt<KD> cur[NB], nxt[NB];
+  auto wgt_load = [&](Wgt<KD> (&g)[NB], int c) {
+    const int kb = min(c * KC + wk, kbs - 1);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) g[b].load(wb[b] + (int64_t)kb * block_bytes(KD), lane);
+  };
+  Acc<KD> tot[NB][MF];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int f = 0; f < MF; ++f) tot[b][f] = Acc<KD>{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < NPT; ++i) st[i] = u32x4{0u, 0u, 0u, 0u};
+  int c = (int)(blockIdx.x >> 3) % chunks;
+  wgt_load(cur, c);
+  stage_load(c);
+  for (int left = chunks; left > 0; --left) {
+    const int next = c + 1 < chunks ? c + 1 : 0;
+    __syncthreads();  // the last chunk's fragments are read
+#pragma unroll
+    for (int i = 0; i < NPT; ++i) {
+      const int r = sr + RS * i;
+      buf[r * RP + (sq ^ (r & 15))] = st[i];
+    }
+    __syncthreads();
+    if (left > 1) {
+      wgt_load(nxt, next);
+      stage_load(next);
+    }
+    if (c * KC + wk < kbs) {
+      Rows<KD, MF> a;
+#pragma unroll
+      for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int j = 0; j < kPieces<KD>; ++j) a[f][j] = buf[(16 * f + li) * RP + ((wk * PP + 4 * j + qd) ^ li)];
+      f32x4 rs[MF];
+      row_sums<KD, ACT, MF>(a, rs);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) use_block<KD, ACT, MF>(cur[b], a, rs, tot[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) cur[b] = nxt[b];
+    c = next;
+  }
+  Acc<KD>* red = reinterpret_cast<Acc<KD>*>(buf);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < MF; ++f) red[(w * MF + f) * 64 + lane] = tot[b][f];
+    __syncthreads();
+    if (nb0 + b < nbs) write_out<KD, ACT, MF, WK>(p, red + wn * WK * MF * 64, nb0 + b, tid - wn * WK * 64, WK * 64);
+  }
+}
+
+template <int KD, int ACT, int MF, int WN, int NB> hipError_t go_rows(const DecodeArgs& p, hipStream_t s) {
+  const int per = WN * NB;
+  hipLaunchKernelGGL((decode_rows_kernel<KD, ACT, MF, WN, NB>), dim3((p.n / 16 + per - 1) / per), dim3(512), 0, s, p);
   return hipGetLastError();
+}
+template <int KD, int ACT, int NW> hipError_t go_direct(const DecodeArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL((decode_kernel<KD, ACT, NW>), dim3(p.n / 16), dim3(64 * NW), 0, s, p);
+  return hipGetLastError();
+}
+// (nb blocks of 16 channels; us of the forms beside each other, wavefronts x channel blocks)
+template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, hipStream_t s) {
+  const int nb = p.n / 16, kbs = p.k / 128;
+  if constexpr (MF == 1) {
+    // Few rows straight from memory: codes up to 16 (16 x 4096 x 14336 fp8 10.7, through LDS
+    // 12.5), 16-bit rows, twice the pieces, up to 8 (8 and 16 x 4096 x 4096 5.0 and 6.3,
+    // through LDS 5.0 and 5.5), 2 where many workgroups bring the same rows (4 and 16 x 20480 x
+    // 3584 11.3 and 19.1, LDS 10.5 and 11.4).  16 wavefronts where few workgroups have much
+    // to read (1 x 4096 x 14336 8.7, 8 wavefronts 10.1; 1 x 20480 x 3584 12.0 and 9.7).
+    if (KD != K_W4G || p.m <= (nb > 512 ? 2 : 8)) {
+      if (KD == K_W4G && nb <= 256 && kbs >= 32) return go_direct<KD, ACT, 16>(p, s);
+      return go_direct<KD, ACT, 8>(p, s);
+    }
+    if constexpr (KD == K_W4G) return nb <= 512 ? go_rows<KD, ACT, 1, 1, 1>(p, s) : go_rows<KD, ACT, 1, 2, 1>(p, s);
+  } else {
+    // A workgroup of its own for every 16 channels as long as that is one round of the 256 CUs;
+    // beyond, more channels to a workgroup, so that the rows come in once for all of them:
+    // 64 x 20480 x 3584 w4g128 with 1, 2, 4 and 6 blocks of channels 54, 37, 33 and 23.
+    if (nb <= 256) return go_rows<KD, ACT, MF, 1, 1>(p, s);
+    if (KD != K_W4G || nb <= 512) return go_rows<KD, ACT, MF, 2, 1>(p, s);
+    if constexpr (KD == K_W4G) return nb <= 1024 ? go_rows<KD, ACT, MF, 2, 2>(p, s) : go_rows<KD, ACT, MF, 2, 3>(p, s);
+  }
+}
+template <int KD, int ACT> hipError_t launch_act(const DecodeArgs& p, hipStream_t s) {
+  if (p.m <= 16) return launch_rows<KD, ACT, 1>(p, s);
+  if (p.m <= 32) return launch_rows<KD, ACT, 2>(p, s);
+  return launch_rows<KD, ACT, 4>(p, s);
+}
+template <int KD> hipError_t launch_kind(const DecodeArgs& p, int act, hipStream_t s) {
+  return act == MXMOE_BF16 ? launch_act<KD, MXMOE_BF16>(p, s) : launch_act<KD, MXMOE_F16>(p, s);
 }
 
 }  // namespace
