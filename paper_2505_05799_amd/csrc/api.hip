@@ -439,7 +439,7 @@ mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual
                                 mxmoe_dtype act, int32_t rows, int32_t cols, double eps, void* sum, int64_t lds,
                                 void* y, int64_t ldy, int32_t qmax, int8_t* codes, float* scales,
                                 hipStream_t stream) {
-  if (!valid_dtype(act) || rows < 0 || cols <= 0 || !(eps > 0.0) || !(eps < 1e300)) return MXMOE_ERR_INVALID_ARG;
+  if (!valid_dtype(act) || rows < 0 || cols <= 0 || !(eps >= 1e-30) || !(eps <= 1e30)) return MXMOE_ERR_INVALID_ARG;
   if (qmax != 0 && qmax != 127 && qmax != kQmaxF8) return MXMOE_ERR_UNSUPPORTED;
   if (cols > kMaxNormCols) return MXMOE_ERR_UNSUPPORTED;
   if (rows == 0) return MXMOE_OK;
@@ -666,12 +666,17 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
 }
 
 // ------------------------------------------------------- balance loss
+#define BAL_COUNT 32
+#define BAL_SMALL 16384
+#define BAL_PART 512
 namespace {
 struct BalWs { size_t counts, probs, total; int n_count, n_part; };
 BalWs bal_layout(int32_t T, int32_t E) {
   BalWs w;
-  w.n_count = std::max(1, std::min(32, T / 512));
-  w.n_part = std::max(1, std::min(512, T / 16));
+  // (n_part 0: one workgroup does everything)
+  const int64_t logits = (int64_t)T * E;
+  w.n_count = std::max(1, std::min(BAL_COUNT, T / 512));
+  w.n_part = logits <= BAL_SMALL ? 0 : (int)std::min<int64_t>(BAL_PART, (logits + 2047) / 2048);
   size_t o = 0;
   w.counts = o; o = align256(o + 4 * (size_t)w.n_count * (E + 1));
   w.probs = o; o = align256(o + 4 * (size_t)w.n_part * E);

@@ -568,7 +568,7 @@ bool decode_kind(int kind);
 hipError_t launch_linear_decode(const DecodeArgs& p, int kind, int act, hipStream_t s);
 
 // Balance loss of the router (balance.hip).  n_count workgroups count, n_part
-// take the tokens' softmax.
+// take the tokens' softmax (0: one workgroup does everything).
 struct BalanceArgs {
   const float* logits;
   const int32_t* ids;
