@@ -190,7 +190,8 @@ MXMOE_API mxmoe_status mxmoe_router_topk(const float* logits, int32_t T, int32_t
                                int32_t* topk_ids, float* topk_w, float* shared_w,
                                hipStream_t stream);
 
-/* Workspace bytes of mxmoe_balance_loss (0 for invalid sizes).               */
+/* Workspace bytes of mxmoe_balance_loss for any top-k; 0 for small batches (they
+ * need no workspace) and for invalid sizes.                                  */
 MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
 
 /* Balance loss of the router, with the experts' counts and the gradient of the
@@ -213,8 +214,9 @@ MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
  *   grad  : fp32 [T, E], or NULL if not wanted; may be `logits` itself
  * With no kept token everything is 0.  Sums over tokens are formed in a fixed
  * order.  Limits: 1 <= k <= E <= 1024, T >= 0, T*k < 2^31.  4-byte aligned,
- * workspace 256-byte.  Outputs share no bytes with inputs (but grad) or each
- * other.  Errors: INVALID_ARG, WORKSPACE, HIP.                               */
+ * workspace 256-byte (NULL where mxmoe_balance_workspace_bytes is 0).  Outputs
+ * share no bytes with inputs (but grad) or each other.  Errors: INVALID_ARG,
+ * WORKSPACE, HIP.                                                            */
 MXMOE_API mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids,
                                 const uint8_t* token_mask, int32_t T, int32_t E, int32_t k,
                                 float alpha, int32_t* counts, float* probs, float* loss,

@@ -666,20 +666,18 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
 }
 
 // ------------------------------------------------------- balance loss
-#define BAL_COUNT 32
-#define BAL_SMALL 16384
-#define BAL_PART 512
 namespace {
-struct BalWs { size_t counts, probs, total; int n_count, n_part; };
+struct BalWs { size_t counts, probs, loss, total; };
+// For every top-k; a small batch needs none.
 BalWs bal_layout(int32_t T, int32_t E) {
+  int32_t n_count, n_part;
+  balance_shares(T, E, 1, &n_count, &n_part);
+  if (n_part == 0) return {0, 0, 0, 0};
   BalWs w;
-  // (n_part 0: one workgroup does everything)
-  const int64_t logits = (int64_t)T * E;
-  w.n_count = std::max(1, std::min(BAL_COUNT, T / 512));
-  w.n_part = logits <= BAL_SMALL ? 0 : (int)std::min<int64_t>(BAL_PART, (logits + 2047) / 2048);
   size_t o = 0;
-  w.counts = o; o = align256(o + 4 * (size_t)w.n_count * (E + 1));
-  w.probs = o; o = align256(o + 4 * (size_t)w.n_part * E);
+  w.counts = o; o = align256(o + 4 * (size_t)kBalCount * (E + 1));
+  w.probs = o; o = align256(o + 4 * (size_t)n_part * E);
+  w.loss = o; o = align256(o + 8 * (size_t)n_part);
   w.total = o;
   return w;
 }
@@ -695,17 +693,18 @@ mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids, co
                                 float* grad, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   if (T < 0 || E <= 0 || E > kMaxE || k <= 0 || k > E || !(alpha - alpha == 0.f)) return MXMOE_ERR_INVALID_ARG;
   if ((int64_t)T * k >= (1LL << 31)) return MXMOE_ERR_INVALID_ARG;
-  if (!counts || !probs || !loss || !workspace) return MXMOE_ERR_INVALID_ARG;
+  if (!counts || !probs || !loss) return MXMOE_ERR_INVALID_ARG;
   if (T > 0 && (!logits || !topk_ids)) return MXMOE_ERR_INVALID_ARG;
   if (!aligned(logits, 4) || !aligned(topk_ids, 4) || !aligned(counts, 4) || !aligned(probs, 4) || !aligned(loss, 4) ||
       !aligned(grad, 4) || !aligned(workspace, 256))
     return MXMOE_ERR_INVALID_ARG;
   const BalWs w = bal_layout(T, E);
+  if (w.total > 0 && !workspace) return MXMOE_ERR_INVALID_ARG;
   if (workspace_bytes < w.total) return MXMOE_ERR_WORKSPACE;
   const int64_t lb = 4 * (int64_t)T * E, ib = 4 * (int64_t)T * k, eb = 4 * (int64_t)E, wb = (int64_t)w.total;
   const int64_t some = T > 0 ? 1 : 0;
   const Rows in[3] = {{logits, lb, lb, some}, {topk_ids, ib, ib, some}, {token_mask, T, T, some}};
-  const Rows out[5] = {{counts, eb, eb, 1}, {probs, eb, eb, 1}, {loss, 4, 4, 1}, {grad, lb, lb, some}, {workspace, wb, wb, 1}};
+  const Rows out[5] = {{counts, eb, eb, 1}, {probs, eb, eb, 1}, {loss, 4, 4, 1}, {grad, lb, lb, some}, {workspace, wb, wb, wb > 0 ? 1 : 0}};
   for (int o = 0; o < 5; ++o) {
     for (int i = 0; i < 3; ++i)  // the gradient may take the logits' place
       if (overlap(out[o], in[i]) && !(o == 3 && i == 0 && grad == logits)) return MXMOE_ERR_INVALID_ARG;
@@ -722,11 +721,11 @@ mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids, co
   a.grad = grad;
   a.part_counts = at<int32_t>(workspace, w.counts);
   a.part_probs = at<float>(workspace, w.probs);
+  a.part_loss = at<double>(workspace, w.loss);
   a.T = T;
   a.E = E;
   a.k = k;
-  a.n_count = w.n_count;
-  a.n_part = w.n_part;
+  balance_shares(T, E, k, &a.n_count, &a.n_part);
   a.alpha = alpha;
   return hip_status(launch_balance_loss(a, stream));
 }

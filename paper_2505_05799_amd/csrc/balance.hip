@@ -7,9 +7,9 @@
 // The counts are constants of the gradient (a choice of experts has none), so a
 // token's gradient needs the counts and its own logits only: the ids are counted
 // first, by a launch of their own, then one pass over the logits writes the gradient
-// and sums the probabilities; the last workgroup to finish it adds up the shares of
-// all, in their order, and forms the loss.  Small batches take one workgroup and one
-// launch.
+// and sums the probabilities and the dots (L = alpha E / n sum_t sum_j f_j p[t,j]), and
+// a last launch adds the workgroups' shares in their order.  Small batches take one
+// workgroup and one launch.
 //
 // A token is held by LT lanes, V consecutive logits to a lane and chunk, so that a
 // wavefront reads 64 / LT tokens side by side; sums over a token are butterflies
@@ -42,14 +42,23 @@ template <int L, typename F> BAL_INL float lanes(float v, F f) {
   return v;
 }
 template <int L> BAL_INL float lanes_sum(float v) { return lanes<L>(v, [](float a, float b) { return a + b; }); }
-// the largest; NaN where one is
-template <int L> BAL_INL float lanes_max(float v) {
-  return lanes<L>(v, [](float a, float b) { return (a > b || a != a) ? a : b; });
+// the larger one; NaN where one is
+BAL_INL float larger(float a, float b) { return (a > b || a != a) ? a : b; }
+template <int L> BAL_INL float lanes_max(float v) { return lanes<L>(v, larger); }
+// exp(d) for d <= 0 within 2 units in the last place: 2^(d log2 e) with the rounding error
+// of the product put back (the library's expf takes three times the instructions; with it
+// and a quotient a probability, one workgroup took 14.4 us for 512 tokens of 64 experts)
+BAL_INL float exp_diff(float d) {
+  constexpr float kL2e = 1.44269504f, kL2eLow = 1.92596303e-8f, kLn2 = 0.693147181f;
+  d = d < -104.f ? -104.f : d;  // 0 from here on, and -inf makes no NaN below (a NaN stays)
+  const float hi = d * kL2e, lo = fmaf(d, kL2e, -hi) + d * kL2eLow;
+  const float x = __builtin_amdgcn_exp2f(hi);
+  return fmaf(x, lo * kLn2, x);
 }
 
 // Logits of a token in a lane: chunk j holds experts V (LT j + l) .. + V - 1 (V = 1: LT j + l).
 template <int LT, int V, int J> struct Tok {
-  float v[J][V];
+  float v[J][V] = {};
   BAL_INL static int expert(int l, int j) { return V * (LT * j + l); }
   BAL_INL void load(const float* row, int l, int E) {
 #pragma unroll
@@ -87,23 +96,26 @@ template <int LT, int V, int J> struct Tok {
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) m = (m > v[j][i] || m != m) ? m : v[j][i];
+      for (int i = 0; i < V; ++i) m = larger(m, v[j][i]);
     m = lanes_max<LT>(m);
-    const bool none = m == -INFINITY;
+    if (m == -INFINITY) m = 0.f;  // (then every exp is 0)
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        v[j][i] = none ? 0.f : expf(v[j][i] - m);
+        v[j][i] = V == 1 ? expf(v[j][i] - m) : exp_diff(v[j][i] - m);
         s += v[j][i];
       }
     s = lanes_sum<LT>(s);
-    if (none) s = 1.f;
+    if (s == 0.f) s = 1.f;
+    // a product with 1 / s where a lane holds many (one more rounding for ten fewer
+    // instructions each), quotients where it holds one or two
+    const float inv = __fdiv_rn(1.f, s);
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[j][i] = __fdiv_rn(v[j][i], s);
+      for (int i = 0; i < V; ++i) v[j][i] = V == 1 ? __fdiv_rn(v[j][i], s) : v[j][i] * inv;
   }
   BAL_INL float dot(const float (&f)[J][V]) const {
     float s = 0.f;
@@ -115,13 +127,11 @@ template <int LT, int V, int J> struct Tok {
   }
 };
 
-// Shared memory of a workgroup of W wavefronts
-template <int W> struct Lds {
-  int32_t hist[kMaxE + 1];  // counts, then kept tokens
-  float f[kMaxE];
-  float col[W][kMaxE];
-  double red[W];
-  int32_t flag;
+// Shared memory of a workgroup of W wavefronts, for at most NE experts
+template <int W, int NE> struct Lds {
+  int32_t hist[NE + 1];  // counts; hist[E]: kept tokens
+  float col[W][NE];      // sums of probabilities
+  double loss[W];        // sums of dots
 };
 
 BAL_INL double wave_sum(double v) {
@@ -129,47 +139,46 @@ BAL_INL double wave_sum(double v) {
   return v;
 }
 
-// Counts of the pairs first .. first + step, ... into L.hist (cleared here), and of the kept tokens
-template <int W> BAL_INL void count_pairs(Lds<W>& L, const BalanceArgs& a, int64_t part, int64_t parts) {
-  for (int e = threadIdx.x; e <= a.E; e += 64 * W) L.hist[e] = 0;
+// Counts of a share of the pairs, and of the kept tokens among them, into hist (cleared
+// here): four pairs to a load.
+template <int W> BAL_INL void count_pairs(int32_t* hist, const BalanceArgs& a, int64_t part, int64_t parts) {
+  for (int e = threadIdx.x; e <= a.E; e += 64 * W) hist[e] = 0;
   __syncthreads();
-  const int64_t P = (int64_t)a.T * a.k;
-  if (!a.mask) {
-    // four pairs to a load
-    for (int64_t p = 4 * (part * (64 * W) + threadIdx.x); p < P; p += 4 * parts * (64 * W)) {
-      i32x4 e = {-1, -1, -1, -1};
-      if (p + 4 <= P) e = *reinterpret_cast<const i32x4_any*>(a.ids + p);
-      else
-        for (int i = 0; i < 3; ++i)
-          if (p + i < P) e[i] = a.ids[p + i];
+  const int64_t P = (int64_t)a.T * a.k, step = 4 * parts * (64 * W);
+#pragma unroll 4
+  for (int64_t p = 4 * (part * (64 * W) + threadIdx.x); p < P; p += step) {
+    i32x4 e = {-1, -1, -1, -1};
+    if (p + 4 <= P) e = *reinterpret_cast<const i32x4_any*>(a.ids + p);
+    else
+      for (int i = 0; i < 3; ++i)
+        if (p + i < P) e[i] = a.ids[p + i];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if ((uint32_t)e[i] < (uint32_t)a.E) atomicAdd(&L.hist[e[i]], 1);
-    }
-    if (part == 0 && threadIdx.x == 0) L.hist[a.E] = a.T;
-  } else {
-    for (int64_t t = part * (64 * W) + threadIdx.x; t < a.T; t += parts * (64 * W)) {
-      if (!a.mask[t]) continue;
-      atomicAdd(&L.hist[a.E], 1);
-      for (int s = 0; s < a.k; ++s) {
-        const int e = a.ids[t * a.k + s];
-        if ((uint32_t)e < (uint32_t)a.E) atomicAdd(&L.hist[e], 1);
+    for (int i = 0; i < 4; ++i) {
+      if (a.mask) {
+        if (p + i >= P) continue;
+        const uint32_t t = (uint32_t)(p + i) / (uint32_t)a.k;
+        if (!a.mask[t]) continue;
+        if (t * (uint32_t)a.k == (uint32_t)(p + i)) atomicAdd(&hist[a.E], 1);
       }
+      if ((uint32_t)e[i] < (uint32_t)a.E) atomicAdd(&hist[e[i]], 1);
     }
   }
+  if (!a.mask && part == 0 && threadIdx.x == 0) hist[a.E] = a.T;
   __syncthreads();
 }
 
-// The tokens of this workgroup's part: gradients out, probabilities summed into L.col[w].
-// counts and kept tokens are in L.hist.
+// The tokens of this workgroup's share, U of a lane at a time: gradients out;
+// probabilities and dots summed into col[w] and loss[w] of every wavefront.  Counts and
+// kept tokens are in hist.
 template <int LT, int V, int J, int U, int W>
-BAL_INL void tokens(Lds<W>& L, const BalanceArgs& a, int64_t part, int64_t parts) {
+BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, int64_t parts) {
   constexpr int G = 64 / LT;  // tokens of a wavefront
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l = lane % LT, g = lane / LT;
   const int n = L.hist[a.E];
   const double per = n > 0 ? 1.0 / n : 0.0;
   const float gs = (float)((double)a.alpha * a.E * per);
   float f[J][V], sum[J][V];
+  double dots = 0.0;
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -179,38 +188,43 @@ BAL_INL void tokens(Lds<W>& L, const BalanceArgs& a, int64_t part, int64_t parts
       sum[j][i] = 0.f;
     }
   const int64_t step = parts * (W * G);
-  for (int64_t t0 = part * (W * G) + w * G + g; t0 - g < a.T; t0 += U * step) {
+  for (int64_t t0 = part * (W * G) + w * G; t0 < a.T; t0 += U * step) {
     Tok<LT, V, J> x[U];
     bool kept[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * step;
-      kept[u] = t < a.T && (!a.mask || a.mask[t]);
-      if (kept[u]) x[u].load(a.logits + t * a.E, l, a.E);
-      else
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int i = 0; i < V; ++i) x[u].v[j][i] = -INFINITY;  // probabilities 0, gradient 0
+      const int64_t t = t0 + g + u * step;
+      kept[u] = t < a.T;
+      if (kept[u]) {
+        x[u].load(a.logits + t * a.E, l, a.E);  // (padding's too: it need not wait for the mask)
+        if (a.mask) kept[u] = a.mask[t] != 0;
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * step;
-      x[u].softmax();
+      const int64_t t = t0 + g + u * step;
+      if (t - g >= a.T) continue;  // (of the whole wavefront)
 #pragma unroll
       for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum[j][i] += x[u].v[j][i];
-      if (a.grad) {
-        const float fp = x[u].dot(f);
+        for (int i = 0; i < V; ++i) x[u].v[j][i] = kept[u] ? x[u].v[j][i] : -INFINITY;  // probabilities 0
+      x[u].softmax();
+      const float fp = x[u].dot(f);
+      dots += (double)fp;
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int i = 0; i < V; ++i) x[u].v[j][i] = kept[u] ? gs * x[u].v[j][i] * (f[j][i] - fp) : 0.f;
-        if (t < a.T) x[u].store(a.grad + t * a.E, l, a.E);
-      }
+        for (int i = 0; i < V; ++i) {
+          const float q = x[u].v[j][i];
+          sum[j][i] += q;
+          x[u].v[j][i] = kept[u] ? gs * q * (f[j][i] - fp) : 0.f;
+        }
+      if (a.grad && t < a.T) x[u].store(a.grad + t * a.E, l, a.E);
     }
   }
+  if (l != 0) dots = 0.0;  // (a token's lanes hold the same dot)
+  dots = wave_sum(dots);
+  if (lane == 0) L.loss[w] = dots;
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -223,110 +237,150 @@ BAL_INL void tokens(Lds<W>& L, const BalanceArgs& a, int64_t part, int64_t parts
   __syncthreads();
 }
 
-// The loss from the sums of probabilities: sum(e) by a lane each.
-template <int W, typename F> BAL_INL void finish(Lds<W>& L, const BalanceArgs& a, F sum) {
-  const int tid = threadIdx.x, n = L.hist[a.E];
-  const double per = n > 0 ? 1.0 / n : 0.0;
-  double s = 0.0;
-  for (int e = tid; e < a.E; e += 64 * W) {
-    const double p = sum(e) * per;
-    a.probs[e] = (float)p;
-    a.counts[e] = L.hist[e];
-    s += (double)L.hist[e] * per / a.k * p;
-  }
-  s = wave_sum(s);
-  if ((tid & 63) == 0) L.red[tid >> 6] = s;
-  __syncthreads();
-  if (tid == 0) {
-    s = 0.0;
-    for (int i = 0; i < W; ++i) s += L.red[i];
-    a.loss[0] = (float)((double)a.alpha * a.E * s);
-  }
-}
-
 // Small batches: everything by one workgroup.
-template <int LT, int V, int J>
+template <int LT, int V, int J, int U>
 __global__ void __launch_bounds__(1024) balance_small_kernel(BalanceArgs a) {
-  __shared__ Lds<16> L;
-  count_pairs<16>(L, a, 0, 1);
-  tokens<LT, V, J, 1, 16>(L, a, 0, 1);
-  finish<16>(L, a, [&](int e) {
+  constexpr int W = 16;
+  __shared__ Lds<W, LT * V * J> L;
+  count_pairs<W>(L.hist, a, 0, 1);
+  tokens<LT, V, J, U, W>(L, a, 0, 1);
+  const int n = L.hist[a.E];
+  const double per = n > 0 ? 1.0 / n : 0.0;
+  for (int e = threadIdx.x; e < a.E; e += 64 * W) {
     double s = 0.0;
-    for (int i = 0; i < 16; ++i) s += (double)L.col[i][e];
-    return s;
-  });
+#pragma unroll
+    for (int i = 0; i < W; ++i) s += (double)L.col[i][e];
+    a.probs[e] = (float)(s * per);
+    a.counts[e] = L.hist[e];
+  }
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) s += L.loss[i];
+    a.loss[0] = (float)((double)a.alpha * a.E * per * s);
+  }
 }
 
 __global__ void __launch_bounds__(kThreads) balance_count_kernel(BalanceArgs a) {
-  __shared__ Lds<kThreads / 64> L;
-  count_pairs<kThreads / 64>(L, a, blockIdx.x, gridDim.x);
-  for (int e = threadIdx.x; e <= a.E; e += kThreads) a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = L.hist[e];
+  __shared__ int32_t hist[kMaxE + 1];
+  count_pairs<kThreads / 64>(hist, a, blockIdx.x, gridDim.x);
+  for (int e = threadIdx.x; e <= a.E; e += kThreads) a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = hist[e];
 }
 
 template <int LT, int V, int J, int U>
 __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs a) {
   constexpr int W = kThreads / 64;
-  __shared__ Lds<W> L;
-  const int tid = threadIdx.x;
-  for (int e = tid; e <= a.E; e += kThreads) {
+  __shared__ Lds<W, LT * V * J> L;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  // the counts: a wavefront adds up some of the shares, lanes along the experts
+  for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = 0;
+  __syncthreads();
+  for (int e = lane; e <= a.E; e += 64) {
     int32_t c = 0;
-    for (int i = 0; i < a.n_count; ++i) c += a.part_counts[(int64_t)i * (a.E + 1) + e];
-    L.hist[e] = c;
+#pragma unroll 8
+    for (int i = w; i < a.n_count; i += W) c += a.part_counts[(int64_t)i * (a.E + 1) + e];
+    atomicAdd(&L.hist[e], c);
   }
   __syncthreads();
   tokens<LT, V, J, U, W>(L, a, blockIdx.x, gridDim.x);
   for (int e = tid; e < a.E; e += kThreads) {
     float s = L.col[0][e];
+#pragma unroll
     for (int i = 1; i < W; ++i) s += L.col[i][e];
     a.part_probs[(int64_t)blockIdx.x * a.E + e] = s;
   }
+  if (tid == 0) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) s += L.loss[i];
+    a.part_loss[blockIdx.x] = s;
+  }
 }
 
-__global__ void __launch_bounds__(1024) balance_loss_kernel(BalanceArgs a) {
-  __shared__ Lds<16> L;
-  __shared__ double part[1024];
-  const int tid = threadIdx.x;
-  for (int e = tid; e <= a.E; e += 1024) {
-    int32_t c = 0;
-    for (int i = 0; i < a.n_count; ++i) c += a.part_counts[(int64_t)i * (a.E + 1) + e];
-    L.hist[e] = c;
-  }
-  // R threads to an expert, each a run of the shares
-  int R = 1;
-  while (2 * R * a.E <= 1024) R *= 2;
-  const int e = tid % a.E, r = tid / a.E;
-  double s = 0.0;
-  if (r < R)
-    for (int i = r; i < a.n_part; i += R) s += (double)a.part_probs[(int64_t)i * a.E + e];
-  part[tid] = s;
+// The shares of all workgroups, added in their order: 32 experts to a workgroup, 16
+// threads each a run of the shares.  The first workgroup also adds the loss.
+__global__ void __launch_bounds__(512) balance_sum_kernel(BalanceArgs a) {
+  __shared__ double sum[16][32];
+  __shared__ int32_t cnt[32], kept;
+  __shared__ double loss[8];
+  const int tid = threadIdx.x, c = tid & 31, r = tid >> 5, e = blockIdx.x * 32 + c;
+  if (tid < 32) cnt[tid] = 0;
+  if (tid == 0) kept = 0;
   __syncthreads();
-  finish<16>(L, a, [&](int c) {
-    double t = 0.0;
-    for (int i = 0; i < R; ++i) t += part[i * a.E + c];
-    return t;
-  });
+  int32_t k = 0;
+  for (int i = tid; i < a.n_count; i += 512) k += a.part_counts[(int64_t)i * (a.E + 1) + a.E];
+  if (tid < a.n_count) atomicAdd(&kept, k);
+  double s = 0.0;
+  if (e < a.E) {
+    int32_t n = 0;
+#pragma unroll 8
+    for (int i = r; i < a.n_count; i += 16) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
+    atomicAdd(&cnt[c], n);
+#pragma unroll 8
+    for (int i = r; i < a.n_part; i += 16) s += (double)a.part_probs[(int64_t)i * a.E + e];
+  }
+  sum[r][c] = s;
+  if (blockIdx.x == 0) {
+    double l = 0.0;
+    for (int i = tid; i < a.n_part; i += 512) l += a.part_loss[i];
+    l = wave_sum(l);
+    if ((tid & 63) == 0) loss[tid >> 6] = l;
+  }
+  __syncthreads();
+  const double per = kept > 0 ? 1.0 / kept : 0.0;
+  if (tid < 32 && e < a.E) {
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += sum[i][c];
+    a.probs[e] = (float)(s * per);
+    a.counts[e] = cnt[c];
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += loss[i];
+    a.loss[0] = (float)((double)a.alpha * a.E * per * s);
+  }
 }
 
 template <int LT, int V, int J> hipError_t go(const BalanceArgs& a, hipStream_t s) {
+  constexpr int U = V * J > 4 ? 1 : 4;  // tokens of a lane in flight
   if (a.n_part == 0) {
-    hipLaunchKernelGGL((balance_small_kernel<LT, V, J>), dim3(1), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((balance_small_kernel<LT, V, J, U>), dim3(1), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(balance_count_kernel, dim3(a.n_count), dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int U = V * J > 4 ? 1 : 4;
   hipLaunchKernelGGL((balance_kernel<LT, V, J, U>), dim3(a.n_part), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(balance_sum_kernel, dim3((a.E + 31) / 32), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Lanes of a token.  Few experts: a lane to an expert (or two), lanes a power of two.
+static int token_lanes(int E) {
+  if (E <= 8) return E == 8 ? 8 : (E > 3 ? 4 : (E > 1 ? 2 : 1));
+  int lt = 4;
+  while (lt < 64 && 4 * lt < E) lt *= 2;
+  return lt;
+}
+
+// Workgroups of a call.  One for everything up to 64 wavefronts' worth of tokens (a launch costs
+// more than they do: 64 tokens of 60 experts 5.7 us against 9.2 in three launches, 256 8.7 and
+// 9.2, 512 of 64 12.0 and 10.2).  Otherwise 4096 pairs to a counting workgroup and 2048 logits
+// to one of the tokens', at most 128 and 256: more of them bring the shares of the counts in more
+// often than they save (65536 x 64: 128 / 256 21.4 us, 32 / 256 23.7, 64 / 512 23.6).
+void balance_shares(int32_t T, int32_t E, int32_t k, int32_t* n_count, int32_t* n_part) {
+  const int64_t pairs = (int64_t)T * k, logits = (int64_t)T * E;
+  *n_part = (int64_t)T * token_lanes(E) <= 64 * 64 ? 0 : (int32_t)(logits >= kBalPart * 2048 ? kBalPart : (logits + 2047) / 2048);
+  *n_count = *n_part == 0 ? 0 : (int32_t)(pairs >= kBalCount * 4096 ? kBalCount : (pairs + 4095) / 4096);
+}
+
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s) {
-  // few experts: a lane to an expert (or two), lanes a power of two
   if (a.E == 1) return go<1, 1, 1>(a, s);
   if (a.E <= 3) return go<2, 1, 2>(a, s);
   if (a.E <= 7) return go<4, 1, 2>(a, s);

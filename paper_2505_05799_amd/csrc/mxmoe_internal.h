@@ -577,9 +577,12 @@ struct BalanceArgs {
   float *probs, *loss, *grad;
   int32_t* part_counts;  // [n_count][E + 1]: the share's counts and kept tokens
   float* part_probs;     // [n_part][E]
+  double* part_loss;     // [n_part]
   int32_t T, E, k, n_count, n_part;
   float alpha;
 };
+constexpr int kBalCount = 128, kBalPart = 256;  // most workgroups of each
+void balance_shares(int32_t T, int32_t E, int32_t k, int32_t* n_count, int32_t* n_part);
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s);
 
 }  // namespace mxmoe

@@ -323,18 +323,20 @@ def linear_forward(pl: PackedLinear, a, stream=None, return_ws: bool = False):
 
 
 # ------------------------------------------------- operators around the block
-def _run_on(device, stream, body, used):
-    """body(stream handle) with `device` current, on `stream` (default: the
+# (a decode step calls these once per layer: what they cost the host beside the
+# launch is one pass of checks, the outputs' allocations and the call)
+def _run_on(dev, stream, body, used):
+    """body(stream handle) with device `dev` current, on `stream` (default: the
     device's current one); what body allocates belongs to that stream, and the
     tensors `used` are kept until its work on them is done."""
     torch = _torch()
     if stream is None:
-        if device.index == torch.cuda.current_device():
-            return body(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.device(device):
-            return body(torch.cuda.current_stream().cuda_stream)
-    if stream.device != device:
-        raise ValueError(f"a stream of {stream.device} for tensors on {device}")
+        if dev.index == torch.cuda.current_device():
+            return body(torch._C._cuda_getCurrentRawStream(dev.index))
+        with torch.cuda.device(dev):
+            return body(torch._C._cuda_getCurrentRawStream(dev.index))
+    if stream.device != dev:
+        raise ValueError(f"a stream of {stream.device} for tensors on {dev}")
     with torch.cuda.stream(stream):
         out = body(stream.cuda_stream)
     for t in used:
@@ -343,34 +345,31 @@ def _run_on(device, stream, body, used):
     return out
 
 
-def _want(t, name, dtype, shape, device, strided: bool = False):
-    """Raise ValueError unless t is a tensor of the dtype(s), shape and device;
-    strided: rows of any stride (elements of a row side by side), else dense."""
-    if t.dtype != dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
-        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != device:
-        raise ValueError(f"{name}: on {t.device}, expected {device}")
-    if strided:
-        if t.shape[1] > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}: the elements of a row have to be side by side")
-        if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-            raise ValueError(f"{name}: rows overlap (stride {t.stride(0)})")
-    elif not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+def _dense(t, name, dtypes, shape, dev):
+    """Raise ValueError unless t is a dense tensor of one of the dtypes, of the
+    shape, on the device; returns its address."""
+    if t.dtype not in dtypes or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}, "
+                         f"expected dense {dtypes} {tuple(shape)} on {dev}")
+    return t.data_ptr()
 
 
-def _cuda_rows(t, name):
-    """Device of a [rows, cols] tensor on a GPU."""
-    if t.dim() != 2 or t.device.type != "cuda":
+def _rows(t, name, dtypes, shape, dev):
+    """The same for [rows, cols] tensors whose rows lie apart by any stride; returns
+    the address and the row stride."""
+    rows, cols = shape
+    if t.dtype not in dtypes or t.shape != shape or t.device != dev:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtypes} {tuple(shape)} on {dev}")
+    ld, one = t.stride()
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise ValueError(f"{name}: strides {t.stride()}; rows of elements side by side, apart from each other, are expected")
+    return t.data_ptr(), (ld if rows > 1 else max(cols, 1))
+
+
+def _cuda_2d(t, name):
+    if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name}: a [rows, columns] tensor on a GPU is expected, got {tuple(t.shape)} on {t.device}")
     return t.device
-
-
-def _ld(t) -> int:
-    """Row stride of a [rows, cols] tensor (a single row's own length)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
 def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, want_y: bool = True, sum_out=None,
@@ -385,34 +384,45 @@ def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, wan
     takes them); 0: neither."""
     torch = _torch()
     lib = load_library()
-    dev = _cuda_rows(x, "x")
-    if x.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError(f"x: {x.dtype}, expected bfloat16 or float16")
-    rows, cols = x.shape
-    _want(x, "x", x.dtype, x.shape, dev, strided=True)
-    _want(weight, "weight", x.dtype, (cols,), dev)
-    if residual is not None:
-        _want(residual, "residual", x.dtype, x.shape, dev, strided=True)
+    dev = _cuda_2d(x, "x")
+    dt = x.dtype
+    if dt is torch.bfloat16:
+        act = BF16
+    elif dt is torch.float16:
+        act = F16
+    else:
+        raise ValueError(f"x: {dt}, expected bfloat16 or float16")
+    shape = x.shape
+    rows, cols = shape
+    own = (dt,)
+    xp, ldx = _rows(x, "x", own, shape, dev)
+    wp = _dense(weight, "weight", own, (cols,), dev)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", own, shape, dev)
     if sum_out is not None:
         if residual is None:
             raise ValueError("sum_out: there is no sum without a residual")
-        _want(sum_out, "sum_out", x.dtype, x.shape, dev, strided=True)
+        _rows(sum_out, "sum_out", own, shape, dev)
 
     def body(s):
-        z = sum_out
-        if residual is not None and z is None:
-            z = torch.empty((rows, cols), dtype=x.dtype, device=dev)
-        y = torch.empty((rows, cols), dtype=x.dtype, device=dev) if want_y else None
-        codes = scales = None
+        y = z = codes = scales = yp = zp = cp = sp = None
+        ldz = cols
+        if residual is not None:
+            if sum_out is None:
+                z = torch.empty(shape, dtype=dt, device=dev)
+            else:
+                z = sum_out
+                ldz = z.stride(0) if rows > 1 else cols
+            zp = z.data_ptr()
+        if want_y:
+            y = torch.empty(shape, dtype=dt, device=dev)
+            yp = y.data_ptr()
         if qmax:
-            codes = torch.empty((rows, cols), dtype=torch.int8, device=dev)
+            codes = torch.empty(shape, dtype=torch.int8, device=dev)
             scales = torch.empty(rows, dtype=torch.float32, device=dev)
-        _check(lib.mxmoe_add_rms_norm(
-            x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(), 0 if residual is None else _ld(residual),
-            weight.data_ptr(), BF16 if x.dtype == torch.bfloat16 else F16, rows, cols, eps,
-            None if z is None else z.data_ptr(), 0 if z is None else _ld(z), None if y is None else y.data_ptr(), cols, qmax,
-            None if codes is None else codes.data_ptr(), None if scales is None else scales.data_ptr(), s),
-            "mxmoe_add_rms_norm")
+            cp, sp = codes.data_ptr(), scales.data_ptr()
+        st = lib.mxmoe_add_rms_norm(xp, ldx, rp, ldr, wp, act, rows, cols, eps, zp, ldz, yp, cols, qmax, cp, sp, s)
+        if st:
+            raise MxmoeError(st, "mxmoe_add_rms_norm")
         return y, z, codes, scales
 
     return _run_on(dev, stream, body, (x, residual, weight, sum_out))
@@ -425,32 +435,34 @@ def linear_decode(pl: PackedLinear, a, scales=None, bias=None, out=None, stream=
     (copied if not 16-byte aligned)."""
     torch = _torch()
     lib = load_library()
-    dev = _cuda_rows(a, "a")
+    dev = _cuda_2d(a, "a")
     q = pl.q
-    m = a.shape[0]
-    act = torch.bfloat16 if pl.act == "bf16" else torch.float16
+    m, n = a.shape[0], q.n
+    act, dt = (BF16, torch.bfloat16) if pl.act == "bf16" else (F16, torch.float16)
     coded = q.scheme.a_bits < 16
-    _want(a, "a", (torch.int8, torch.uint8) if coded else act, (m, q.k), dev, strided=True)
+    ap, lda = _rows(a, "a", (torch.int8, torch.uint8) if coded else (dt,), (m, q.k), dev)
     if pl.buf.device != dev:
         raise ValueError(f"a: on {dev}, the packed weights on {pl.buf.device}")
     if coded != (scales is not None):
         raise ValueError(f"{q.scheme.name}: scales are the rows' of 8-bit codes")
-    if scales is not None:
-        _want(scales, "scales", torch.float32, (m,), dev)
-    if bias is not None:
-        _want(bias, "bias", act, (q.n,), dev)
+    sp = None if scales is None else _dense(scales, "scales", (torch.float32,), (m,), dev)
+    bp = None if bias is None else _dense(bias, "bias", (dt,), (n,), dev)
     if out is not None:
-        _want(out, "out", act, (m, q.n), dev, strided=True)
+        op, ldo = _rows(out, "out", (dt,), (m, n), dev)
 
     def body(s):
-        rows = a
-        if rows.data_ptr() % 16 or (m > 1 and rows.stride(0) * rows.element_size() % 16):
-            rows = rows.clone(memory_format=torch.contiguous_format)
-        o = torch.empty((m, q.n), dtype=act, device=dev) if out is None else out
-        _check(lib.mxmoe_linear_decode(
-            C.byref(pl.L), BF16 if pl.act == "bf16" else F16, pl.buf.data_ptr(), m, rows.data_ptr(), _ld(rows),
-            None if scales is None else scales.data_ptr(), None if bias is None else bias.data_ptr(), o.data_ptr(), _ld(o), s),
-            "mxmoe_linear_decode")
+        rows, rp, ldr = a, ap, lda
+        if rp % 16 or (m > 1 and ldr * (1 if coded else 2) % 16):
+            rows = a.clone(memory_format=torch.contiguous_format)
+            rp, ldr = rows.data_ptr(), q.k
+        if out is None:
+            o = torch.empty((m, n), dtype=dt, device=dev)
+            p, ld = o.data_ptr(), n
+        else:
+            o, p, ld = out, op, ldo
+        st = lib.mxmoe_linear_decode(C.byref(pl.L), act, pl.buf.data_ptr(), m, rp, ldr, sp, bp, p, ld, s)
+        if st:
+            raise MxmoeError(st, "mxmoe_linear_decode")
         return o
 
     return _run_on(dev, stream, body, (a, scales, bias, out, pl.buf))
@@ -466,27 +478,27 @@ def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_gra
     factor."""
     torch = _torch()
     lib = load_library()
-    dev = _cuda_rows(logits, "logits")
-    T, E = logits.shape
-    _want(logits, "logits", torch.float32, logits.shape, dev)
+    dev = _cuda_2d(logits, "logits")
+    shape = logits.shape
+    T, E = shape
+    lp = _dense(logits, "logits", (torch.float32,), shape, dev)
     if topk_ids.dim() != 2:
         raise ValueError(f"topk_ids: shape {tuple(topk_ids.shape)}, expected [T, k]")
     k = topk_ids.shape[1]
-    _want(topk_ids, "topk_ids", torch.int32, (T, k), dev)
-    if token_mask is not None:
-        _want(token_mask, "token_mask", (torch.bool, torch.uint8), (T,), dev)
+    ip = _dense(topk_ids, "topk_ids", (torch.int32,), (T, k), dev)
+    mp = None if token_mask is None else _dense(token_mask, "token_mask", (torch.bool, torch.uint8), (T,), dev)
+    wsb = lib.mxmoe_balance_workspace_bytes(T, E)
 
     def body(s):
         counts = torch.empty(E, dtype=torch.int32, device=dev)
         probs = torch.empty(E, dtype=torch.float32, device=dev)
         loss = torch.empty((), dtype=torch.float32, device=dev)
-        grad = torch.empty((T, E), dtype=torch.float32, device=dev) if want_grad else None
-        wsb = lib.mxmoe_balance_workspace_bytes(T, E)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
-        _check(lib.mxmoe_balance_loss(
-            logits.data_ptr(), topk_ids.data_ptr(), None if token_mask is None else token_mask.data_ptr(), T, E, k, alpha,
-            counts.data_ptr(), probs.data_ptr(), loss.data_ptr(), None if grad is None else grad.data_ptr(), ws.data_ptr(),
-            wsb, s), "mxmoe_balance_loss")
+        grad = torch.empty(shape, dtype=torch.float32, device=dev) if want_grad else None
+        ws = torch.empty(wsb, dtype=torch.uint8, device=dev) if wsb else None
+        st = lib.mxmoe_balance_loss(lp, ip, mp, T, E, k, alpha, counts.data_ptr(), probs.data_ptr(), loss.data_ptr(),
+                                    grad.data_ptr() if want_grad else None, ws.data_ptr() if wsb else None, wsb, s)
+        if st:
+            raise MxmoeError(st, "mxmoe_balance_loss")
         return loss, counts, probs, grad
 
     return _run_on(dev, stream, body, (logits, topk_ids, token_mask))

@@ -180,7 +180,7 @@ def test_decode_refuses_unsupported_and_takes_nothing(lib):
     assert decode_call(lib, m=0, packed=None, a=None, out=None) == M.OK
 
 
-def balance_call(lib, logits=at(1), ids=at(2), mask=at(3), T=100, E=16, k=2, alpha=1.0, counts=at(4), probs=at(5),
+def balance_call(lib, logits=at(1), ids=at(2), mask=at(3), T=5000, E=16, k=2, alpha=1.0, counts=at(4), probs=at(5),
                  loss=at(6), grad=at(7), ws=at(8), wsb=None):
     wsb = lib.mxmoe_balance_workspace_bytes(max(T, 0), 16) if wsb is None else wsb
     return lib.mxmoe_balance_loss(logits, ids, mask, T, E, k, alpha, counts, probs, loss, grad, ws, wsb, None)
@@ -198,13 +198,13 @@ def test_balance_refuses(lib, bad):
 
 
 def test_balance_workspace(lib):
-    assert balance_call(lib, wsb=lib.mxmoe_balance_workspace_bytes(100, 16) - 1) == M.ERR_WORKSPACE
+    assert balance_call(lib, wsb=lib.mxmoe_balance_workspace_bytes(5000, 16) - 1) == M.ERR_WORKSPACE
     for T, E in ((-1, 8), (8, 0), (8, 1025)):
         assert lib.mxmoe_balance_workspace_bytes(T, E) == 0
     last = 0
     for T in (0, 1, 17, 512, 4096, 65536, 1 << 20):   # a workspace serves every smaller batch
         b = lib.mxmoe_balance_workspace_bytes(T, 64)
-        assert b >= last > 0 or last == 0
+        assert b >= last
         last = b
     assert last < 1 << 20
 
