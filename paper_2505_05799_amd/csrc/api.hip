@@ -662,7 +662,8 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
   p.m = m;
   p.n = L->n;
   p.k = L->k;
-  return hip_status(launch_linear_decode(p, kd, act, stream));
+  p.act = act;
+  return hip_status(launch_linear_decode(p, kd, stream));
 }
 
 // ------------------------------------------------------- balance loss

@@ -10,9 +10,10 @@
 //           1024 + z leaves q - z.  Both are exact in their dtype.
 //   w8a8    int8 MFMA, int32 sums; fp8  FP8 MFMA, fp32 sums; times s_a s_w at the end.
 //
-// A workgroup takes 16 channels; its wavefronts take the k blocks in turn and meet
-// once, through LDS, in wavefront order.  Rows past the last one repeat it (their sums
-// are dropped).
+// The wavefronts of a workgroup take the k blocks of its channels in turn and meet once,
+// through LDS, in wavefront order.  Rows past the last one repeat it (their sums are
+// dropped).  A launch is bound by the weights' way from memory for few rows, and by the
+// rows' way from the L2 to every CU for many.
 #include "mxmoe_internal.h"
 
 namespace mxmoe {
@@ -34,14 +35,12 @@ template <int ACT> DEC_INL f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-template <int ACT> DEC_INL float act_load(const uint16_t* p) {
-  if constexpr (ACT == MXMOE_BF16) return __uint_as_float((uint32_t)*p << 16);
-  else return (float)__builtin_bit_cast(_Float16, *p);
+DEC_INL float act_load(const uint16_t* p, int act) {
+  return act == MXMOE_BF16 ? __uint_as_float((uint32_t)*p << 16) : (float)__builtin_bit_cast(_Float16, *p);
 }
-template <int ACT> DEC_INL uint16_t act_round(float f) {
+DEC_INL uint16_t act_round(float f, int act) {
   asm("" : "+v"(f));  // the fp32 value is rounded, not the expression it came from
-  if constexpr (ACT == MXMOE_BF16) return __builtin_bit_cast(uint16_t, (__bf16)f);
-  else return __builtin_bit_cast(uint16_t, (_Float16)f);
+  return act == MXMOE_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)f) : __builtin_bit_cast(uint16_t, (_Float16)f);
 }
 
 // What a lane holds of one k block: its weights (and the group's scale and zero point),
@@ -123,7 +122,7 @@ DEC_INL void use_block(const Wgt<KD>& s, const Rows<KD, MF>& a, const f32x4 (&rs
 // The wavefronts' sums of one block of channels, added in wavefront order, to the
 // output.  red: [NW][MF][64] accumulators in LDS.  Output o = 64 (4 f + i) + l:
 // fragment f, row 4 (l / 16) + i of it, channel l % 16.
-template <int KD, int ACT, int MF, int NW>
+template <int KD, int MF, int NW>
 DEC_INL void write_out(const DecodeArgs& p, const Acc<KD>* red, int nb, int t, int threads) {
   for (int o = t; o < MF * 256; o += threads) {
     const int l = o & 63, i = (o >> 6) & 3, f = o >> 8, r = 16 * f + 4 * (l >> 4) + i;
@@ -134,23 +133,28 @@ DEC_INL void write_out(const DecodeArgs& p, const Acc<KD>* red, int nb, int t, i
     const int c = nb * 16 + (l & 15);
     float x = (float)v;
     if constexpr (KD != K_W4G) x = x * p.a_scales[r] * p.wscale[c];
-    if (p.bias) x += act_load<ACT>(reinterpret_cast<const uint16_t*>(p.bias) + c);
-    reinterpret_cast<uint16_t*>(p.out)[(int64_t)r * p.ldo + c] = act_round<ACT>(x);
+    if (p.bias) x += act_load(reinterpret_cast<const uint16_t*>(p.bias) + c, p.act);
+    reinterpret_cast<uint16_t*>(p.out)[(int64_t)r * p.ldo + c] = act_round(x, p.act);
   }
 }
 
-// ---- At most 16 rows, straight from memory.  NW wavefronts share 16 channels; a
-// wavefront's next k block is asked for before this one is used.  One token through
-// 4096 x 4096 w4g128 3.8 us a launch in a graph, one wavefront for all k blocks 10.7; 20480 x
-// 3584 9.8 us, 4.0 TB/s with the weights in the Infinity Cache.
+// LDS operations of a wavefront are done in order; this keeps the compiler to it between the
+// lanes' writes and other lanes' reads.
+DEC_INL void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---- One row, straight from memory.  NW wavefronts share 16 channels; a wavefront's
+// next k block is asked for before this one is used.  4096 x 4096 w4g128 3.9 us a launch in
+// a graph (one wavefront for all k blocks: 10.7); 20480 x 3584 9.7 us, 4.0 TB/s.
 template <int KD, int ACT, int NW>
-__global__ void __launch_bounds__(64 * NW) decode_kernel(DecodeArgs p) {
+__global__ void __launch_bounds__(64 * NW) decode_one_kernel(DecodeArgs p) {
   __shared__ Acc<KD> red[NW * 64];
-  constexpr int ES = KD == K_W4G ? 2 : 1;
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, qd = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), qd = lane >> 4;
   const int kbs = p.k / 128;
   const uint8_t* wb = p.packed + (int64_t)blockIdx.x * kbs * block_bytes(KD);
-  const uint8_t* ar = reinterpret_cast<const uint8_t*>(p.a) + (int64_t)min(li, p.m - 1) * p.lda * ES + 16 * qd;
+  const uint8_t* ar = reinterpret_cast<const uint8_t*>(p.a) + 16 * qd;
   Acc<KD> tot[1] = {Acc<KD>{0, 0, 0, 0}};
   struct Step { Wgt<KD> w; Rows<KD, 1> a; } cur, nxt;
   auto load = [&](Step& s, int kb) {
@@ -169,19 +173,93 @@ __global__ void __launch_bounds__(64 * NW) decode_kernel(DecodeArgs p) {
   }
   red[w * 64 + lane] = tot[0];
   __syncthreads();
-  write_out<KD, ACT, 1, NW>(p, red, blockIdx.x, tid, 64 * NW);
+  write_out<KD, 1, NW>(p, red, blockIdx.x, tid, 64 * NW);
 }
 
-// ---- Rows through LDS.  Fragments of many rows straight from memory are 64-byte
-// pieces of as many rows, which the cache serves at a quarter of its rate (64 rows of
-// fp8, 4096 x 14336: 28.7 us whatever n).  Here 8 wavefronts bring KC k blocks of all rows into
-// LDS, row by row in whole lines, and share them: WN groups of wavefronts take NB blocks of
+// ---- Rows through a wavefront's own LDS.  A fragment straight from memory takes 64
+// addresses a load, lane by lane, where the cache serves four lanes at a time that read 64
+// bytes side by side (64 rows of fp8, 4096 x 14336: 28.9 us, bound by that).  So four lanes
+// bring a row's 64 bytes, and the wavefront turns them into a fragment through 1 KB of LDS
+// of its own, without a barrier: 16.2 us, 3.6 TB/s.  Its next k block, weights and rows, is on
+// its way meanwhile.  NB blocks of channels use the fragments.
+template <int KD, int ACT, int MF, int NW, int NB>
+__global__ void __launch_bounds__(64 * NW) decode_wave_kernel(DecodeArgs p) {
+  constexpr int P = kPieces<KD>, ES = KD == K_W4G ? 2 : 1;
+  constexpr int kStage = NW * MF * P * 64, kRed = NW * MF * 64;
+  __shared__ u32x4 buf[kStage > kRed ? kStage : kRed];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, qd = lane >> 4;
+  const int kbs = p.k / 128, nbs = p.n / 16, nb0 = (int)blockIdx.x * NB;
+  const uint8_t* wb[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) wb[b] = p.packed + (int64_t)min(nb0 + b, nbs - 1) * kbs * block_bytes(KD);
+  // lane 4 i + q brings piece 4 j + q of row i of a fragment; element (i, q) of the
+  // fragment lies at 16 q + (i + 4 q) % 16
+  const int mi = lane >> 2, mq = lane & 3;
+  const uint8_t* src[MF];
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+    src[f] = reinterpret_cast<const uint8_t*>(p.a) + (int64_t)min(16 * f + mi, p.m - 1) * p.lda * ES + 16 * mq;
+  u32x4* put = buf + w * (MF * P * 64) + 16 * mq + ((mi + 4 * mq) & 15);
+  const u32x4* get = buf + w * (MF * P * 64) + 16 * qd + ((li + 4 * qd) & 15);
+  u32x4 st[MF][P];
+  Wgt<KD> cur[NB], nxt[NB];
+  auto load = [&](Wgt<KD> (&g)[NB], int kb) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) g[b].load(wb[b] + (int64_t)kb * block_bytes(KD), lane);
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int j = 0; j < P; ++j) st[f][j] = *reinterpret_cast<const u32x4*>(src[f] + (int64_t)kb * (64 * P) + 64 * j);
+  };
+  Acc<KD> tot[NB][MF];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int f = 0; f < MF; ++f) tot[b][f] = Acc<KD>{0, 0, 0, 0};
+  if (w < kbs) load(cur, w);
+  for (int kb = w; kb < kbs; kb += NW) {
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int j = 0; j < P; ++j) put[(f * P + j) * 64] = st[f][j];
+    wave_order();
+    if (kb + NW < kbs) load(nxt, kb + NW);
+    Rows<KD, MF> a;
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int j = 0; j < P; ++j) a[f][j] = get[(f * P + j) * 64];
+    wave_order();
+    f32x4 rs[MF];
+    row_sums<KD, ACT, MF>(a, rs);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) use_block<KD, ACT, MF>(cur[b], a, rs, tot[b]);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) cur[b] = nxt[b];
+  }
+  Acc<KD>* red = reinterpret_cast<Acc<KD>*>(buf);
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    __syncthreads();
+#pragma unroll
+    for (int f = 0; f < MF; ++f) red[(w * MF + f) * 64 + lane] = tot[b][f];
+    __syncthreads();
+    if (nb0 + b < nbs) write_out<KD, MF, NW>(p, red, nb0 + b, tid, 64 * NW);
+  }
+}
+template <int KD, int ACT, int MF, int NW, int NB> hipError_t go_wave(const DecodeArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL((decode_wave_kernel<KD, ACT, MF, NW, NB>), dim3((p.n / 16 + NB - 1) / NB), dim3(64 * NW), 0, s, p);
+  return hipGetLastError();
+}
+
+// ---- Rows through LDS that the workgroup shares, for the widest linears: 8 wavefronts
+// bring KC k blocks of all rows into LDS, and WN groups of wavefronts take NB blocks of
 // 16 channels each, the WK wavefronts of a group one k block each.  Piece q of
 // row r lies at q ^ (r % 16), so that both the writes along a row and the fragment reads
 // across rows are free of bank conflicts.  The next k blocks' rows and weights are on
-// their way in registers meanwhile.  Workgroups start at different k blocks: all at the
-// same lines, they waited for the same few channels of the L2 (that fp8 case 26.7 -> 22.6 us).
-// What it is bound by then: the rows' way from the L2, 13 TB/s over all CUs.
+// their way in registers meanwhile, and workgroups start at different ones (all at the same
+// lines, they waited for the same channels of the L2).  The rows come to a CU once for 64
+// or 96 channels; the barriers, a chunk at a time, cost more where channels are few.
 template <int KD, int ACT, int MF, int WN, int NB>
 __global__ void __launch_bounds__(512) decode_rows_kernel(DecodeArgs p) {
   constexpr int NW = 8, WK = NW / WN, KC = WK, PP = 4 * kPieces<KD>, RP = KC * PP, RS = 512 / RP, NPT = 16 * MF / RS;
@@ -256,60 +334,64 @@ __global__ void __launch_bounds__(512) decode_rows_kernel(DecodeArgs p) {
 #pragma unroll
     for (int f = 0; f < MF; ++f) red[(w * MF + f) * 64 + lane] = tot[b][f];
     __syncthreads();
-    if (nb0 + b < nbs) write_out<KD, ACT, MF, WK>(p, red + wn * WK * MF * 64, nb0 + b, tid - wn * WK * 64, WK * 64);
+    if (nb0 + b < nbs) write_out<KD, MF, WK>(p, red + wn * WK * MF * 64, nb0 + b, tid - wn * WK * 64, WK * 64);
   }
 }
 
-template <int KD, int ACT, int MF, int WN, int NB> hipError_t go_rows(const DecodeArgs& p, hipStream_t s) {
-  const int per = WN * NB;
-  hipLaunchKernelGGL((decode_rows_kernel<KD, ACT, MF, WN, NB>), dim3((p.n / 16 + per - 1) / per), dim3(512), 0, s, p);
+template <int KD, int ACT, int NW> hipError_t go_one(const DecodeArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL((decode_one_kernel<KD, ACT, NW>), dim3(p.n / 16), dim3(64 * NW), 0, s, p);
   return hipGetLastError();
 }
-template <int KD, int ACT, int NW> hipError_t go_direct(const DecodeArgs& p, hipStream_t s) {
-  hipLaunchKernelGGL((decode_kernel<KD, ACT, NW>), dim3(p.n / 16), dim3(64 * NW), 0, s, p);
+template <int KD, int ACT, int MF, int NB> hipError_t go_rows(const DecodeArgs& p, hipStream_t s) {
+  hipLaunchKernelGGL((decode_rows_kernel<KD, ACT, MF, 2, NB>), dim3((p.n / 16 + 2 * NB - 1) / (2 * NB)), dim3(512), 0, s, p);
   return hipGetLastError();
 }
-// (nb blocks of 16 channels; us of the forms beside each other, wavefronts x channel blocks)
+
+// Rows of a call in MF fragments, nb blocks of 16 channels.
 template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, hipStream_t s) {
-  const int nb = p.n / 16, kbs = p.k / 128;
-  if constexpr (MF == 1) {
-    // Few rows straight from memory: codes up to 16 (16 x 4096 x 14336 fp8 10.7, through LDS
-    // 12.5), 16-bit rows, twice the pieces, up to 8 (8 and 16 x 4096 x 4096 5.0 and 6.3,
-    // through LDS 5.0 and 5.5), 2 where many workgroups bring the same rows (4 and 16 x 20480 x
-    // 3584 11.3 and 19.1, LDS 10.5 and 11.4).  16 wavefronts where few workgroups have much
-    // to read (1 x 4096 x 14336 8.7, 8 wavefronts 10.1; 1 x 20480 x 3584 12.0 and 9.7).
-    if (KD != K_W4G || p.m <= (nb > 512 ? 2 : 8)) {
-      if (KD == K_W4G && nb <= 256 && kbs >= 32) return go_direct<KD, ACT, 16>(p, s);
-      return go_direct<KD, ACT, 8>(p, s);
+  const int nb = p.n / 16;
+  // 33 and more 16-bit rows, wide linears: a workgroup's rows shared by 4 or 6 blocks (64 x 20480 x
+  // 3584 22.8 us, 27.7 by wavefronts; 64 x 16384 x 2048 12.7, 15.7; 64 x 12288 x 4096 24.2, 16.6)
+  if constexpr (KD == K_W4G && MF == 4)
+    if (nb > 768) return (nb + 1535) / 1536 * 4 <= (nb + 1023) / 1024 * 3 ? go_rows<KD, ACT, MF, 3>(p, s) : go_rows<KD, ACT, MF, 2>(p, s);
+  // Blocks of a workgroup: what the busiest CU does, its workgroups times the rows (about the
+  // weights of one block) and their blocks.  16 x 8192 x 4096 w4g128 with 1, 2, 3 blocks 7.1, 6.2,
+  // 7.4; 32 x 12288 x 4096 13.7, 14.0, 10.4; 64 x 4096 x 14336 fp8 16.2, 18.7, 22.3.
+  int NB = 1, best = 0;
+  for (int b = 1; b <= 3; ++b) {
+    const int cost = ((nb + b - 1) / b + 255) / 256 * (1 + b);
+    if (b == 1 || cost < best) {
+      NB = b;
+      best = cost;
     }
-    if constexpr (KD == K_W4G) return nb <= 512 ? go_rows<KD, ACT, 1, 1, 1>(p, s) : go_rows<KD, ACT, 1, 2, 1>(p, s);
-  } else {
-    // A workgroup of its own for every 16 channels as long as that is one round of the 256 CUs;
-    // beyond, more channels to a workgroup, so that the rows come in once for all of them:
-    // 64 x 20480 x 3584 w4g128 with 1, 2, 4 and 6 blocks of channels 54, 37, 33 and 23.
-    if (nb <= 256) return go_rows<KD, ACT, MF, 1, 1>(p, s);
-    if (KD != K_W4G || nb <= 512) return go_rows<KD, ACT, MF, 2, 1>(p, s);
-    if constexpr (KD == K_W4G) return nb <= 1024 ? go_rows<KD, ACT, MF, 2, 2>(p, s) : go_rows<KD, ACT, MF, 2, 3>(p, s);
   }
+  // 8 wavefronts where a CU has one workgroup, else 4 (64 x 20480 x 3584 int8, 3 blocks: 21.1 and
+  // 17.5; 64 x 8192 x 4096, 2 blocks: 9.8 and 10.2)
+  const bool one = (nb + NB - 1) / NB <= 256;
+  if (NB == 1) return go_wave<KD, ACT, MF, 8, 1>(p, s);
+  if (NB == 2) return one ? go_wave<KD, ACT, MF, 8, 2>(p, s) : go_wave<KD, ACT, MF, 4, 2>(p, s);
+  if constexpr (KD != K_W4G || MF < 4)  // (64 16-bit rows for 3 blocks do not fit the registers of 8)
+    if (one) return go_wave<KD, ACT, MF, 8, 3>(p, s);
+  return go_wave<KD, ACT, MF, 4, 3>(p, s);
 }
-template <int KD, int ACT> hipError_t launch_act(const DecodeArgs& p, hipStream_t s) {
+template <int KD, int ACT> hipError_t launch(const DecodeArgs& p, hipStream_t s) {
+  // One row straight from memory, with 16 wavefronts where few workgroups have much to read
+  // (1 x 4096 x 14336 8.6 us, 8 wavefronts 10.0, through LDS 9.0; 1 x 20480 x 3584 12.2, 9.7, 9.8).
+  if (p.m == 1) return p.n <= 4096 && p.k >= 4096 ? go_one<KD, ACT, 16>(p, s) : go_one<KD, ACT, 8>(p, s);
   if (p.m <= 16) return launch_rows<KD, ACT, 1>(p, s);
   if (p.m <= 32) return launch_rows<KD, ACT, 2>(p, s);
   return launch_rows<KD, ACT, 4>(p, s);
-}
-template <int KD> hipError_t launch_kind(const DecodeArgs& p, int act, hipStream_t s) {
-  return act == MXMOE_BF16 ? launch_act<KD, MXMOE_BF16>(p, s) : launch_act<KD, MXMOE_F16>(p, s);
 }
 
 }  // namespace
 
 bool decode_kind(int kind) { return kind == K_W4G || kind == K_W8A8 || kind == K_F8A8; }
 
-hipError_t launch_linear_decode(const DecodeArgs& p, int kind, int act, hipStream_t s) {
+hipError_t launch_linear_decode(const DecodeArgs& p, int kind, hipStream_t s) {
   switch (kind) {
-    case K_W4G: return launch_kind<K_W4G>(p, act, s);
-    case K_W8A8: return launch_kind<K_W8A8>(p, act, s);
-    default: return launch_kind<K_F8A8>(p, act, s);
+    case K_W4G: return p.act == MXMOE_BF16 ? launch<K_W4G, MXMOE_BF16>(p, s) : launch<K_W4G, MXMOE_F16>(p, s);
+    case K_W8A8: return launch<K_W8A8, MXMOE_BF16>(p, s);  // (codes: the dtype is the output's only)
+    default: return launch<K_F8A8, MXMOE_BF16>(p, s);
   }
 }
 

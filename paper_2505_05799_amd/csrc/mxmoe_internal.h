@@ -562,10 +562,10 @@ struct DecodeArgs {
   const void* bias;
   void* out;
   int64_t lda, ldo;
-  int32_t m, n, k;
+  int32_t m, n, k, act;
 };
 bool decode_kind(int kind);
-hipError_t launch_linear_decode(const DecodeArgs& p, int kind, int act, hipStream_t s);
+hipError_t launch_linear_decode(const DecodeArgs& p, int kind, hipStream_t s);
 
 // Balance loss of the router (balance.hip).  n_count workgroups count, n_part
 // take the tokens' softmax (0: one workgroup does everything).

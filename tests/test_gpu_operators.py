@@ -236,6 +236,18 @@ def test_decode_shapes(scheme, m, n, k):
 
 
 @pytest.mark.parametrize("scheme", DECODE_SCHEMES, ids=lambda s: s.name)
+@pytest.mark.parametrize("n", [4112, 6000, 8208, 10000, 12304, 16400, 19232, 24592])
+def test_decode_wide(scheme, n):
+    """Every number of channel blocks to a workgroup, the last one not full, for each
+    number of row fragments."""
+    k = 384
+    for m, act in ((1, "fp16"), (9, "bf16"), (24, "fp16"), (40, "bf16")):
+        q, pl, a, sc, bt, ad, b = decode_case(scheme, act, m, n, k, n, True)
+        worst = check_decode(q, ad, b, act, M.linear_decode(pl, a, scales=sc, bias=bt))
+        say(f"decode {scheme.name} {act} {m}x{n}x{k}: {worst:.3f} of the bound")
+
+
+@pytest.mark.parametrize("scheme", DECODE_SCHEMES, ids=lambda s: s.name)
 def test_decode_strides(scheme):
     """Rows and outputs of wider tensors, rows that are not 16-byte aligned (the
     binding copies them), and what lies beside the output stays as it was."""
