@@ -190,8 +190,8 @@ MXMOE_API mxmoe_status mxmoe_router_topk(const float* logits, int32_t T, int32_t
                                int32_t* topk_ids, float* topk_w, float* shared_w,
                                hipStream_t stream);
 
-/* Workspace bytes of mxmoe_balance_loss for any top-k; 0 for small batches (they
- * need no workspace) and for invalid sizes.                                  */
+/* Workspace bytes of mxmoe_balance_loss: 0 for small batches (they need none) and
+ * for invalid sizes.                                                         */
 MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
 
 /* Balance loss of the router, with the experts' counts and the gradient of the

@@ -668,17 +668,13 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
 
 // ------------------------------------------------------- balance loss
 namespace {
-struct BalWs { size_t counts, probs, loss, total; };
-// For every top-k; a small batch needs none.
-BalWs bal_layout(int32_t T, int32_t E) {
-  int32_t n_count, n_part;
-  balance_shares(T, E, 1, &n_count, &n_part);
-  if (n_part == 0) return {0, 0, 0, 0};
+struct BalWs { size_t counts, probs, total; int32_t n_part, n_grad; };
+BalWs bal_layout(int32_t T, int32_t E) {  // (a small batch needs none)
   BalWs w;
+  balance_shares(T, E, &w.n_part, &w.n_grad);
   size_t o = 0;
-  w.counts = o; o = align256(o + 4 * (size_t)kBalCount * (E + 1));
-  w.probs = o; o = align256(o + 4 * (size_t)n_part * E);
-  w.loss = o; o = align256(o + 8 * (size_t)n_part);
+  w.counts = o; o = align256(o + 4 * (size_t)w.n_part * (E + 1));
+  w.probs = o; o = align256(o + 4 * (size_t)w.n_part * E);
   w.total = o;
   return w;
 }
@@ -722,11 +718,11 @@ mxmoe_status mxmoe_balance_loss(const float* logits, const int32_t* topk_ids, co
   a.grad = grad;
   a.part_counts = at<int32_t>(workspace, w.counts);
   a.part_probs = at<float>(workspace, w.probs);
-  a.part_loss = at<double>(workspace, w.loss);
   a.T = T;
   a.E = E;
   a.k = k;
-  balance_shares(T, E, k, &a.n_count, &a.n_part);
+  a.n_part = w.n_part;
+  a.n_grad = w.n_grad;
   a.alpha = alpha;
   return hip_status(launch_balance_loss(a, stream));
 }

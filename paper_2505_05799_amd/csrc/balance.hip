@@ -4,16 +4,19 @@
 //   P_e = 1/n sum_t p[t,e],  p[t] = softmax of the token's logits
 //   L = alpha E sum_e f_e P_e
 //   dL/dlogits[t,e] = alpha E / n * p[t,e] (f_e - sum_j f_j p[t,j])
-// The counts are constants of the gradient (a choice of experts has none), so a
-// token's gradient needs the counts and its own logits only: the ids are counted
-// first, by a launch of their own, then one pass over the logits writes the gradient
-// and sums the probabilities and the dots (L = alpha E / n sum_t sum_j f_j p[t,j]), and
-// a last launch adds the workgroups' shares in their order.  Small batches take one
-// workgroup and one launch.
+// The counts are constants of the gradient (a choice of experts has none), so a token's
+// gradient needs all counts and its own logits.  Two launches: the first counts and sums
+// the probabilities, the second writes the gradient, and its first workgroup adds the
+// shares of the first in their order, to counts, mean probabilities and loss.  The logits are
+// read twice, the second time from the caches: with one pass over them and a launch for
+// the counts before it and one for the shares behind it, 65536 x 64 took 20.9 us and
+// 4096 x 60 12.9, and a workgroup that finishes last adding the shares waits for the L2s to
+// be written back (29 us).  Small batches take one workgroup and one launch.
 //
 // A token is held by LT lanes, V consecutive logits to a lane and chunk, so that a
 // wavefront reads 64 / LT tokens side by side; sums over a token are butterflies
 // over its lanes.
+#include <algorithm>
 #include "mxmoe_internal.h"
 
 namespace mxmoe {
@@ -42,9 +45,7 @@ template <int L, typename F> BAL_INL float lanes(float v, F f) {
   return v;
 }
 template <int L> BAL_INL float lanes_sum(float v) { return lanes<L>(v, [](float a, float b) { return a + b; }); }
-// the larger one; NaN where one is
-BAL_INL float larger(float a, float b) { return (a > b || a != a) ? a : b; }
-template <int L> BAL_INL float lanes_max(float v) { return lanes<L>(v, larger); }
+template <int L> BAL_INL float lanes_max(float v) { return lanes<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
 // exp(d) for d <= 0 within 2 units in the last place: 2^(d log2 e) with the rounding error
 // of the product put back (the library's expf takes three times the instructions; with it
 // and a quotient a probability, one workgroup took 14.4 us for 512 tokens of 64 experts)
@@ -60,17 +61,29 @@ BAL_INL float exp_diff(float d) {
 template <int LT, int V, int J> struct Tok {
   float v[J][V] = {};
   BAL_INL static int expert(int l, int j) { return V * (LT * j + l); }
+  // (V = 4: E >= 4; the chunk that E ends in is read from E - 4 on and moved into place, so
+  // that every lane has one load to a chunk)
   BAL_INL void load(const float* row, int l, int E) {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int e = expert(l, j);
-      if (V == 4 && e + 4 <= E) {
-        const f32x4 x = *reinterpret_cast<const f32x4_any*>(row + e);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = x[i];
+      if constexpr (V == 1) {
+        v[j][0] = e < E ? row[e] : -INFINITY;
       } else {
+        const int at = min(e, E - 4), d = e - at;
+        const f32x4 x = *reinterpret_cast<const f32x4_any*>(row + at);
+        if ((E & 3) == 0) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[j][i] = e + i < E ? row[e + i] : -INFINITY;
+          for (int i = 0; i < 4; ++i) v[j][i] = d == 0 ? x[i] : -INFINITY;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float y = -INFINITY;
+#pragma unroll
+            for (int q = 3; q >= i; --q) y = d == q - i ? x[q] : y;
+            v[j][i] = y;
+          }
+        }
       }
     }
   }
@@ -78,15 +91,15 @@ template <int LT, int V, int J> struct Tok {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int e = expert(l, j);
-      if (V == 4 && e + 4 <= E) {
-        f32x4 x;
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = v[j][i];
-        *reinterpret_cast<f32x4_any*>(row + e) = x;
+      if constexpr (V == 1) {
+        if (e < E) row[e] = v[j][0];
       } else {
+        if (e + 4 <= E) *reinterpret_cast<f32x4_any*>(row + e) = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
+        if (E & 3) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (e + i < E) row[e + i] = v[j][i];
+          for (int i = 0; i < 3; ++i)
+            if (e + 4 > E && e + i < E) row[e + i] = v[j][i];
+        }
       }
     }
   }
@@ -96,7 +109,7 @@ template <int LT, int V, int J> struct Tok {
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) m = larger(m, v[j][i]);
+      for (int i = 0; i < V; ++i) m = fmaxf(m, v[j][i]);  // (a NaN makes the sum below NaN)
     m = lanes_max<LT>(m);
     if (m == -INFINITY) m = 0.f;  // (then every exp is 0)
     float s = 0.f;
@@ -109,8 +122,9 @@ template <int LT, int V, int J> struct Tok {
       }
     s = lanes_sum<LT>(s);
     if (s == 0.f) s = 1.f;
-    // a product with 1 / s where a lane holds many (one more rounding for ten fewer
-    // instructions each), quotients where it holds one or two
+    // A product with 1 / s where a lane holds many: one more rounding for ten fewer
+    // instructions each.  Where it holds one or two, the definition's own operations, each
+    // rounded: with equal counts the gradient is 0 but for these roundings.
     const float inv = __fdiv_rn(1.f, s);
 #pragma unroll
     for (int j = 0; j < J; ++j)
@@ -122,7 +136,11 @@ template <int LT, int V, int J> struct Tok {
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < V; ++i) s += v[j][i] * f[j][i];
+      for (int i = 0; i < V; ++i) {
+        float x = v[j][i] * f[j][i];
+        if (V == 1) asm("" : "+v"(x));  // (rounded before it is added)
+        s += x;
+      }
     return lanes_sum<LT>(s);
   }
 };
@@ -131,7 +149,7 @@ template <int LT, int V, int J> struct Tok {
 template <int W, int NE> struct Lds {
   int32_t hist[NE + 1];  // counts; hist[E]: kept tokens
   float col[W][NE];      // sums of probabilities
-  double loss[W];        // sums of dots
+  double loss[W];        // of the loss
 };
 
 BAL_INL double wave_sum(double v) {
@@ -167,26 +185,31 @@ template <int W> BAL_INL void count_pairs(int32_t* hist, const BalanceArgs& a, i
   __syncthreads();
 }
 
-// The tokens of this workgroup's share, U of a lane at a time: gradients out;
-// probabilities and dots summed into col[w] and loss[w] of every wavefront.  Counts and
-// kept tokens are in hist.
-template <int LT, int V, int J, int U, int W>
+// The tokens of this workgroup's share, U of a lane at a time.  SUM: probabilities summed
+// into col[w] of every wavefront.  GRAD: gradients out, from the counts and kept tokens in hist.
+template <int LT, int V, int J, int U, int W, bool SUM, bool GRAD>
 BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, int64_t parts) {
   constexpr int G = 64 / LT;  // tokens of a wavefront
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l = lane % LT, g = lane / LT;
-  const int n = L.hist[a.E];
-  const double per = n > 0 ? 1.0 / n : 0.0;
-  const float gs = (float)((double)a.alpha * a.E * per);
-  float f[J][V], sum[J][V];
-  double dots = 0.0;
+  float f[J][V], sum[J][V], gs = 0.f;
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = Tok<LT, V, J>::expert(l, j) + i;
-      f[j][i] = e < a.E ? (float)((double)L.hist[e] * per / a.k) : 0.f;
-      sum[j][i] = 0.f;
-    }
+    for (int i = 0; i < V; ++i) sum[j][i] = 0.f;
+  if constexpr (GRAD) {
+    const int n = L.hist[a.E];
+    const double per = n > 0 ? 1.0 / n : 0.0;
+    const double per_pair = per / a.k;
+    gs = (float)((double)a.alpha * a.E * per);
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int e = Tok<LT, V, J>::expert(l, j) + i;
+        const double c = e < a.E ? (double)L.hist[e] : 0.0;
+        f[j][i] = (float)(V == 1 ? c * per / a.k : c * per_pair);
+      }
+  }
   const int64_t step = parts * (W * G);
   for (int64_t t0 = part * (W * G) + w * G; t0 < a.T; t0 += U * step) {
     Tok<LT, V, J> x[U];
@@ -209,32 +232,35 @@ BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, i
 #pragma unroll
         for (int i = 0; i < V; ++i) x[u].v[j][i] = kept[u] ? x[u].v[j][i] : -INFINITY;  // probabilities 0
       x[u].softmax();
-      const float fp = x[u].dot(f);
-      dots += (double)fp;
+      if constexpr (SUM) {
 #pragma unroll
-      for (int j = 0; j < J; ++j)
+        for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float q = x[u].v[j][i];
-          sum[j][i] += q;
-          x[u].v[j][i] = kept[u] ? gs * q * (f[j][i] - fp) : 0.f;
-        }
-      if (a.grad && t < a.T) x[u].store(a.grad + t * a.E, l, a.E);
+          for (int i = 0; i < V; ++i) sum[j][i] += x[u].v[j][i];
+      }
+      if constexpr (GRAD) {
+        if (SUM && !a.grad) continue;
+        const float fp = x[u].dot(f);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int i = 0; i < V; ++i) x[u].v[j][i] = kept[u] ? gs * x[u].v[j][i] * (f[j][i] - fp) : 0.f;
+        if (t < a.T) x[u].store(a.grad + t * a.E, l, a.E);
+      }
     }
   }
-  if (l != 0) dots = 0.0;  // (a token's lanes hold the same dot)
-  dots = wave_sum(dots);
-  if (lane == 0) L.loss[w] = dots;
+  if constexpr (SUM) {
 #pragma unroll
-  for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float s = sum[j][i];
-      for (int d = LT; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
-      const int e = Tok<LT, V, J>::expert(l, j) + i;
-      if (g == 0 && e < a.E) L.col[w][e] = s;
-    }
-  __syncthreads();
+      for (int i = 0; i < V; ++i) {
+        float s = sum[j][i];
+        for (int d = LT; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
+        const int e = Tok<LT, V, J>::expert(l, j) + i;
+        if (g == 0 && e < a.E) L.col[w][e] = s;
+      }
+    __syncthreads();
+  }
 }
 
 // Small batches: everything by one workgroup.
@@ -243,119 +269,156 @@ __global__ void __launch_bounds__(1024) balance_small_kernel(BalanceArgs a) {
   constexpr int W = 16;
   __shared__ Lds<W, LT * V * J> L;
   count_pairs<W>(L.hist, a, 0, 1);
-  tokens<LT, V, J, U, W>(L, a, 0, 1);
-  const int n = L.hist[a.E];
+  tokens<LT, V, J, U, W, true, true>(L, a, 0, 1);
+  const int tid = threadIdx.x, n = L.hist[a.E];
   const double per = n > 0 ? 1.0 / n : 0.0;
-  for (int e = threadIdx.x; e < a.E; e += 64 * W) {
-    double s = 0.0;
+  double s = 0.0;
+  for (int e = tid; e < a.E; e += 64 * W) {
+    double p = 0.0;
 #pragma unroll
-    for (int i = 0; i < W; ++i) s += (double)L.col[i][e];
-    a.probs[e] = (float)(s * per);
+    for (int i = 0; i < W; ++i) p += (double)L.col[i][e];
+    p *= per;
+    a.probs[e] = (float)p;
     a.counts[e] = L.hist[e];
+    s += (double)L.hist[e] * per / a.k * p;
   }
-  if (threadIdx.x == 0) {
-    double s = 0.0;
+  s = wave_sum(s);
+  if ((tid & 63) == 0) L.loss[tid >> 6] = s;
+  __syncthreads();
+  if (tid == 0) {
+    s = 0.0;
 #pragma unroll
     for (int i = 0; i < W; ++i) s += L.loss[i];
-    a.loss[0] = (float)((double)a.alpha * a.E * per * s);
+    a.loss[0] = (float)((double)a.alpha * a.E * s);
   }
-}
-
-__global__ void __launch_bounds__(kThreads) balance_count_kernel(BalanceArgs a) {
-  __shared__ int32_t hist[kMaxE + 1];
-  count_pairs<kThreads / 64>(hist, a, blockIdx.x, gridDim.x);
-  for (int e = threadIdx.x; e <= a.E; e += kThreads) a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = hist[e];
 }
 
 template <int LT, int V, int J, int U>
-__global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs a) {
-  constexpr int W = kThreads / 64;
+__global__ void __launch_bounds__(1024) balance_sums_kernel(BalanceArgs a) {
+  constexpr int W = 16;
   __shared__ Lds<W, LT * V * J> L;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  // the counts: a wavefront adds up some of the shares, lanes along the experts
-  for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = 0;
-  __syncthreads();
-  for (int e = lane; e <= a.E; e += 64) {
-    int32_t c = 0;
-#pragma unroll 8
-    for (int i = w; i < a.n_count; i += W) c += a.part_counts[(int64_t)i * (a.E + 1) + e];
-    atomicAdd(&L.hist[e], c);
-  }
-  __syncthreads();
-  tokens<LT, V, J, U, W>(L, a, blockIdx.x, gridDim.x);
-  for (int e = tid; e < a.E; e += kThreads) {
+  count_pairs<W>(L.hist, a, blockIdx.x, gridDim.x);
+  for (int e = threadIdx.x; e <= a.E; e += 64 * W) a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = L.hist[e];
+  tokens<LT, V, J, U, W, true, false>(L, a, blockIdx.x, gridDim.x);
+  for (int e = threadIdx.x; e < a.E; e += 64 * W) {
     float s = L.col[0][e];
 #pragma unroll
     for (int i = 1; i < W; ++i) s += L.col[i][e];
     a.part_probs[(int64_t)blockIdx.x * a.E + e] = s;
   }
-  if (tid == 0) {
+}
+
+// Many shares of many experts, added in their order to the first one: 32 columns to a
+// workgroup, 16 threads each a run of the shares.
+__global__ void __launch_bounds__(512) balance_fold_kernel(BalanceArgs a, int n_part) {
+  __shared__ double sum[16][32];
+  __shared__ int32_t cnt[32];
+  const int tid = threadIdx.x, c = tid & 31, r = tid >> 5, e = blockIdx.x * 32 + c;
+  if (tid < 32) cnt[tid] = 0;
+  __syncthreads();
+  if (e <= a.E) {
+    int32_t n = 0;
+#pragma unroll 8
+    for (int i = r; i < n_part; i += 16) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
+    atomicAdd(&cnt[c], n);
+    double s = 0.0;
+    if (e < a.E)
+#pragma unroll 8
+      for (int i = r; i < n_part; i += 16) s += (double)a.part_probs[(int64_t)i * a.E + e];
+    sum[r][c] = s;
+  }
+  __syncthreads();
+  if (tid < 32 && e <= a.E) {
+    a.part_counts[e] = cnt[c];
+    if (e == a.E) return;
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < W; ++i) s += L.loss[i];
-    a.part_loss[blockIdx.x] = s;
+    for (int i = 0; i < 16; ++i) s += sum[i][c];
+    a.part_probs[e] = (float)s;
   }
 }
 
-// The shares of all workgroups, added in their order: 32 experts to a workgroup, 16
-// threads each a run of the shares.  The first workgroup also adds the loss.
-__global__ void __launch_bounds__(512) balance_sum_kernel(BalanceArgs a) {
-  __shared__ double sum[16][32];
-  __shared__ int32_t cnt[32], kept;
-  __shared__ double loss[8];
-  const int tid = threadIdx.x, c = tid & 31, r = tid >> 5, e = blockIdx.x * 32 + c;
-  if (tid < 32) cnt[tid] = 0;
-  if (tid == 0) kept = 0;
+// The first workgroup: counts, mean probabilities and loss from the shares; the others: the
+// gradient of their tokens.
+template <int LT, int V, int J, int U>
+__global__ void __launch_bounds__(kThreads) balance_grad_kernel(BalanceArgs a) {
+  constexpr int W = kThreads / 64;
+  __shared__ Lds<W, LT * V * J> L;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  if (a.n_part == 1) {
+    for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = a.part_counts[e];
+  } else {  // a wavefront adds up some of the shares, lanes along the experts
+    for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = 0;
+    __syncthreads();
+    for (int e = lane; e <= a.E; e += 64) {
+      int32_t n = 0;
+#pragma unroll 8
+      for (int i = w; i < a.n_part; i += W) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
+      atomicAdd(&L.hist[e], n);
+    }
+  }
+  if (blockIdx.x > 0) {
+    __syncthreads();
+    tokens<LT, V, J, U, W, false, true>(L, a, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  // EP threads (a power of two) along the experts, the rest of the workgroup along the shares
+  int EP = 32;
+  while (EP < a.E && EP < kThreads) EP *= 2;
+  const int c = tid & (EP - 1), r = tid / EP, R = kThreads / EP;
+  __shared__ double share[kThreads];
   __syncthreads();
-  int32_t k = 0;
-  for (int i = tid; i < a.n_count; i += 512) k += a.part_counts[(int64_t)i * (a.E + 1) + a.E];
-  if (tid < a.n_count) atomicAdd(&kept, k);
+  const int n = L.hist[a.E];
+  const double per = n > 0 ? 1.0 / n : 0.0;
   double s = 0.0;
-  if (e < a.E) {
-    int32_t n = 0;
+  for (int e0 = 0; e0 < a.E; e0 += EP) {
+    const int e = e0 + c;
+    double p = 0.0;
+    if (e < a.E)
 #pragma unroll 8
-    for (int i = r; i < a.n_count; i += 16) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
-    atomicAdd(&cnt[c], n);
-#pragma unroll 8
-    for (int i = r; i < a.n_part; i += 16) s += (double)a.part_probs[(int64_t)i * a.E + e];
+      for (int i = r; i < a.n_part; i += R) p += (double)a.part_probs[(int64_t)i * a.E + e];
+    share[tid] = p;
+    __syncthreads();
+    if (r == 0 && e < a.E) {
+      for (int i = 1; i < R; ++i) p += share[i * EP + c];
+      p *= per;
+      a.probs[e] = (float)p;
+      a.counts[e] = L.hist[e];
+      s += (double)L.hist[e] * per / a.k * p;
+    }
+    __syncthreads();
   }
-  sum[r][c] = s;
-  if (blockIdx.x == 0) {
-    double l = 0.0;
-    for (int i = tid; i < a.n_part; i += 512) l += a.part_loss[i];
-    l = wave_sum(l);
-    if ((tid & 63) == 0) loss[tid >> 6] = l;
-  }
+  s = wave_sum(s);
+  if (lane == 0) L.loss[w] = s;
   __syncthreads();
-  const double per = kept > 0 ? 1.0 / kept : 0.0;
-  if (tid < 32 && e < a.E) {
+  if (tid == 0) {
     s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sum[i][c];
-    a.probs[e] = (float)(s * per);
-    a.counts[e] = cnt[c];
-  }
-  if (blockIdx.x == 0 && tid == 0) {
-    s = 0.0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += loss[i];
-    a.loss[0] = (float)((double)a.alpha * a.E * per * s);
+    for (int i = 0; i < W; ++i) s += L.loss[i];
+    a.loss[0] = (float)((double)a.alpha * a.E * s);
   }
 }
 
 template <int LT, int V, int J> hipError_t go(const BalanceArgs& a, hipStream_t s) {
-  constexpr int U = V * J > 4 ? 1 : 4;  // tokens of a lane in flight
+  constexpr int U = V * J > 8 ? 2 : 4;  // tokens of a lane in flight
   if (a.n_part == 0) {
     hipLaunchKernelGGL((balance_small_kernel<LT, V, J, U>), dim3(1), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(balance_count_kernel, dim3(a.n_count), dim3(kThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL((balance_sums_kernel<LT, V, J, U>), dim3(a.n_part), dim3(1024), 0, s, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((balance_kernel<LT, V, J, U>), dim3(a.n_part), dim3(kThreads), 0, s, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(balance_sum_kernel, dim3((a.E + 31) / 32), dim3(512), 0, s, a);
+  BalanceArgs b = a;
+  // (every gradient workgroup reads all shares of the counts: with many experts a launch
+  // adds them up once, 8192 x 160 17.1 -> 15.8 us, 4096 x 1000 46.5 -> 22.2; 65536 x 64 19.6
+  // and 20.6 with it)
+  if (a.E > 128 && a.n_part > 1) {
+    hipLaunchKernelGGL(balance_fold_kernel, dim3((a.E + 32) / 32), dim3(512), 0, s, a, a.n_part);
+    const hipError_t f = hipGetLastError();
+    if (f != hipSuccess) return f;
+    b.n_part = 1;
+  }
+  hipLaunchKernelGGL((balance_grad_kernel<LT, V, J, U>), dim3(1 + (a.grad ? a.n_grad : 0)), dim3(kThreads), 0, s, b);
   return hipGetLastError();
 }
 
@@ -370,14 +433,14 @@ static int token_lanes(int E) {
 }
 
 // Workgroups of a call.  One for everything up to 64 wavefronts' worth of tokens (a launch costs
-// more than they do: 64 tokens of 60 experts 5.7 us against 9.2 in three launches, 256 8.7 and
-// 9.2, 512 of 64 12.0 and 10.2).  Otherwise 4096 pairs to a counting workgroup and 2048 logits
-// to one of the tokens', at most 128 and 256: more of them bring the shares of the counts in more
-// often than they save (65536 x 64: 128 / 256 21.4 us, 32 / 256 23.7, 64 / 512 23.6).
-void balance_shares(int32_t T, int32_t E, int32_t k, int32_t* n_count, int32_t* n_part) {
-  const int64_t pairs = (int64_t)T * k, logits = (int64_t)T * E;
-  *n_part = (int64_t)T * token_lanes(E) <= 64 * 64 ? 0 : (int32_t)(logits >= kBalPart * 2048 ? kBalPart : (logits + 2047) / 2048);
-  *n_count = *n_part == 0 ? 0 : (int32_t)(pairs >= kBalCount * 4096 ? kBalCount : (pairs + 4095) / 4096);
+// more than they do: 64 tokens of 60 experts 4.9 us, 7.5 in two launches; 256 7.3 and 7.9; 512
+// of 64 11.4 and 7.6).  Otherwise two tokens to a lane of a summing workgroup (65536 x 64: at
+// most 128 of them 20.6 us, 256 19.6; 4096 x 60: 60 of them 11.8, 30 11.1) and 2048 logits to
+// a gradient one.
+void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad) {
+  const int64_t waves = ((int64_t)T * token_lanes(E) + 63) / 64, logits = (int64_t)T * E;
+  *n_part = waves <= 64 ? 0 : (int32_t)std::min<int64_t>(256, (waves + 31) / 32);
+  *n_grad = (int32_t)std::min<int64_t>(512, (logits + 2047) / 2048);
 }
 
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s) {

@@ -567,22 +567,20 @@ struct DecodeArgs {
 bool decode_kind(int kind);
 hipError_t launch_linear_decode(const DecodeArgs& p, int kind, hipStream_t s);
 
-// Balance loss of the router (balance.hip).  n_count workgroups count, n_part
-// take the tokens' softmax (0: one workgroup does everything).
+// Balance loss of the router (balance.hip): n_part workgroups count and sum the
+// probabilities, n_grad write the gradient (n_part 0: one workgroup does everything).
 struct BalanceArgs {
   const float* logits;
   const int32_t* ids;
   const uint8_t* mask;
   int32_t* counts;
   float *probs, *loss, *grad;
-  int32_t* part_counts;  // [n_count][E + 1]: the share's counts and kept tokens
+  int32_t* part_counts;  // [n_part][E + 1]: the share's counts and kept tokens
   float* part_probs;     // [n_part][E]
-  double* part_loss;     // [n_part]
-  int32_t T, E, k, n_count, n_part;
+  int32_t T, E, k, n_part, n_grad;
   float alpha;
 };
-constexpr int kBalCount = 128, kBalPart = 256;  // most workgroups of each
-void balance_shares(int32_t T, int32_t E, int32_t k, int32_t* n_count, int32_t* n_part);
+void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad);
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s);
 
 }  // namespace mxmoe

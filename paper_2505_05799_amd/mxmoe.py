@@ -326,17 +326,17 @@ def linear_forward(pl: PackedLinear, a, stream=None, return_ws: bool = False):
 # (a decode step calls these once per layer: what they cost the host beside the
 # launch is one pass of checks, the outputs' allocations and the call)
 def _run_on(dev, stream, body, used):
-    """body(stream handle) with device `dev` current, on `stream` (default: the
-    device's current one); what body allocates belongs to that stream, and the
-    tensors `used` are kept until its work on them is done."""
+    """body(stream handle) with GPU `dev` current, on `stream` (default: the GPU's
+    current one); what body allocates belongs to that stream, and the tensors
+    `used` are kept until its work on them is done."""
     torch = _torch()
     if stream is None:
-        if dev.index == torch.cuda.current_device():
-            return body(torch._C._cuda_getCurrentRawStream(dev.index))
+        if dev == torch.cuda.current_device():
+            return body(torch._C._cuda_getCurrentRawStream(dev))
         with torch.cuda.device(dev):
-            return body(torch._C._cuda_getCurrentRawStream(dev.index))
-    if stream.device != dev:
-        raise ValueError(f"a stream of {stream.device} for tensors on {dev}")
+            return body(torch._C._cuda_getCurrentRawStream(dev))
+    if stream.device.index != dev:
+        raise ValueError(f"a stream of {stream.device} for tensors on GPU {dev}")
     with torch.cuda.stream(stream):
         out = body(stream.cuda_stream)
     for t in used:
@@ -347,29 +347,31 @@ def _run_on(dev, stream, body, used):
 
 def _dense(t, name, dtypes, shape, dev):
     """Raise ValueError unless t is a dense tensor of one of the dtypes, of the
-    shape, on the device; returns its address."""
-    if t.dtype not in dtypes or t.shape != shape or t.device != dev or not t.is_contiguous():
+    shape, on GPU `dev`; returns its address."""
+    if t.dtype not in dtypes or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} (strides {t.stride()}) on {t.device}, "
-                         f"expected dense {dtypes} {tuple(shape)} on {dev}")
+                         f"expected dense {dtypes} {tuple(shape)} on GPU {dev}")
     return t.data_ptr()
 
 
 def _rows(t, name, dtypes, shape, dev):
     """The same for [rows, cols] tensors whose rows lie apart by any stride; returns
     the address and the row stride."""
+    if t.dtype not in dtypes or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtypes} {tuple(shape)} on GPU {dev}")
     rows, cols = shape
-    if t.dtype not in dtypes or t.shape != shape or t.device != dev:
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtypes} {tuple(shape)} on {dev}")
     ld, one = t.stride()
     if (one != 1 and cols > 1) or (ld < cols and rows > 1):
         raise ValueError(f"{name}: strides {t.stride()}; rows of elements side by side, apart from each other, are expected")
     return t.data_ptr(), (ld if rows > 1 else max(cols, 1))
 
 
-def _cuda_2d(t, name):
-    if t.dim() != 2 or not t.is_cuda:
+def _gpu_of(t, name):
+    """Index of the GPU that holds a [rows, columns] tensor."""
+    dev = t.get_device()
+    if dev < 0 or t.dim() != 2:
         raise ValueError(f"{name}: a [rows, columns] tensor on a GPU is expected, got {tuple(t.shape)} on {t.device}")
-    return t.device
+    return dev
 
 
 def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, want_y: bool = True, sum_out=None,
@@ -383,8 +385,8 @@ def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, wan
     448: FP8 e4m3 bytes in an int8 tensor, with fp32 scales per row (linear_decode
     takes them); 0: neither."""
     torch = _torch()
-    lib = load_library()
-    dev = _cuda_2d(x, "x")
+    lib = _lib or load_library()
+    dev = _gpu_of(x, "x")
     dt = x.dtype
     if dt is torch.bfloat16:
         act = BF16
@@ -398,29 +400,27 @@ def add_rms_norm(x, weight, residual=None, eps: float = 1e-6, qmax: int = 0, wan
     xp, ldx = _rows(x, "x", own, shape, dev)
     wp = _dense(weight, "weight", own, (cols,), dev)
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", own, shape, dev)
+    zp, ldz = None, cols
     if sum_out is not None:
         if residual is None:
             raise ValueError("sum_out: there is no sum without a residual")
-        _rows(sum_out, "sum_out", own, shape, dev)
+        zp, ldz = _rows(sum_out, "sum_out", own, shape, dev)
 
     def body(s):
-        y = z = codes = scales = yp = zp = cp = sp = None
-        ldz = cols
-        if residual is not None:
-            if sum_out is None:
-                z = torch.empty(shape, dtype=dt, device=dev)
-            else:
-                z = sum_out
-                ldz = z.stride(0) if rows > 1 else cols
-            zp = z.data_ptr()
+        d = x.device
+        y = codes = scales = yp = cp = sp = None
+        z, p = sum_out, zp
+        if residual is not None and z is None:
+            z = torch.empty(rows, cols, dtype=dt, device=d)
+            p = z.data_ptr()
         if want_y:
-            y = torch.empty(shape, dtype=dt, device=dev)
+            y = torch.empty(rows, cols, dtype=dt, device=d)
             yp = y.data_ptr()
         if qmax:
-            codes = torch.empty(shape, dtype=torch.int8, device=dev)
-            scales = torch.empty(rows, dtype=torch.float32, device=dev)
+            codes = torch.empty(rows, cols, dtype=torch.int8, device=d)
+            scales = torch.empty(rows, dtype=torch.float32, device=d)
             cp, sp = codes.data_ptr(), scales.data_ptr()
-        st = lib.mxmoe_add_rms_norm(xp, ldx, rp, ldr, wp, act, rows, cols, eps, zp, ldz, yp, cols, qmax, cp, sp, s)
+        st = lib.mxmoe_add_rms_norm(xp, ldx, rp, ldr, wp, act, rows, cols, eps, p, ldz, yp, cols, qmax, cp, sp, s)
         if st:
             raise MxmoeError(st, "mxmoe_add_rms_norm")
         return y, z, codes, scales
@@ -434,38 +434,36 @@ def linear_decode(pl: PackedLinear, a, scales=None, bias=None, out=None, stream=
     codes [m, k] and scales [m] of act_quant or add_rms_norm.  Rows of any stride
     (copied if not 16-byte aligned)."""
     torch = _torch()
-    lib = load_library()
-    dev = _cuda_2d(a, "a")
-    q = pl.q
-    m, n = a.shape[0], q.n
+    lib = _lib or load_library()
+    dev = _gpu_of(a, "a")
+    q, buf = pl.q, pl.buf
+    n, k, coded = q.n, q.k, q.scheme.a_bits < 16
+    m = a.shape[0]
     act, dt = (BF16, torch.bfloat16) if pl.act == "bf16" else (F16, torch.float16)
-    coded = q.scheme.a_bits < 16
-    ap, lda = _rows(a, "a", (torch.int8, torch.uint8) if coded else (dt,), (m, q.k), dev)
-    if pl.buf.device != dev:
-        raise ValueError(f"a: on {dev}, the packed weights on {pl.buf.device}")
+    ap, lda = _rows(a, "a", (torch.int8, torch.uint8) if coded else (dt,), (m, k), dev)
+    if buf.get_device() != dev:
+        raise ValueError(f"a: on GPU {dev}, the packed weights on {buf.device}")
     if coded != (scales is not None):
         raise ValueError(f"{q.scheme.name}: scales are the rows' of 8-bit codes")
     sp = None if scales is None else _dense(scales, "scales", (torch.float32,), (m,), dev)
     bp = None if bias is None else _dense(bias, "bias", (dt,), (n,), dev)
-    if out is not None:
-        op, ldo = _rows(out, "out", (dt,), (m, n), dev)
+    op, ldo = (None, n) if out is None else _rows(out, "out", (dt,), (m, n), dev)
 
     def body(s):
         rows, rp, ldr = a, ap, lda
         if rp % 16 or (m > 1 and ldr * (1 if coded else 2) % 16):
             rows = a.clone(memory_format=torch.contiguous_format)
-            rp, ldr = rows.data_ptr(), q.k
-        if out is None:
-            o = torch.empty((m, n), dtype=dt, device=dev)
-            p, ld = o.data_ptr(), n
-        else:
-            o, p, ld = out, op, ldo
-        st = lib.mxmoe_linear_decode(C.byref(pl.L), act, pl.buf.data_ptr(), m, rp, ldr, sp, bp, p, ld, s)
+            rp, ldr = rows.data_ptr(), k
+        o, p = out, op
+        if o is None:
+            o = torch.empty(m, n, dtype=dt, device=a.device)
+            p = o.data_ptr()
+        st = lib.mxmoe_linear_decode(C.byref(pl.L), act, buf.data_ptr(), m, rp, ldr, sp, bp, p, ldo, s)
         if st:
             raise MxmoeError(st, "mxmoe_linear_decode")
         return o
 
-    return _run_on(dev, stream, body, (a, scales, bias, out, pl.buf))
+    return _run_on(dev, stream, body, (a, scales, bias, out, buf))
 
 
 def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_grad: bool = True, stream=None):
@@ -477,8 +475,8 @@ def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_gra
     ``torch.autograd.backward([out, logits], [None, grad])``; alpha takes its
     factor."""
     torch = _torch()
-    lib = load_library()
-    dev = _cuda_2d(logits, "logits")
+    lib = _lib or load_library()
+    dev = _gpu_of(logits, "logits")
     shape = logits.shape
     T, E = shape
     lp = _dense(logits, "logits", (torch.float32,), shape, dev)
@@ -490,11 +488,12 @@ def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_gra
     wsb = lib.mxmoe_balance_workspace_bytes(T, E)
 
     def body(s):
-        counts = torch.empty(E, dtype=torch.int32, device=dev)
-        probs = torch.empty(E, dtype=torch.float32, device=dev)
-        loss = torch.empty((), dtype=torch.float32, device=dev)
-        grad = torch.empty(shape, dtype=torch.float32, device=dev) if want_grad else None
-        ws = torch.empty(wsb, dtype=torch.uint8, device=dev) if wsb else None
+        d = logits.device
+        counts = torch.empty(E, dtype=torch.int32, device=d)
+        probs = torch.empty(E, dtype=torch.float32, device=d)
+        loss = torch.empty((), dtype=torch.float32, device=d)
+        grad = torch.empty(T, E, dtype=torch.float32, device=d) if want_grad else None
+        ws = torch.empty(wsb, dtype=torch.uint8, device=d) if wsb else None
         st = lib.mxmoe_balance_loss(lp, ip, mp, T, E, k, alpha, counts.data_ptr(), probs.data_ptr(), loss.data_ptr(),
                                     grad.data_ptr() if want_grad else None, ws.data_ptr() if wsb else None, wsb, s)
         if st:
