@@ -543,6 +543,129 @@ def test_two_streams_at_once():
             _same(torch, a, b)
 
 
+def test_norm_more_rows_than_workgroups():
+    """Row counts past the largest grid (workgroups then take several rows): eight rows
+    repeated give their outputs repeated."""
+    torch = torch_mod()
+    for rows, cols in ((33_600_000, 3), (4_400_000, 300)):
+        rng = np.random.default_rng(cols)
+        x, w = norm_rows(rng, 8, cols, "bf16"), norm_rows(rng, 1, cols, "bf16")
+        few, wt = M.act_tensor(x, "bf16"), M.act_tensor(w, "bf16")[0]
+        y8, _, c8, s8 = M.add_rms_norm(few, wt, qmax=127)
+        check_norm(x, None, w, "bf16", 127, (y8, None, c8, s8))
+        y, _, c, s = M.add_rms_norm(few.repeat(rows // 8, 1), wt, qmax=127)
+        assert bool((y.view(rows // 8, 8, cols) == y8).all()) and bool((c.view(rows // 8, 8, cols) == c8).all())
+        assert bool((s.view(rows // 8, 8) == s8).all())
+        del y, c, s
+        torch.cuda.empty_cache()
+
+
+def test_decode_largest_weight():
+    """Weights whose byte offsets pass 31 bits: the last channels of 131056 x 16384."""
+    torch = torch_mod()
+    n, k, m = 131056, 16384, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    codes = torch.randint(-127, 128, (n, k), generator=g, device="cuda", dtype=torch.int8)
+    scales = torch.rand(n, generator=g, device="cuda") * 1e-3
+    pl = M.PackedLinear(W.QLinear(W.W8A8, n, k, codes, scales), "bf16")
+    a = torch.randint(-127, 128, (m, k), generator=g, device="cuda", dtype=torch.int8)
+    sa = torch.rand(m, generator=g, device="cuda") * 1e-2
+    out = M.linear_decode(pl, a, scales=sa)
+    for lo in (0, n - 64):
+        want = (a.double() @ codes[lo:lo + 64].double().t().contiguous()) * sa.double()[:, None] * scales[lo:lo + 64].double()
+        want = want.cpu().numpy()
+        got = O.act_values(M.act_numpy(out[:, lo:lo + 64], "bf16"), "bf16")
+        assert np.all(np.abs(got - want) <= TL.slot_bound(want, 4 * TL.U32 * np.abs(want), "bf16"))
+    del codes, pl, out
+    torch.cuda.empty_cache()
+
+
+def test_decode_poisoned_channel():
+    """A channel whose packed scale is NaN (a zero point outside its range) is NaN, its
+    neighbours are not."""
+    torch = torch_mod()
+    q = W.quantize_linear(W.draw_weight(3, 1, 0, 48, 512), W.W4G128)
+    ref = M.PackedLinear(q, "bf16")
+    zeros = q.zeros.copy()
+    zeros[19, 2] = 16.0
+    bad = M.PackedLinear(W.QLinear(q.scheme, q.n, q.k, q.codes, q.scales, zeros), "bf16")
+    for m in (1, 7, 40):
+        a = torch.randn(m, 512, device="cuda").bfloat16()
+        x, y = M.linear_decode(ref, a), M.linear_decode(bad, a)
+        assert bool(torch.isnan(y[:, 19]).all())
+        keep = [c for c in range(48) if c != 19]
+        assert torch.equal(x[:, keep], y[:, keep])
+
+
+def _larger(torch):
+    """One call of each operator at a size that takes several workgroups and launches."""
+    rng = np.random.default_rng(6)
+    x, res = (M.act_tensor(norm_rows(rng, 600, 5000, "fp16"), "fp16") for _ in range(2))
+    w = M.act_tensor(norm_rows(rng, 1, 5000, "fp16"), "fp16")[0]
+    q, pl, a, sc, bt, ad, b = decode_case(W.FP8, "bf16", 40, 2064, 1408, 1, True)
+    q4, pl4, a4, *_ = decode_case(W.W4G128, "fp16", 60, 12800, 384, 1, False)
+    cases = []
+    for T, E, k in ((3000, 200, 4), (5000, 60, 4)):
+        l, ids, mask = balance_case(T, E, k, 5, 0.2)
+        cases.append([torch.from_numpy(v).cuda() for v in (l, ids, mask)])
+
+    def run():
+        out = list(M.add_rms_norm(x, w, residual=res, qmax=448))
+        out += [M.linear_decode(pl, a, scales=sc, bias=bt), M.linear_decode(pl4, a4)]
+        for l, ids, mask in cases:
+            out += M.balance_loss(l, ids, token_mask=mask)
+        return out
+    return run
+
+
+def test_larger_calls_in_a_graph():
+    """Captured and replayed, with eager calls and synchronizations in between, and twice
+    in a row: the same bits."""
+    torch = torch_mod()
+    run = _larger(torch)
+    ref = run()
+    _same(torch, ref, run())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cap = run()
+    for rep in range(3):
+        for t in cap:
+            t.reshape(-1).view(torch.uint8).zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        _same(torch, ref, cap)
+        _same(torch, ref, run())
+        torch.cuda.synchronize()
+
+
+def test_side_stream_memory_is_kept():
+    """Inputs dropped right after a call on another stream stay whole until it has run:
+    the calls hold them back from the allocator."""
+    torch = torch_mod()
+    s = torch.cuda.Stream()
+    x = torch.randn(2048, 4096, device="cuda").bfloat16()
+    w = torch.ones(4096, dtype=torch.bfloat16, device="cuda")
+    want = M.add_rms_norm(x, w)[0]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        tmp = x.clone()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(2_000_000)                 # the call waits behind this
+        y = M.add_rms_norm(tmp, w, stream=s)[0]
+        del tmp
+        for _ in range(4):
+            torch.full((2048, 4096), 7.0, dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        assert torch.equal(y.view(torch.int16), want.view(torch.int16))
+
+
 def test_far_offsets():
     """Rows whose byte offsets pass 32 bits: the rows at the end of a 5 GB buffer."""
     torch = torch_mod()
