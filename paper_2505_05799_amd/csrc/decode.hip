@@ -192,15 +192,17 @@ __global__ void __launch_bounds__(64 * NW) decode_wave_kernel(DecodeArgs p) {
   const uint8_t* wb[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) wb[b] = p.packed + (int64_t)min(nb0 + b, nbs - 1) * kbs * block_bytes(KD);
-  // lane 4 i + q brings piece 4 j + q of row i of a fragment; element (i, q) of the
-  // fragment lies at 16 q + (i + 4 q) % 16
+  // lane 4 i + q brings piece 4 j + q of row i of a fragment, which lies at 16 q + (i ^ 2 q): the
+  // lanes that a 16-byte LDS operation serves together, lanes 0-3 and 20-23, 4-7 and 16-19
+  // and so on, then meet 8 different sets of banks both in the writes and in the reads
+  // (with (i + 4 q) % 16 a third of the kernel's time were conflicts)
   const int mi = lane >> 2, mq = lane & 3;
   const uint8_t* src[MF];
 #pragma unroll
   for (int f = 0; f < MF; ++f)
     src[f] = reinterpret_cast<const uint8_t*>(p.a) + (int64_t)min(16 * f + mi, p.m - 1) * p.lda * ES + 16 * mq;
-  u32x4* put = buf + w * (MF * P * 64) + 16 * mq + ((mi + 4 * mq) & 15);
-  const u32x4* get = buf + w * (MF * P * 64) + 16 * qd + ((li + 4 * qd) & 15);
+  u32x4* put = buf + w * (MF * P * 64) + 16 * mq + (mi ^ (2 * mq));
+  const u32x4* get = buf + w * (MF * P * 64) + 16 * qd + (li ^ (2 * qd));
   u32x4 st[MF][P];
   Wgt<KD> cur[NB], nxt[NB];
   auto load = [&](Wgt<KD> (&g)[NB], int kb) {
