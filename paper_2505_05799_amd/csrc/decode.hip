@@ -382,6 +382,7 @@ template <int KD, int ACT> hipError_t launch(const DecodeArgs& p, hipStream_t s)
   if (p.m == 1) return p.n <= 4096 && p.k >= 4096 ? go_one<KD, ACT, 16>(p, s) : go_one<KD, ACT, 8>(p, s);
   if (p.m <= 16) return launch_rows<KD, ACT, 1>(p, s);
   if (p.m <= 32) return launch_rows<KD, ACT, 2>(p, s);
+  if (p.m <= 48) return launch_rows<KD, ACT, 3>(p, s);
   return launch_rows<KD, ACT, 4>(p, s);
 }
 
