@@ -236,7 +236,8 @@ MXMOE_API mxmoe_status mxmoe_act_quant(const void* a, mxmoe_dtype act, int32_t r
 /* Residual addition, RMS norm and per-row 8-bit encoding, one launch:
  *   z = round(x + residual)                       (to `act`; x without residual)
  *   r = fl32(1 / sqrt(mean over the row of z^2 + eps)), mean, root and quotient
- *       in 64 bits (the same bits whatever the order of the sum)
+ *       in 64 bits (another order of the sum gives other bits of r for about one
+ *       row in 2^25)
  *   y = round(fl32(fl32(z * r) * weight))         (to `act`)
  *   codes, scales: of the rounded y, with the recipe and formats of
  *       mxmoe_act_quant for qmax = 127 (int8) or 448 (FP8 e4m3); the codes that
@@ -250,10 +251,10 @@ MXMOE_API mxmoe_status mxmoe_act_quant(const void* a, mxmoe_dtype act, int32_t r
  *   y       : row stride ldy, or NULL if only the codes are wanted
  *   qmax    : 0 (codes and scales NULL), 127 or 448 (UNSUPPORTED otherwise)
  *   codes   : int8 [rows, cols] dense, scales: fp32 [rows]
- * 16-bit pointers 2-byte, scales 4-byte aligned; rows whose pointers and strides
- * are multiples of 16 bytes take the wide path, others the same results.  sum and
- * y may each be x or residual itself (same pointer and stride), but not share
- * bytes with them otherwise, nor with each other, weight, codes or scales.
+ * 16-bit pointers 2-byte, scales 4-byte aligned; any row strides up to 2^40 bytes
+ * over all rows.  sum and y may each be x or residual itself (same pointer and
+ * stride), but not share bytes with them otherwise, nor with each other, weight,
+ * codes or scales.
  * 1e-30 <= eps <= 1e30 (the factor is finite), cols <= 2^24.
  * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                     */
 MXMOE_API mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr,
@@ -289,9 +290,12 @@ MXMOE_API mxmoe_status mxmoe_linear_forward(const mxmoe_linear* L, mxmoe_dtype a
 /* One packed linear on the few rows of a decode step, one launch without plan or
  * workspace: out = a W^T + bias, rounded once to `act`.
  *   wNg128 with N = 4: a `act` [m, k], a_scales NULL; per group the exact sum of
- *       a * (q - z) in fp32, times the group's scale, added over the groups;
+ *       a * (q - z) in fp32, times the group's scale, added over the groups; a row
+ *       that is not finite throughout has no finite output, and neither may a bf16
+ *       row have one whose sum of 143 |a| over a group passes the largest fp32;
  *   w8a8: a int8 [m, k] codes, a_scales fp32 [m] (mxmoe_act_quant with qmax 127
- *       or mxmoe_add_rms_norm): exact int32 sums times a_scales[m] * s_w[n];
+ *       or mxmoe_add_rms_norm): exact int32 sums times a_scales[m] * s_w[n]
+ *       (k < 2^17, UNSUPPORTED beyond);
  *   fp8:  a e4m3 bytes [m, k], a_scales fp32 [m] (qmax 448): products
  *       accumulated in fp32 by the FP8 MFMA, times a_scales[m] * s_w[n];
  *   other schemes: UNSUPPORTED (mxmoe_linear_forward takes them, and more rows).

@@ -431,7 +431,9 @@ bool overlap(const Rows& a, const Rows& b) {
   return d < a.bytes || a.pitch - d < b.bytes;
 }
 bool same_rows(const Rows& a, const Rows& b) { return a.p == b.p && (a.pitch == b.pitch || a.rows == 1); }
-constexpr int64_t kMaxPitch = (int64_t)1 << 38;  // bytes; more than the device's memory is a mistake
+constexpr int64_t kMaxSpan = (int64_t)1 << 40;  // bytes; what exceeds the device's memory is a mistake
+// Whether rows of `cols` elements of es bytes may lie ld elements apart.
+bool row_stride_ok(int64_t ld, int64_t cols, int es, int64_t rows) { return ld >= cols && ld <= kMaxSpan / es / rows; }
 constexpr int32_t kMaxNormCols = 1 << 24;
 }  // namespace
 
@@ -445,9 +447,8 @@ mxmoe_status mxmoe_add_rms_norm(const void* x, int64_t ldx, const void* residual
   if (rows == 0) return MXMOE_OK;
   if (!x || !weight || (!y && !qmax) || (sum && !residual)) return MXMOE_ERR_INVALID_ARG;
   if (qmax ? (!codes || !scales) : (codes || scales)) return MXMOE_ERR_INVALID_ARG;
-  const int64_t most = kMaxPitch / 2;
-  if (ldx < cols || ldx > most || (residual && (ldr < cols || ldr > most)) || (sum && (lds < cols || lds > most)) ||
-      (y && (ldy < cols || ldy > most)))
+  if (!row_stride_ok(ldx, cols, 2, rows) || (residual && !row_stride_ok(ldr, cols, 2, rows)) ||
+      (sum && !row_stride_ok(lds, cols, 2, rows)) || (y && !row_stride_ok(ldy, cols, 2, rows)))
     return MXMOE_ERR_INVALID_ARG;
   if (!aligned(x, 2) || !aligned(residual, 2) || !aligned(weight, 2) || !aligned(sum, 2) || !aligned(y, 2) ||
       !aligned(scales, 4))
@@ -637,10 +638,11 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
   if (st != MXMOE_OK) return st;
   if (!valid_dtype(act) || m < 0) return MXMOE_ERR_INVALID_ARG;
   if (!decode_kind(kd) || m > MXMOE_DECODE_ROWS) return MXMOE_ERR_UNSUPPORTED;
+  if (kd == K_W8A8 && L->k >= 1 << 17) return MXMOE_ERR_UNSUPPORTED;  // a sum of k products of 2^14 may leave int32
   if (m == 0) return MXMOE_OK;
   const int es = kind_is_int(kd) ? 1 : 2;
   if (!packed || !a || !out || (es == 1) != (a_scales != nullptr)) return MXMOE_ERR_INVALID_ARG;
-  if (lda < L->k || lda > kMaxPitch / es || ldo < L->n || ldo > kMaxPitch / 2) return MXMOE_ERR_INVALID_ARG;
+  if (!row_stride_ok(lda, L->k, es, m) || !row_stride_ok(ldo, L->n, 2, m)) return MXMOE_ERR_INVALID_ARG;
   if (!aligned(packed, 256) || !aligned(a, 16) || (m > 1 && lda * es % 16) || !aligned(a_scales, 4) || !aligned(bias, 2) ||
       !aligned(out, 2))
     return MXMOE_ERR_INVALID_ARG;

@@ -6,9 +6,9 @@
 //   codes, scale = the per-token recipe of rowquant.h on the rounded y
 //
 // The squares of 16-bit values are exact in 64 bits and their sum errs by some
-// 2^-50, so r is the same whatever the order of the sum, and with it every bit
-// of y, the codes and the scale: they equal act_quant of y, for any split of a
-// row over lanes.
+// 2^-50 of it, so another split of a row over lanes gives another r, by one unit in its
+// last place, for about one row in 2^25 only.  The codes and the scale equal act_quant of
+// the rounded y always.
 //
 // A row is read once: its elements stay in registers, 8 to a lane and chunk, and
 // turn from x into z into y in place.  Rows whose pointers or strides are not

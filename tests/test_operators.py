@@ -150,6 +150,14 @@ def test_norm_refuses_unsupported_and_takes_nothing(lib):
     assert norm_call(lib, rows=0, x=None, res=None, w=None, sum_=None, y=None, codes=None, scales=None) == M.OK
 
 
+def test_norm_refuses_spans_past_any_memory(lib):
+    """Strides whose product with the rows passes 2^40 bytes (2^63 among them)."""
+    far = 1 << 37
+    for bad in (dict(ldx=far), dict(ldr=far), dict(lds=far), dict(ldy=far)):
+        assert norm_call(lib, rows=1 << 30, **bad) == M.ERR_INVALID_ARG
+        assert norm_call(lib, rows=8, **bad) == M.ERR_INVALID_ARG
+
+
 def decode_call(lib, scheme=W.W4G128, n=64, k=256, act=M.BF16, packed=at(1), m=4, a=at(2), lda=256, scales=None,
                 bias=at(4), out=at(5), ldo=64):
     L = M.Linear_t(n, k, M.scheme_t(scheme))
@@ -177,6 +185,8 @@ def test_decode_refuses_unsupported_and_takes_nothing(lib):
     assert decode_call(lib, m=M.DECODE_ROWS + 1) == M.ERR_UNSUPPORTED
     assert decode_call(lib, n=72) == M.ERR_UNSUPPORTED
     assert decode_call(lib, k=200) == M.ERR_UNSUPPORTED
+    # codes of -128 on both sides: 2^17 products of 2^14 pass the int32 sums
+    assert decode_call(lib, scheme=W.W8A8, scales=at(3), k=1 << 17, lda=1 << 17) == M.ERR_UNSUPPORTED
     assert decode_call(lib, m=0, packed=None, a=None, out=None) == M.OK
 
 
