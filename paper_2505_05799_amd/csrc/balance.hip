@@ -308,6 +308,24 @@ __global__ void __launch_bounds__(1024) balance_sums_kernel(BalanceArgs a) {
   }
 }
 
+// p[i * stride] of the shares i = first, first + step, ..., added in that order, eight on their
+// way at a time, the last ones too (one by one, each costs a trip to memory).
+template <typename S, typename P> BAL_INL S add_shares(const P* p, int stride, int first, int step, int n_part) {
+  S s = 0;
+  int i = first;
+  for (; i + 7 * step < n_part; i += 8 * step)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += (S)p[(i + u * step) * stride];
+  if (i < n_part) {
+    P v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = p[min(i + u * step, n_part - 1) * stride];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += i + u * step < n_part ? (S)v[u] : (S)0;
+  }
+  return s;
+}
+
 // Many shares of many experts, added in their order to the first one: 32 columns to a
 // workgroup, 16 threads each a run of the shares.
 __global__ void __launch_bounds__(512) balance_fold_kernel(BalanceArgs a, int n_part) {
@@ -317,15 +335,8 @@ __global__ void __launch_bounds__(512) balance_fold_kernel(BalanceArgs a, int n_
   if (tid < 32) cnt[tid] = 0;
   __syncthreads();
   if (e <= a.E) {
-    int32_t n = 0;
-#pragma unroll 8
-    for (int i = r; i < n_part; i += 16) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
-    atomicAdd(&cnt[c], n);
-    double s = 0.0;
-    if (e < a.E)
-#pragma unroll 8
-      for (int i = r; i < n_part; i += 16) s += (double)a.part_probs[(int64_t)i * a.E + e];
-    sum[r][c] = s;
+    atomicAdd(&cnt[c], add_shares<int32_t>(a.part_counts + e, a.E + 1, r, 16, n_part));
+    sum[r][c] = e < a.E ? add_shares<double>(a.part_probs + e, a.E, r, 16, n_part) : 0.0;
   }
   __syncthreads();
   if (tid < 32 && e <= a.E) {
@@ -344,18 +355,13 @@ template <int LT, int V, int J, int U>
 __global__ void __launch_bounds__(kThreads) balance_grad_kernel(BalanceArgs a) {
   constexpr int W = kThreads / 64;
   __shared__ Lds<W, LT * V * J> L;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (a.n_part == 1) {
     for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = a.part_counts[e];
   } else {  // a wavefront adds up some of the shares, lanes along the experts
     for (int e = tid; e <= a.E; e += kThreads) L.hist[e] = 0;
     __syncthreads();
-    for (int e = lane; e <= a.E; e += 64) {
-      int32_t n = 0;
-#pragma unroll 8
-      for (int i = w; i < a.n_part; i += W) n += a.part_counts[(int64_t)i * (a.E + 1) + e];
-      atomicAdd(&L.hist[e], n);
-    }
+    for (int e = lane; e <= a.E; e += 64) atomicAdd(&L.hist[e], add_shares<int32_t>(a.part_counts + e, a.E + 1, w, W, a.n_part));
   }
   if (blockIdx.x > 0) {
     __syncthreads();
@@ -373,10 +379,7 @@ __global__ void __launch_bounds__(kThreads) balance_grad_kernel(BalanceArgs a) {
   double s = 0.0;
   for (int e0 = 0; e0 < a.E; e0 += EP) {
     const int e = e0 + c;
-    double p = 0.0;
-    if (e < a.E)
-#pragma unroll 8
-      for (int i = r; i < a.n_part; i += R) p += (double)a.part_probs[(int64_t)i * a.E + e];
+    double p = e < a.E ? add_shares<double>(a.part_probs + e, a.E, r, R, a.n_part) : 0.0;
     share[tid] = p;
     __syncthreads();
     if (r == 0 && e < a.E) {
@@ -409,10 +412,12 @@ template <int LT, int V, int J> hipError_t go(const BalanceArgs& a, hipStream_t 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   BalanceArgs b = a;
-  // (every gradient workgroup reads all shares of the counts: with many experts a launch
-  // adds them up once, 8192 x 160 17.1 -> 15.8 us, 4096 x 1000 46.5 -> 22.2; 65536 x 64 19.6
-  // and 20.6 with it)
-  if (a.E > 128 && a.n_part > 1) {
+  // (every gradient workgroup reads all shares of the counts: where they are many, a launch
+  // adds them up once.  us without / with it, shares x experts: 256 x 128 18.0 / 15.6, 256 x 256
+  // 27.8 / 21.7, 128 x 160 13.1 / 11.9, 256 x 64 19.6 / 20.5, 64 x 256 11.2 / 11.5, 64 x 128
+  // 10.0 / 11.4; and, as a wavefront goes through the experts 64 at a time, 32 x 512 14.2 / 13.2,
+  // 10 x 1000 19.9 / 15.5)
+  if (a.n_part > 1 && (a.n_part * a.E > 16384 || a.E > 256)) {
     hipLaunchKernelGGL(balance_fold_kernel, dim3((a.E + 32) / 32), dim3(512), 0, s, a, a.n_part);
     const hipError_t f = hipGetLastError();
     if (f != hipSuccess) return f;
@@ -433,13 +438,14 @@ static int token_lanes(int E) {
 }
 
 // Workgroups of a call.  One for everything up to 64 wavefronts' worth of tokens (a launch costs
-// more than they do: 64 tokens of 60 experts 4.9 us, 7.5 in two launches; 256 7.3 and 7.9; 512
-// of 64 11.4 and 7.6).  Otherwise two tokens to a lane of a summing workgroup (65536 x 64: at
-// most 128 of them 20.6 us, 256 19.6; 4096 x 60: 60 of them 11.8, 30 11.1) and 2048 logits to
-// a gradient one.
+// more than they do: 64 tokens of 60 experts 5.0 us, 6.6 in two launches; 256 7.3 and 7.5; 512
+// of 64 11.1 and 8.2).  Otherwise a token to a lane of a summing workgroup up to 64 of them (4096 x
+// 60: 64 of them 9.1 us, 32 9.8, 16 11.2; 1000 x 512: 63 of them 11.8, 32 13.3), then two, as the
+// shares cost too (4096 x 128: 128 of them 10.7, 64 10.0; 65536 x 64: 256 19.6, 128 20.4), and 2048
+// logits to a gradient one.
 void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad) {
   const int64_t waves = ((int64_t)T * token_lanes(E) + 63) / 64, logits = (int64_t)T * E;
-  *n_part = waves <= 64 ? 0 : (int32_t)std::min<int64_t>(256, (waves + 31) / 32);
+  *n_part = waves <= 64 ? 0 : (int32_t)std::max(std::min<int64_t>(64, (waves + 15) / 16), std::min<int64_t>(256, (waves + 31) / 32));
   *n_grad = (int32_t)std::min<int64_t>(512, (logits + 2047) / 2048);
 }
 

@@ -147,7 +147,7 @@ DEC_INL void wave_order() {
 
 // ---- One row, straight from memory.  NW wavefronts share 16 channels; a wavefront's
 // next k block is asked for before this one is used.  4096 x 4096 w4g128 3.9 us a launch in
-// a graph (one wavefront for all k blocks: 10.7); 20480 x 3584 9.7 us, 4.0 TB/s.
+// a graph (one wavefront for all k blocks: 10.7); 20480 x 3584 9.9 us, 3.9 TB/s.
 template <int KD, int ACT, int NW>
 __global__ void __launch_bounds__(64 * NW) decode_one_kernel(DecodeArgs p) {
   __shared__ Acc<KD> red[NW * 64];
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(64 * NW) decode_one_kernel(DecodeArgs p) {
 // addresses a load, lane by lane, where the cache serves four lanes at a time that read 64
 // bytes side by side (64 rows of fp8, 4096 x 14336: 28.9 us, bound by that).  So four lanes
 // bring a row's 64 bytes, and the wavefront turns them into a fragment through 1 KB of LDS
-// of its own, without a barrier: 16.2 us, 3.6 TB/s.  Its next k block, weights and rows, is on
+// of its own, without a barrier: 16.0 us, 3.7 TB/s.  Its next k block, weights and rows, is on
 // its way meanwhile.  NB blocks of channels use the fragments.
 template <int KD, int ACT, int MF, int NW, int NB>
 __global__ void __launch_bounds__(64 * NW) decode_wave_kernel(DecodeArgs p) {
@@ -352,13 +352,13 @@ template <int KD, int ACT, int MF, int NB> hipError_t go_rows(const DecodeArgs& 
 // Rows of a call in MF fragments, nb blocks of 16 channels.
 template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, hipStream_t s) {
   const int nb = p.n / 16;
-  // 33 and more 16-bit rows, wide linears: a workgroup's rows shared by 4 or 6 blocks (64 x 20480 x
-  // 3584 22.8 us, 27.7 by wavefronts; 64 x 16384 x 2048 12.7, 15.7; 64 x 12288 x 4096 24.2, 16.6)
+  // 49 and more 16-bit rows, wide linears: a workgroup's rows shared by 4 or 6 blocks (64 x 20480 x
+  // 3584 23.0 us, 26.0 by wavefronts; 64 x 16384 x 2048 12.6, 15.6; 64 x 12288 x 4096 19.7, 16.4)
   if constexpr (KD == K_W4G && MF == 4)
     if (nb > 768) return (nb + 1535) / 1536 * 4 <= (nb + 1023) / 1024 * 3 ? go_rows<KD, ACT, MF, 3>(p, s) : go_rows<KD, ACT, MF, 2>(p, s);
   // Blocks of a workgroup: what the busiest CU does, its workgroups times the rows (about the
-  // weights of one block) and their blocks.  16 x 8192 x 4096 w4g128 with 1, 2, 3 blocks 7.1, 6.2,
-  // 7.4; 32 x 12288 x 4096 13.7, 14.0, 10.4; 64 x 4096 x 14336 fp8 16.2, 18.7, 22.3.
+  // weights of one block) and their blocks.  16 x 8192 x 4096 w4g128 with 1, 2, 3 blocks 6.7, 6.2,
+  // 7.5; 32 x 12288 x 4096 14.0, 13.9, 10.7; 64 x 4096 x 14336 fp8 15.9, 18.8, 22.3.
   int NB = 1, best = 0;
   for (int b = 1; b <= 3; ++b) {
     const int cost = ((nb + b - 1) / b + 255) / 256 * (1 + b);
@@ -367,8 +367,8 @@ template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, h
       best = cost;
     }
   }
-  // 8 wavefronts where a CU has one workgroup, else 4 (64 x 20480 x 3584 int8, 3 blocks: 21.1 and
-  // 17.5; 64 x 8192 x 4096, 2 blocks: 9.8 and 10.2)
+  // 8 wavefronts where a CU has one workgroup, else 4 (64 x 20480 x 3584 int8, 3 blocks: 21.2 and
+  // 17.7; 64 x 8192 x 4096, 2 blocks: 9.8 and 10.1)
   const bool one = (nb + NB - 1) / NB <= 256;
   if (NB == 1) return go_wave<KD, ACT, MF, 8, 1>(p, s);
   if (NB == 2) return one ? go_wave<KD, ACT, MF, 8, 2>(p, s) : go_wave<KD, ACT, MF, 4, 2>(p, s);
@@ -378,7 +378,8 @@ template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, h
 }
 template <int KD, int ACT> hipError_t launch(const DecodeArgs& p, hipStream_t s) {
   // One row straight from memory, with 16 wavefronts where few workgroups have much to read
-  // (1 x 4096 x 14336 8.6 us, 8 wavefronts 10.0, through LDS 9.0; 1 x 20480 x 3584 12.2, 9.7, 9.8).
+  // (w4g128, 16 wavefronts, 8, through LDS: 1 x 4096 x 14336 8.6 us, 9.9, 8.4; 1 x 20480 x 3584
+  // 11.8, 9.9, 9.3; 1 x 16384 x 1024 5.4, 3.9, 4.3; w8a8 1 x 2048 x 14336 6.4, 7.5, 7.5).
   if (p.m == 1) return p.n <= 4096 && p.k >= 4096 ? go_one<KD, ACT, 16>(p, s) : go_one<KD, ACT, 8>(p, s);
   if (p.m <= 16) return launch_rows<KD, ACT, 1>(p, s);
   if (p.m <= 32) return launch_rows<KD, ACT, 2>(p, s);

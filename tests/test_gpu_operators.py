@@ -341,7 +341,7 @@ def check_balance(l, ids, mask, alpha, got):
 
 BALANCE = [(1, 1, 1), (1, 8, 2), (2, 2, 2), (3, 5, 5), (17, 8, 2), (64, 60, 4), (100, 64, 6), (257, 33, 1), (300, 128, 8),
            (511, 160, 6), (1000, 3, 2), (1025, 256, 8), (2048, 60, 4), (33, 1024, 8), (700, 1000, 3), (4099, 64, 8),
-           (20000, 8, 2)]
+           (20000, 8, 2), (4200, 128, 3), (9000, 120, 2), (1100, 200, 2)]
 
 
 @pytest.mark.parametrize("masked", [0.0, 0.3])
