@@ -441,12 +441,13 @@ static int token_lanes(int E) {
 // more than they do: 64 tokens of 60 experts 5.0 us, 6.6 in two launches; 256 7.3 and 7.5; 512
 // of 64 11.1 and 8.2).  Otherwise a token to a lane of a summing workgroup up to 64 of them (4096 x
 // 60: 64 of them 9.1 us, 32 9.8, 16 11.2; 1000 x 512: 63 of them 11.8, 32 13.3), then two, as the
-// shares cost too (4096 x 128: 128 of them 10.7, 64 10.0; 65536 x 64: 256 19.6, 128 20.4), and 2048
-// logits to a gradient one.
+// shares cost too (4096 x 128: 128 of them 10.7, 64 10.0; 65536 x 64: 256 19.6, 128 20.4), and 1024
+// logits to a gradient one (4096 x 60 8.5 us, with 2048 9.0, 512 8.6; 2000 x 60 8.5, 8.9, 8.5; others
+// within 2%).
 void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad) {
   const int64_t waves = ((int64_t)T * token_lanes(E) + 63) / 64, logits = (int64_t)T * E;
   *n_part = waves <= 64 ? 0 : (int32_t)std::max(std::min<int64_t>(64, (waves + 15) / 16), std::min<int64_t>(256, (waves + 31) / 32));
-  *n_grad = (int32_t)std::min<int64_t>(512, (logits + 2047) / 2048);
+  *n_grad = (int32_t)std::min<int64_t>(512, (logits + 1023) / 1024);
 }
 
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s) {
