@@ -684,3 +684,48 @@ def test_far_offsets():
     M.linear_decode(pl, xt, out=out)
     assert torch.equal(out.contiguous().view(torch.int16), dense.view(torch.int16))
     check_norm(x, None, w, act, 0, (M.add_rms_norm(xt, wt)[0], None, None, None))
+
+
+# ------------------------------------------- every launch form against its oracle
+def decode_want(q, ad, b, act):
+    """What a decode linear gives for decoded rows ad, and how far the stored values
+    may be from it (the models of check_decode)."""
+    wd = O.dequant(q, act)
+    want = ad @ wd.T
+    if q.scheme == W.W8A8:
+        bound = 4 * TL.U32 * np.abs(want)
+    elif q.scheme == W.FP8:
+        bound = TL.fp8_block_bound(ad, wd) + 4 * TL.U32 * np.abs(want)
+    else:
+        bound = TL.acc_bound(np.abs(ad), np.abs(wd))
+    want = want + O.act_values(b, act)
+    return want, TL.slot_bound(want, bound + 2 * TL.U32 * np.abs(want) + 1e-30, act)
+
+
+@pytest.mark.parametrize("scheme", DECODE_SCHEMES, ids=lambda s: s.name)
+@pytest.mark.parametrize("n,k", [(4096, 1408), (4112, 1152), (8208, 1408), (12304, 1152), (16400, 1408), (20480, 1152),
+                                 (24592, 1152)])
+def test_decode_four_fragments(scheme, n, k):
+    """49 to 64 rows: one, two and three blocks of channels to a workgroup, by 4 and by 8
+    wavefronts, the last workgroup not full; past 12288 channels the 16-bit rows lie in
+    LDS that the workgroup shares, a chunk of 4 k blocks at a time (9 and 11 k blocks: the
+    last chunk is not full, and the workgroups start at different ones)."""
+    torch = torch_mod()
+    q = W.quantize_linear(W.draw_weight(n, 1, 0, n, k), scheme)
+    rng = np.random.default_rng(n + k)
+    for act in ("bf16", "fp16"):
+        pl = M.PackedLinear(q, act)
+        b, x = W.f64_to_act(rng.standard_normal((1, n)), act), W.f64_to_act(rng.standard_normal((64, k)), act)
+        xv = O.act_values(x, act)
+        if scheme == W.W4G128:
+            a, sc, ad = M.act_tensor(x, act), None, xv
+        else:
+            codes, s = O.act_quant(xv, 127) if scheme == W.W8A8 else O.fp8_quant(xv)
+            a, sc = torch.from_numpy(codes.view(np.int8).copy()).cuda(), torch.from_numpy(s.copy()).cuda()
+            ad = (codes.astype(np.float64) if scheme == W.W8A8 else O.e4m3_values(codes)) * s.astype(np.float64)[:, None]
+        want, bound = decode_want(q, ad, b, act)
+        for m in (49, 63, 64):
+            got = M.linear_decode(pl, a[:m], scales=None if sc is None else sc[:m], bias=M.act_tensor(b, act)[0])
+            off = np.abs(O.act_values(M.act_numpy(got, act), act) - want[:m]) / bound[:m]
+            assert off.max() <= 1.0, (act, m, float(off.max()))
+            say(f"decode {scheme.name} {act} {m}x{n}x{k}: {off.max():.3f} of the bound")
