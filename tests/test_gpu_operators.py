@@ -729,3 +729,125 @@ def test_decode_four_fragments(scheme, n, k):
             off = np.abs(O.act_values(M.act_numpy(got, act), act) - want[:m]) / bound[:m]
             assert off.max() <= 1.0, (act, m, float(off.max()))
             say(f"decode {scheme.name} {act} {m}x{n}x{k}: {off.max():.3f} of the bound")
+
+
+def balance_want(l, ids, mask, alpha):
+    """The definition in 64 bits, whole arrays at a time: (loss, counts, probabilities,
+    gradient) and how far the kernel's may be from them.
+
+    With d = l - max l of a token, exp errs by the rounding of d (|d| U32 of its value)
+    and 4 U32 (2 units in the last place); the sum s by its terms' errors and at most 22
+    additions; 1 / s and the product by 2 U32 more: p within e = (|d| + sum p |d| + 32)
+    U32 of its value.  The probabilities' sums are held in 64 bits up to four roundings (a
+    wavefront's, a workgroup's, a fold's and the result's): 5 U32, however many the tokens.
+    f - sum f p errs as f (1 rounding), the products and at most 22 additions do."""
+    T, E = l.shape
+    k = ids.shape[1]
+    kept = np.ones(T, bool) if mask is None else np.asarray(mask, bool)
+    n = max(1, int(kept.sum()))
+    x = np.where(kept[:, None], l, -np.inf).astype(np.float64)
+    top = x.max(axis=1, keepdims=True)
+    d = np.where(np.isfinite(x), x - np.where(np.isfinite(top), top, 0.0), -np.inf)
+    p = np.exp(d)
+    p /= np.where(p.sum(axis=1, keepdims=True) > 0, p.sum(axis=1, keepdims=True), 1.0)
+    d = np.where(p > 0, np.abs(d), 0.0)
+    e = d + (p * d).sum(axis=1, keepdims=True) + 32
+    of = ids[kept]
+    c = np.bincount(of[(of >= 0) & (of < E)], minlength=E)
+    f = c / (k * n)
+    P = p.sum(axis=0) / n
+    fp = (p * f).sum(axis=1, keepdims=True)
+    g = alpha * E / n * p * (f - fp)
+    off_P = TL.U32 * ((p * e).sum(axis=0) / n + 5 * P) + 1e-37
+    L = alpha * E * float((f * P).sum())
+    off_L = abs(alpha) * E * float((f * off_P).sum()) + 2 * TL.U32 * abs(L) + 1e-37
+    off_g = TL.U32 * abs(alpha) * E / n * p * ((e + 6) * (f + fp) + (p * f * (e + 24)).sum(axis=1, keepdims=True)) + 1e-37
+    return (L, c, P, g), (off_L, off_P, off_g)
+
+
+def check_balance64(l, ids, mask, alpha, got):
+    loss, counts, probs, grad = [None if t is None else t.cpu().numpy() for t in got]
+    (L, c, P, g), (off_L, off_P, off_g) = balance_want(l, ids, mask, alpha)
+    assert np.array_equal(counts, c)
+    assert np.all(np.abs(probs - P) <= off_P), float((np.abs(probs - P) / off_P).max())
+    assert abs(float(loss) - L) <= off_L
+    if grad is not None:
+        assert np.all(np.abs(grad - g) <= off_g), float((np.abs(grad - g) / off_g).max())
+
+
+# one workgroup, and two or three launches, for every number of lanes and logits to a lane; batches that take
+# a workgroup's loops round again (2000 x 3, 140001 x 64, 300007 x 8), and shares that are folded (30011 x 160)
+BALANCE_FORMS = [(300, 12, 2), (5000, 16, 2), (300, 32, 4), (9000, 24, 3), (60, 300, 2), (40, 512, 8), (900, 512, 8),
+                 (2600, 384, 2), (5000, 1, 1), (2500, 3, 2), (3000, 2, 1), (1500, 5, 5), (60, 128, 4), (50, 200, 4),
+                 (33, 100, 3), (2000, 3, 3), (30011, 160, 6), (140001, 64, 8), (300007, 8, 2)]
+
+
+@pytest.mark.parametrize("masked", [0.0, 0.3])
+@pytest.mark.parametrize("T,E,k", BALANCE_FORMS)
+def test_balance_forms(T, E, k, masked):
+    torch = torch_mod()
+    l, ids, mask = balance_case(T, E, k, T + E, masked)
+    lt, it = torch.from_numpy(l).cuda(), torch.from_numpy(ids).cuda()
+    mt = None if mask is None else torch.from_numpy(mask).cuda()
+    got = M.balance_loss(lt, it, alpha=0.7, token_mask=mt)
+    check_balance64(l, ids, mask, 0.7, got)
+    none = M.balance_loss(lt, it, alpha=0.7, token_mask=mt, want_grad=False)
+    for a, b in zip(none[:3], got[:3]):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("masked", [0.0, 0.3])
+@pytest.mark.parametrize("T,E,k", BALANCE_FORMS)
+def test_balance_counts_every_token_once(T, E, k, masked):
+    """Logits that are 0 for one expert and -inf for the others: probabilities of exactly 0 and
+    1, whose sums are whole numbers, so that a token left out or taken twice shows in any
+    batch; the gradient is 0."""
+    torch = torch_mod()
+    rng = np.random.default_rng(T + E)
+    hot = (rng.random(T) ** 2 * E).astype(np.int64)
+    l = np.full((T, E), -np.inf, np.float32)
+    l[np.arange(T), hot] = 0.0
+    mask = rng.random(T) >= masked if masked else np.ones(T, bool)
+    loss, counts, probs, grad = M.balance_loss(torch.from_numpy(l).cuda(), torch.from_numpy(hot[:, None].astype(np.int32)).cuda(),
+                                               token_mask=torch.from_numpy(mask).cuda() if masked else None)
+    c, n = np.bincount(hot[mask], minlength=E), int(mask.sum())
+    assert np.array_equal(counts.cpu().numpy(), c)
+    probs = probs.cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(probs - c / n) <= 1.001 * TL.U32 * c / n)      # one rounding, that of the result
+    want = E * float(((c / n) ** 2).sum())
+    assert abs(float(loss) - want) <= 1.001 * TL.U32 * want
+    assert not bool(grad.any())
+
+
+@pytest.mark.parametrize("T,E,k", [(48, 8, 2), (700, 60, 4)])
+def test_balance_gradient_in_a_backward_pass(T, E, k):
+    """The gradient enters a backward pass beside another loss of the same logits, as the binding
+    says; the reference differentiates the sum of both in 64 bits on the CPU.  The returned
+    tensors have no graph of their own."""
+    torch = torch_mod()
+    alpha, H = 0.25, 32
+    g = torch.Generator().manual_seed(T)
+    x, r = torch.randn(T, H, generator=g), torch.randn(H, E, generator=g) * 0.3
+    v = torch.randn(T, E, generator=g) * 0.01
+    xg, rg = x.cuda(), r.cuda().requires_grad_()
+    logits = (xg[:, :, None] * rg[None]).sum(1)
+    ids = torch.topk(logits.detach(), k, dim=1).indices.to(torch.int32)
+    loss, counts, probs, grad = M.balance_loss(logits, ids, alpha=alpha)
+    assert not any(t.requires_grad for t in (loss, counts, probs, grad))
+    main = (torch.softmax(logits, 1) * v.cuda()).sum()
+    torch.autograd.backward([main, logits], [None, grad])
+    # in 64 bits, from the same 32-bit logits (their own rounding is not the loss's)
+    l = logits.detach().cpu().double().requires_grad_()
+    p = torch.softmax(l, 1)
+    f = torch.bincount(ids.cpu().reshape(-1).long(), minlength=E).double() / (k * T)
+    ((p * v.double()).sum() + alpha * E * (f * p.mean(0)).sum()).backward()
+    want = (x.double().t() @ l.grad).numpy()
+    # both gradients of the logits are p (u - sum u p) for some u: (|d| + sum p |d| + 32 + 50) U32 of p (|u| + sum |u| p)
+    # covers theirs (at most 50 more roundings where sums go one by one); then T products are added up
+    with torch.no_grad():
+        d = l.amax(1, keepdim=True) - l
+        e = d + (p * d).sum(1, keepdim=True) + 32 + 50 + E
+        u = v.double().abs() + alpha * E / T * f
+        off = TL.U32 * 2 * e * p * (u + (u * p).sum(1, keepdim=True))
+        bound = (x.double().abs().t() @ (off + (T + 2) * TL.U32 * l.grad.abs())).numpy()
+    assert np.all(np.abs(rg.grad.cpu().numpy() - want) <= bound)
