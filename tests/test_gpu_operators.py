@@ -851,3 +851,48 @@ def test_balance_gradient_in_a_backward_pass(T, E, k):
         off = TL.U32 * 2 * e * p * (u + (u * p).sum(1, keepdim=True))
         bound = (x.double().abs().t() @ (off + (T + 2) * TL.U32 * l.grad.abs())).numpy()
     assert np.all(np.abs(rg.grad.cpu().numpy() - want) <= bound)
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp16"])
+@pytest.mark.parametrize("cols", [200, 5000, 33000, 40003])
+def test_norm_every_place(cols, act):
+    """Every output in the place of every input that may give it up, rows held in registers
+    and rows that are read again (past 32768 elements), with and without codes; what lies
+    beside the rows stays as it was."""
+    torch = torch_mod()
+    lib = M.load_library()
+    rng = np.random.default_rng(cols)
+    rows, pad, off = 3, 21, 5
+    ld = cols + pad
+    x, res, w = norm_rows(rng, rows, cols, act), norm_rows(rng, rows, cols, act), norm_rows(rng, 1, cols, act)
+    wt = M.act_tensor(w, act)[0]
+    # (residual given, where z goes, where y goes): "x", "r" the inputs' places, "n" new rows, "" nowhere
+    for has_res, zp, yp in ((True, "r", "x"), (True, "x", "r"), (True, "x", "n"), (True, "r", ""), (True, "x", ""),
+                            (True, "", "x"), (True, "", "r"), (True, "n", "x"), (True, "n", "r"), (False, "", "x")):
+        for qmax in (0, 127, 448):
+            if not yp and not qmax:
+                continue
+            at = {"": (None, None), "n": strided(torch, x, act, pad, off), "x": strided(torch, x, act, pad, off),
+                  "r": strided(torch, res, act, pad, off)}
+            codes = torch.full((rows, cols), 99, dtype=torch.int8, device="cuda") if qmax else None
+            scales = torch.full((rows,), 99.0, device="cuda") if qmax else None
+            p = {k: None if v[0] is None else v[0].data_ptr() for k, v in at.items()}
+            st = lib.mxmoe_add_rms_norm(p["x"], ld, p["r"] if has_res else None, ld, wt.data_ptr(), M.act_code(act), rows, cols,
+                                        1e-6, p[zp], ld, p[yp], ld, qmax, M._ptr(codes), M._ptr(scales), M._stream_ptr())
+            assert st == M.OK
+            y, z, _ = O.add_rms_norm(O.act_values(x, act), O.act_values(res, act) if has_res else None, O.act_values(w, act)[0],
+                                     act, 1e-6)
+            if zp:
+                assert np.array_equal(bits(at[zp][0]), act_bits(z, act)), (has_res, zp, yp, qmax)
+            if yp:
+                assert np.array_equal(bits(at[yp][0]), act_bits(y, act)), (has_res, zp, yp, qmax)
+            if qmax:
+                qc, qs = O.act_quant(y, qmax) if qmax == 127 else O.fp8_quant(y)
+                assert np.array_equal(scales.cpu().numpy().view(np.uint32), qs.view(np.uint32))
+                assert np.array_equal(codes.cpu().numpy().view(np.uint8), qc.view(np.uint8))
+            for k in ("x", "r"):                        # an input whose place is not given up is as it was
+                v, wide = at[k]
+                if k not in (zp, yp):
+                    assert np.array_equal(bits(v), bits(M.act_tensor(x if k == "x" else res, act)))
+                v[:] = 77.0
+                assert bool((wide == 77.0).all())
