@@ -289,10 +289,12 @@ MXMOE_API mxmoe_status mxmoe_linear_forward(const mxmoe_linear* L, mxmoe_dtype a
 
 /* One packed linear on the few rows of a decode step, one launch without plan or
  * workspace: out = a W^T + bias, rounded once to `act`.
- *   wNg128 with N = 4: a `act` [m, k], a_scales NULL; per group the exact sum of
- *       a * (q - z) in fp32, times the group's scale, added over the groups; a row
- *       that is not finite throughout has no finite output, and neither may a bf16
- *       row have one whose sum of 143 |a| over a group passes the largest fp32;
+ *   wNg128 with N = 4: a `act` [m, k], a_scales NULL; per group the sum of
+ *       a * (q - z), times the group's scale, added over the groups, in fp32.  fp16
+ *       rows: the exact products a (q - z) are added up; bf16 rows: the difference of
+ *       sum a (16 + q) and (16 + z) sum a, whose roundings are parts of 31 sum |a|.
+ *       A row that is not finite throughout has no finite output, and neither may a
+ *       bf16 row have one whose sum of 31 |a| over a group passes the largest fp32;
  *   w8a8: a int8 [m, k] codes, a_scales fp32 [m] (mxmoe_act_quant with qmax 127
  *       or mxmoe_add_rms_norm): exact int32 sums times a_scales[m] * s_w[n]
  *       (k < 2^17, UNSUPPORTED beyond);

@@ -5,9 +5,13 @@
 // writes; the rows are the A operand (16 rows a fragment), the weights the B
 // operand, so that a lane's four accumulators share one channel:
 //   w4g128  per k block b:  out += s_b (sum_k a q - z_b sum_k a).  bf16: the codes become
-//           128 + q (an OR), and 128 + z is taken off through the row sums, an MFMA of the rows
-//           against ones; fp16: 1024 + q, from which a packed subtraction of
-//           1024 + z leaves q - z.  Both are exact in their dtype.
+//           16 + q (an OR), and 16 + z is taken off through the row sums, an MFMA of the rows
+//           against ones: the difference of two fp32 sums, which err by parts of
+//           sum |a| (16 + q) and not of sum |a (q - z)|.  16 is the least offset that leaves 16
+//           codes one exponent (128, where the codes need no shift of their own, errs five
+//           times as much and overflows sooner; q - z itself takes 6 operations for two
+//           codes, this takes 2).  fp16: 1024 + q, from which a packed subtraction of
+//           1024 + z leaves q - z.  All of them are exact in their dtype.
 //   w8a8    int8 MFMA, int32 sums; fp8  FP8 MFMA, fp32 sums; times s_a s_w at the end.
 //
 // The wavefronts of a workgroup take the k blocks of its channels in turn and meet once,
@@ -88,10 +92,11 @@ DEC_INL void use_block(const Wgt<KD>& s, const Rows<KD, MF>& a, const f32x4 (&rs
       u32x4 b;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t v = (s.w[0][j] >> (4 * i)) & 0x000F000Fu;
-        if constexpr (ACT == MXMOE_BF16) {
-          v |= 0x43004300u;
+        uint32_t v;
+        if constexpr (ACT == MXMOE_BF16) {  // 16 + q = 0x4180 | q << 3
+          v = ((i ? s.w[0][j] >> (4 * i - 3) : s.w[0][j] << 3) & 0x00780078u) | 0x41804180u;
         } else {
+          v = (s.w[0][j] >> (4 * i)) & 0x000F000Fu;
           const _Float16 off = (_Float16)1024.f + z;
           v = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v | 0x64006400u) - f16x2{off, off});
         }
@@ -102,7 +107,7 @@ DEC_INL void use_block(const Wgt<KD>& s, const Rows<KD, MF>& a, const f32x4 (&rs
     }
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
-      if constexpr (ACT == MXMOE_BF16) acc[f] -= (128.f + (float)z) * rs[f];
+      if constexpr (ACT == MXMOE_BF16) acc[f] -= (16.f + (float)z) * rs[f];
       tot[f] += sc * acc[f];
     }
   } else if constexpr (KD == K_W8A8) {

@@ -896,3 +896,24 @@ def test_norm_every_place(cols, act):
                     assert np.array_equal(bits(v), bits(M.act_tensor(x if k == "x" else res, act)))
                 v[:] = 77.0
                 assert bool((wide == 77.0).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 64, 1408), (1, 4096, 4096), (5, 64, 1408), (20, 4112, 384), (40, 64, 640), (64, 8208, 384),
+                                   (64, 12304, 1152)])
+def test_decode_w4_large_rows(m, n, k):
+    """bf16 rows near the end of the range, of one sign and of both: the sums that a group
+    goes through stay below 31 sum |a|, so the outputs are finite and as near as any
+    others'.  (sum |a| of a group is below 2^123 here, 31 times it below 2^128.)"""
+    torch_mod()
+    rng = np.random.default_rng(m + n + k)
+    q = W.quantize_linear(W.draw_weight(n, 1, 0, n, k), W.W4G128)
+    pl = M.PackedLinear(q, "bf16")
+    v = rng.uniform(1.0, 2.0, (m, k)) * 2.0 ** 115
+    v[m // 2:] *= rng.choice([-1.0, 1.0], (m - m // 2, k))
+    if m == 1:
+        v = np.abs(v)
+    a, b = W.f64_to_act(v, "bf16"), W.f64_to_act(rng.standard_normal((1, n)), "bf16")
+    want, bound = decode_want(q, O.act_values(a, "bf16"), b, "bf16")
+    got = O.act_values(M.act_numpy(M.linear_decode(pl, M.act_tensor(a, "bf16"), bias=M.act_tensor(b, "bf16")[0]), "bf16"), "bf16")
+    assert np.isfinite(got).all()
+    assert np.all(np.abs(got - want) <= bound)

@@ -121,6 +121,48 @@ def test_decode_w4_error_model(act, k):
     assert np.all(4 * err <= TL.acc_bound(np.abs(a), np.abs(wd))), float((err / TL.acc_bound(np.abs(a), np.abs(wd))).max())
 
 
+def w4_bf16_emulated(a, q, offset):
+    """The decode linear of w4g128 on bf16 rows in IEEE float32, one term after another: a group's
+    sums of a (offset + q) and of a, (offset + z) times the latter taken off, times the scale, over
+    up to 16 partial sums of every 16th group."""
+    f = np.float32
+    (m, k), n = a.shape, q.n
+    s, z, code = q.scales.astype(f), q.zeros.astype(f), q.codes.astype(f)
+    part = np.zeros((16, m, n), f)
+    for g in range(k // 128):
+        acc, rs = np.zeros((m, n), f), np.zeros((m, 1), f)
+        for c in range(128 * g, 128 * g + 128):
+            acc = acc + a[:, c:c + 1].astype(f) * (code[:, c] + f(offset))[None]
+            rs = rs + a[:, c:c + 1].astype(f)
+        acc = (acc.astype(np.float64) - (f(offset) + z[:, g])[None].astype(np.float64) * rs).astype(f)   # one fma
+        part[g % 16] = (part[g % 16].astype(np.float64) + s[:, g][None].astype(np.float64) * acc).astype(f)
+    tot = part[0]
+    for i in range(1, 16):
+        tot = tot + part[i]
+    return tot
+
+
+@pytest.mark.parametrize("k", [128, 2048, 14336])
+def test_decode_w4_bf16_offset(k):
+    """Codes as 16 + q, as the kernel has them: at least four times inside ACC16_EPS sum |a||w|
+    for weights that use their codes; and, where one weight stretches each group's range and the
+    others sit on the zero point, the error is of sum |a| (16 + q), a third at the most of what
+    an offset of 128 leaves (143 / 31 = 4.6 times as much)."""
+    rng = np.random.default_rng(k)
+    a = O.act_values(W.f64_to_act(np.abs(rng.standard_normal((4, k))), "bf16"), "bf16")   # one sign
+    a[0] *= rng.choice([-1.0, 1.0], k)
+    q = W.quantize_linear(W.draw_weight(7, 0, 0, 16, k), W.W4G128)
+    wd = O.dequant(q, "bf16")
+    err = np.abs(w4_bf16_emulated(a, q, 16) - a @ wd.T)
+    assert np.all(4 * err <= TL.acc_bound(np.abs(a), np.abs(wd)))
+    w = np.zeros((16, k), np.float32)
+    w[:, 5::128] = 1.0
+    q = W.quantize_linear(w, W.W4G128)
+    want = a @ O.dequant(q, "bf16").T
+    rms = [np.sqrt(np.mean((w4_bf16_emulated(a, q, off) - want) ** 2)) for off in (16, 128)]
+    assert rms[0] <= rms[1] / 3, rms
+
+
 # ------------------------------------------------------------------ refusals
 def norm_call(lib, x=at(1), ldx=64, res=at(2), ldr=64, w=at(3), act=M.BF16, rows=4, cols=64, eps=1e-6, sum_=at(4), lds=64,
               y=at(5), ldy=64, qmax=127, codes=at(6), scales=at(7)):
