@@ -16,6 +16,12 @@
 // A token is held by LT lanes, V consecutive logits to a lane and chunk, so that a
 // wavefront reads 64 / LT tokens side by side; sums over a token are butterflies
 // over its lanes.
+//
+// Sums over tokens are 64-bit in a lane and wherever they are added up, so that their error
+// does not grow with the batch.  They are kept as fp32 in between, a wavefront's in LDS, a
+// workgroup's share in the workspace and the folded one: each rounds a sum of positive terms
+// once, within 2^-24 of it, and halves what the last launch reads (summed in fp32 throughout,
+// 2^22 like tokens of 8 experts came out 19 x 2^-24 off).
 #include <algorithm>
 #include "mxmoe_internal.h"
 
@@ -148,7 +154,7 @@ template <int LT, int V, int J> struct Tok {
 // Shared memory of a workgroup of W wavefronts, for at most NE experts
 template <int W, int NE> struct Lds {
   int32_t hist[NE + 1];  // counts; hist[E]: kept tokens
-  float col[W][NE];      // sums of probabilities
+  float col[W][NE];      // sums of probabilities of the wavefronts
   double loss[W];        // of the loss
 };
 
@@ -191,11 +197,12 @@ template <int LT, int V, int J, int U, int W, bool SUM, bool GRAD>
 BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, int64_t parts) {
   constexpr int G = 64 / LT;  // tokens of a wavefront
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, l = lane % LT, g = lane / LT;
-  float f[J][V], sum[J][V], gs = 0.f;
+  float f[J][V], gs = 0.f;
+  double sum[J][V];
 #pragma unroll
   for (int j = 0; j < J; ++j)
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum[j][i] = 0.f;
+    for (int i = 0; i < V; ++i) sum[j][i] = 0.0;
   if constexpr (GRAD) {
     const int n = L.hist[a.E];
     const double per = n > 0 ? 1.0 / n : 0.0;
@@ -236,7 +243,7 @@ BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, i
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-          for (int i = 0; i < V; ++i) sum[j][i] += x[u].v[j][i];
+          for (int i = 0; i < V; ++i) sum[j][i] += (double)x[u].v[j][i];
       }
       if constexpr (GRAD) {
         if (SUM && !a.grad) continue;
@@ -254,10 +261,10 @@ BAL_INL void tokens(Lds<W, LT * V * J>& L, const BalanceArgs& a, int64_t part, i
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        float s = sum[j][i];
+        double s = sum[j][i];
         for (int d = LT; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
         const int e = Tok<LT, V, J>::expert(l, j) + i;
-        if (g == 0 && e < a.E) L.col[w][e] = s;
+        if (g == 0 && e < a.E) L.col[w][e] = (float)s;
       }
     __syncthreads();
   }
@@ -301,10 +308,10 @@ __global__ void __launch_bounds__(1024) balance_sums_kernel(BalanceArgs a) {
   for (int e = threadIdx.x; e <= a.E; e += 64 * W) a.part_counts[(int64_t)blockIdx.x * (a.E + 1) + e] = L.hist[e];
   tokens<LT, V, J, U, W, true, false>(L, a, blockIdx.x, gridDim.x);
   for (int e = threadIdx.x; e < a.E; e += 64 * W) {
-    float s = L.col[0][e];
+    double s = (double)L.col[0][e];
 #pragma unroll
-    for (int i = 1; i < W; ++i) s += L.col[i][e];
-    a.part_probs[(int64_t)blockIdx.x * a.E + e] = s;
+    for (int i = 1; i < W; ++i) s += (double)L.col[i][e];
+    a.part_probs[(int64_t)blockIdx.x * a.E + e] = (float)s;
   }
 }
 

@@ -917,3 +917,16 @@ def test_decode_w4_large_rows(m, n, k):
     got = O.act_values(M.act_numpy(M.linear_decode(pl, M.act_tensor(a, "bf16"), bias=M.act_tensor(b, "bf16")[0]), "bf16"), "bf16")
     assert np.isfinite(got).all()
     assert np.all(np.abs(got - want) <= bound)
+
+
+@pytest.mark.parametrize("T,E", [(1 << 22, 8), (1 << 20, 64), (1 << 17, 512)])
+def test_balance_like_tokens(T, E):
+    """A batch of one token over and over: the mean probabilities are the token's own, at most
+    four roundings apart (a wavefront's sum, a workgroup's, a fold's, the result's; the mean
+    of 2^j tokens is exact), however many tokens a lane adds up."""
+    torch = torch_mod()
+    row = torch.from_numpy(np.random.default_rng(E).standard_normal((1, E)).astype(np.float32)).cuda()
+    one = M.balance_loss(row, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), want_grad=False)[2].double()
+    ids = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    probs = M.balance_loss(row.expand(T, E).contiguous(), ids, want_grad=False)[2].double()
+    assert bool(((probs - one).abs() <= 5 * TL.U32 * one).all()), float(((probs - one).abs() / one).max() / TL.U32)
