@@ -203,8 +203,9 @@ MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
  *             = alpha E / n * p[t,e] (f_e - sum_j f_j p[t,j]), f_e = counts[e] / (k n)
  *               (the counts are constants of the gradient), 0 for other tokens.
  * alpha also takes the factor of a gradient from above.
- *   logits    : fp32 [T, E]; -inf is a probability of 0, a token with nothing but
- *               -inf has probabilities 0 throughout (it counts in n); a NaN or
+ *   logits    : fp32 [T, E]; -inf is a probability of 0 (and a probability below
+ *               the least normal fp32 number may come out as 0), a token with nothing
+ *               but -inf has probabilities 0 throughout (it counts in n); a NaN or
  *               +inf of a kept token makes loss and probs NaN
  *   topk_ids  : int32 [T, k]; ids outside [0, E) are not counted, an id that a
  *               token holds twice counts twice
@@ -212,8 +213,8 @@ MXMOE_API size_t mxmoe_balance_workspace_bytes(int32_t T, int32_t E);
  *               used, whatever they hold), or NULL
  *   counts: int32 [E], probs: fp32 [E], loss: fp32 [1]
  *   grad  : fp32 [T, E], or NULL if not wanted; may be `logits` itself
- * With no kept token everything is 0.  Sums over tokens are formed in a fixed
- * order.  Limits: 1 <= k <= E <= 1024, T >= 0, T*k < 2^31.  4-byte aligned,
+ * With no kept token everything is 0.  Sums over tokens are 64-bit and formed in
+ * a fixed order.  Limits: 1 <= k <= E <= 1024, T >= 0, T*k < 2^31.  4-byte aligned,
  * workspace 256-byte (NULL where mxmoe_balance_workspace_bytes is 0).  Outputs
  * share no bytes with inputs (but grad) or each other.  Errors: INVALID_ARG,
  * WORKSPACE, HIP.                                                            */

@@ -8,7 +8,8 @@
 // The squares of 16-bit values are exact in 64 bits and their sum errs by some
 // 2^-50 of it, so another split of a row over lanes gives another r, by one unit in its
 // last place, for about one row in 2^25 only.  The codes and the scale equal act_quant of
-// the rounded y always.
+// the rounded y for rows that are finite and whose largest |y| is 0 or at least 2^-118;
+// others have scale NaN (act_quant passes over NaN) and 0.
 //
 // A row is read once: its elements stay in registers, 8 to a lane and chunk, and
 // turn from x into z into y in place.  Rows whose pointers or strides are not

@@ -471,7 +471,8 @@ def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_gra
     [E], mean probabilities [E], gradient of the logits [T, E] or None).
 
     logits fp32 [T, E]; topk_ids int32 [T, k]; token_mask bool or uint8 [T], False
-    for padding.  The gradient enters a backward pass as
+    for padding.  The returned tensors have no autograd graph, also where the logits
+    have one: the gradient enters a backward pass as
     ``torch.autograd.backward([out, logits], [None, grad])``; alpha takes its
     factor."""
     torch = _torch()
