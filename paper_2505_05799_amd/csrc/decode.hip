@@ -382,10 +382,18 @@ template <int KD, int ACT, int MF> hipError_t launch_rows(const DecodeArgs& p, h
   return go_wave<KD, ACT, MF, 4, 3>(p, s);
 }
 template <int KD, int ACT> hipError_t launch(const DecodeArgs& p, hipStream_t s) {
-  // One row straight from memory, with 16 wavefronts where few workgroups have much to read
-  // (w4g128, 16 wavefronts, 8, through LDS: 1 x 4096 x 14336 8.6 us, 9.9, 8.4; 1 x 20480 x 3584
-  // 11.8, 9.9, 9.3; 1 x 16384 x 1024 5.4, 3.9, 4.3; w8a8 1 x 2048 x 14336 6.4, 7.5, 7.5).
-  if (p.m == 1) return p.n <= 4096 && p.k >= 4096 ? go_one<KD, ACT, 16>(p, s) : go_one<KD, ACT, 8>(p, s);
+  // One row straight from memory, with 16 wavefronts where few workgroups have much to read.
+  // w4g128 that is wide and deep goes through LDS with two or three channel blocks to a
+  // workgroup: a row's pieces and their sums serve all of them.  us with weights from the
+  // caches / from memory, with 8 wavefronts, with 16, through LDS:
+  //   bf16 w4g128  4096 x 4096 4.0 / 5.8, 4.0 / 5.0, 4.0 / 5.2;  4096 x 14336 10.0 / 14.2, 8.7 / 12.8,
+  //     8.5 / 12.9;  16384 x 1024 3.8 / 5.2, 5.1 / 6.9, 4.0 / 4.8;  20480 x 256 3.2 / 4.0, 4.6 / 6.6, 3.4 / 4.1;
+  //     14336 x 4096 9.3 / 12.3, 10.8 / 13.6, 8.4 / 11.0;  8192 x 14336 15.6 / 21.6, -, 13.2 / 16.5
+  //   fp16 w4g128  20480 x 2048 5.9 / 8.7, -, 7.1 / 8.6;  20480 x 3584 9.5 / 13.8, -, 10.8 / 12.4;  24576 x 4096
+  //     12.1 / 17.6, -, 12.2 / 14.1;  8192 x 14336 14.6 / 21.1, -, 13.2 / 16.5
+  //   w8a8         2048 x 14336 6.1 / 12.0, 5.7 / 10.2, 6.0 / 11.5;  20480 x 3584 12.1 / 15.3, 12.4 / 15.7, 12.9 / 16.6
+  if (p.m == 1 && !(KD == K_W4G && p.n >= 8192 && p.k >= 4096))
+    return p.n <= 4096 && p.k >= 4096 ? go_one<KD, ACT, 16>(p, s) : go_one<KD, ACT, 8>(p, s);
   if (p.m <= 16) return launch_rows<KD, ACT, 1>(p, s);
   if (p.m <= 32) return launch_rows<KD, ACT, 2>(p, s);
   if (p.m <= 48) return launch_rows<KD, ACT, 3>(p, s);

@@ -930,3 +930,22 @@ def test_balance_like_tokens(T, E):
     ids = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
     probs = M.balance_loss(row.expand(T, E).contiguous(), ids, want_grad=False)[2].double()
     assert bool(((probs - one).abs() <= 5 * TL.U32 * one).all()), float(((probs - one).abs() / one).max() / TL.U32)
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp16"])
+@pytest.mark.parametrize("n,k", [(8176, 4096), (8192, 3968), (8192, 4096), (12304, 4224), (16400, 4096), (20480, 3584)])
+def test_decode_one_wide_row(n, k, act):
+    """One row of w4g128 on both sides of 8192 channels and 4096 k, where the launch form changes,
+    contiguous, at an odd place (the binding copies it) and with what follows it in its buffer
+    left alone and unread (NaN)."""
+    torch = torch_mod()
+    q, pl, a, _, bt, ad, b = decode_case(W.W4G128, act, 1, n, k, n + k, True)
+    ref = M.linear_decode(pl, a, bias=bt)
+    check_decode(q, ad, b, act, ref)
+    for off in (8, 3):
+        wide = torch.full((2 * k + 64,), float("nan"), dtype=a.dtype, device="cuda")
+        wide[off:off + k] = a[0]
+        out = torch.full((n + 40,), 9.0, dtype=a.dtype, device="cuda")
+        M.linear_decode(pl, wide[off:off + k][None], bias=bt, out=out[20:20 + n][None])
+        assert torch.equal(out[20:20 + n].view(torch.int16), ref[0].view(torch.int16))
+        assert bool((out[:20] == 9.0).all()) and bool((out[20 + n:] == 9.0).all())
