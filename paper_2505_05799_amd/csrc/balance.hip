@@ -454,7 +454,7 @@ static int token_lanes(int E) {
 // 60: 64 of them 9.1 us, 32 9.8, 16 11.2; 1000 x 512: 63 of them 11.8, 32 13.3), then two, as the
 // shares cost too (4096 x 128: 128 of them 10.7, 64 10.0; 65536 x 64: 256 19.6, 128 20.4), and 1024
 // logits to a gradient one (4096 x 60 8.5 us, with 2048 9.0, 512 8.6; 2000 x 60 8.5, 8.9, 8.5; others
-// within 2%).
+// within 2%).  All of them with fp32 sums over tokens; 64-bit ones add 0 to 3% to each.
 void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad) {
   const int64_t waves = ((int64_t)T * token_lanes(E) + 63) / 64, logits = (int64_t)T * E;
   *n_part = waves <= 64 ? 0 : (int32_t)std::max(std::min<int64_t>(64, (waves + 15) / 16), std::min<int64_t>(256, (waves + 31) / 32));

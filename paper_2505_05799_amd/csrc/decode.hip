@@ -152,7 +152,8 @@ DEC_INL void wave_order() {
 
 // ---- One row, straight from memory.  NW wavefronts share 16 channels; a wavefront's
 // next k block is asked for before this one is used.  4096 x 4096 w4g128 3.9 us a launch in
-// a graph (one wavefront for all k blocks: 10.7); 20480 x 3584 9.9 us, 3.9 TB/s.
+// a graph (one wavefront for all k blocks: 10.7); 20480 x 3584 9.9 us, 3.9 TB/s
+// (14.4 us with weights that no cache holds).
 template <int KD, int ACT, int NW>
 __global__ void __launch_bounds__(64 * NW) decode_one_kernel(DecodeArgs p) {
   __shared__ Acc<KD> red[NW * 64];
