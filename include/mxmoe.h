@@ -311,6 +311,107 @@ MXMOE_API mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype ac
                                  int32_t m, const void* a, int64_t lda, const float* a_scales,
                                  const void* bias, void* out, int64_t ldo, hipStream_t stream);
 
+/* ------------------------------------------- attention of a decode step */
+
+/* A paged cache of keys and values.  A page holds page_size tokens of every kv head;
+ * token slots are numbered page * page_size + place in the page.  The order inside a page
+ * is the matrix cores' (opaque; mxmoe_kv_append writes it, mxmoe_kv_read reads it);
+ * a page's bytes are contiguous in each buffer, so pages may be copied whole.
+ *   k, v    : [n_pages][heads][page_size * dim], `act` values (qmax 0) or one byte an
+ *             element: int8 codes (qmax 127) or FP8 e4m3 (qmax 448); 16-byte aligned
+ *   k_scales, v_scales: fp32 [n_pages][heads][page_size] (NULL for qmax 0), 16-byte aligned
+ * Limits: dim 64, 128 or 256; page_size a power of two, 32 .. 1024 (UNSUPPORTED
+ * otherwise); 1 <= heads <= 1024; n_pages * page_size < 2^31.                */
+typedef struct {
+  int32_t n_pages, heads, dim, page_size;
+  mxmoe_dtype act;
+  int32_t qmax;
+  void *k, *v;
+  float *k_scales, *v_scales;
+} mxmoe_kv_cache;
+
+/* Bytes of k (and of v), and of k_scales (and v_scales; 0 for qmax 0); 0 if the cache is
+ * outside the limits.  The pointers are not looked at.                       */
+MXMOE_API size_t mxmoe_kv_cache_bytes(const mxmoe_kv_cache* cache);
+MXMOE_API size_t mxmoe_kv_scale_bytes(const mxmoe_kv_cache* cache);
+
+/* Heads of new tokens, one launch: queries and keys are normalized per head and rotated,
+ * keys and values written into the cache.  Per row of a head, in fp32:
+ *   y = x * r * weight, r = fl32(1 / sqrt(mean x^2 + eps)), mean and root in 64 bits
+ *       (without weight: y = x)
+ *   pairs (a, b) of the first `rot` elements become (a cos - b sin, b cos + a sin) of the
+ *       angle positions[t] * freqs[i], formed in 64 bits; pair i is (i, i + rot/2), or
+ *       (2 i, 2 i + 1) with interleaved 1
+ *   q_out: y rounded to `act`.  The cache: y (values: x) rounded to `act`, or codes and scale of
+ *       y with the recipe of mxmoe_act_quant (of the fp32 values: nothing is
+ *       rounded in between).  A row that is not finite throughout gets scale NaN and codes
+ *       0, one whose largest magnitude is below 2^-118 counts as zero.
+ *   q, q_out : `act` [n_tokens, q_heads, dim], heads side by side, tokens ldq / ldo elements
+ *              apart; q_out may be q itself (same stride).  NULL with q_heads 0
+ *   k, v     : `act` [n_tokens, heads, dim], tokens ldk / ldv apart
+ *   q_weight, k_weight: `act` [dim] or NULL (no norm)
+ *   positions: int32 [n_tokens], freqs: double [rot / 2]; NULL with rot 0
+ *   slots    : int32 [n_tokens]; a token whose slot is outside the cache is not kept (its
+ *              q_out is written).  A slot given twice in a call holds either token's
+ *              bytes or some of both: what is read from it is undefined, other slots are not
+ *              affected.
+ * `act` is the cache's.  rot: a multiple of 16 up to dim (UNSUPPORTED otherwise).
+ * 2-byte aligned rows, 4-byte positions and slots, 8-byte freqs.  Outputs share no
+ * byte with inputs (but q_out with q) or each other.  1e-30 <= eps <= 1e30 where there is a
+ * weight; q_heads <= 65536.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                     */
+MXMOE_API mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_tokens, const void* q, int64_t ldq,
+                             int32_t q_heads, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                             const void* q_weight, const void* k_weight, double eps,
+                             const int32_t* positions, const double* freqs, int32_t rot,
+                             int32_t interleaved, const int32_t* slots, void* q_out, int64_t ldo,
+                             hipStream_t stream);
+
+/* Rows of the cache back: k_out, v_out `act` [n_tokens, heads, dim] dense, code * scale
+ * rounded once (16-bit rows as they are); slots int32 [n_tokens], zeros for a slot outside the
+ * cache.  Outputs 2-byte aligned; they share no byte with the cache, slots or each
+ * other.  Errors: INVALID_ARG, UNSUPPORTED, HIP.                             */
+MXMOE_API mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const int32_t* slots,
+                           void* k_out, void* v_out, hipStream_t stream);
+
+/* Most query tokens of a sequence in mxmoe_attention_decode.                */
+#define MXMOE_ATTENTION_QUERIES 16
+
+/* Bytes of workspace for mxmoe_attention_decode with these sizes (0: none needed, or
+ * sizes outside the limits).                                                 */
+MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, int32_t batch, int32_t n_q,
+                                       int32_t q_heads, int32_t width, int32_t prefix_len);
+
+/* out = softmax(x) v of each query over the tokens that it sees, x = scale * (q . k), or
+ * softcap * tanh(scale * (q . k) / softcap) with softcap > 0.
+ *   q, out : `act` [batch * n_q, q_heads, dim], sequence by sequence, heads side by side, tokens
+ *            ldq / ldo elements apart; query head h reads kv head h / (q_heads / heads)
+ *   lengths: int32 [batch]: tokens of a sequence, its queries' own (the last n_q) among
+ *            them: query j sees the first lengths[b] - n_q + 1 + j.  A query that sees none
+ *            (padding: length 0, or shorter than n_q) gets zeros.
+ *   table  : int32 [batch, width]: pages of the positions from prefix_len on, page_size to a
+ *            page.  Entries past a sequence's length are not read.
+ *   prefix : int32 [ceil(prefix_len / page_size)]: pages of the first prefix_len positions, the
+ *            same for every sequence and read once for all; NULL with prefix_len 0.  The
+ *            result is that of a table in which they come first.
+ * A page id outside the cache makes the queries that see one of its tokens NaN, a
+ * length past prefix_len + width * page_size those of its sequence.  What lies in
+ * the cache past a query's last token does not reach it, whatever it is.  A query with
+ * NaN or inf, and a seen key or value row that is not finite, may make the outputs that depend
+ * on it NaN or inf.  Scores, weights and sums are fp32; weights are rounded to fp16 (bf16 with
+ * a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
+ * value's scale is in them (scales below 2^-80 count for less).
+ * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
+ * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^26
+ * (UNSUPPORTED beyond).  scale finite, 0 <= softcap finite.  q and out 2-byte
+ * aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
+ * each other or the inputs.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.  */
+MXMOE_API mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, int64_t ldq, int32_t batch,
+                                    int32_t n_q, int32_t q_heads, const int32_t* table, int32_t width,
+                                    const int32_t* lengths, const int32_t* prefix, int32_t prefix_len,
+                                    float scale, float softcap, void* out, int64_t ldo,
+                                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* ---------------------------------------------------------- MoE block */
 
 typedef struct {

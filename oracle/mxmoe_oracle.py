@@ -345,6 +345,68 @@ def add_rms_norm(x: np.ndarray, residual: Optional[np.ndarray], weight: np.ndarr
 
 
 # ----------------------------------------------------------------------------
+# Attention of a decode step: heads into a cache, attention over what is cached
+# ----------------------------------------------------------------------------
+
+
+def head_rows(x: np.ndarray, weight: Optional[np.ndarray], eps: float, positions: Optional[np.ndarray],
+              freqs: Optional[np.ndarray], interleaved: bool = False) -> np.ndarray:
+    """Heads' rows [tokens, heads, dim] (fp64 values) normalized and rotated, in fp64, nothing
+    rounded: x weight / sqrt(mean x^2 + eps), then the pairs (i, i + rot/2) or (2 i, 2 i + 1)
+    of the first rot = 2 len(freqs) elements as complex numbers times e^(i position freq)."""
+    y = np.array(x, dtype=np.float64)
+    if weight is not None:
+        y = y / np.sqrt((y * y).mean(axis=-1, keepdims=True) + eps) * weight
+    if freqs is None or len(freqs) == 0:
+        return y
+    half = len(freqs)
+    turn = np.exp(1j * np.outer(positions.astype(np.float64), freqs))[:, None, :]
+    a, b = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    z = (y[..., a] + 1j * y[..., b]) * turn
+    y[..., a], y[..., b] = z.real, z.imag
+    return y
+
+
+def cache_rows(y: np.ndarray, qmax: int) -> Tuple[np.ndarray, Optional[np.ndarray]]:
+    """(codes, scales) of fp64 rows [..., dim] that fp32 holds: the per-token recipe of the
+    activations (qmax 127: int8, 448: e4m3 bytes); the rows themselves with qmax 0."""
+    if qmax == 0:
+        return y, None
+    flat = y.reshape(-1, y.shape[-1])
+    codes, scales = act_quant(flat, qmax) if qmax == 127 else fp8_quant(flat)
+    return codes.reshape(y.shape), scales.reshape(y.shape[:-1])
+
+
+def cache_values(codes: np.ndarray, scales: Optional[np.ndarray], qmax: int) -> np.ndarray:
+    """What the codes stand for, in fp64 (exact products)."""
+    if qmax == 0:
+        return codes
+    v = e4m3_values(codes.view(np.uint8)) if qmax == 448 else codes.astype(np.float64)
+    return v * scales.astype(np.float64)[..., None]
+
+
+def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, seen: Sequence[int], scale: float, softcap: float = 0.0):
+    """(out, mass) for one sequence in fp64: q [n_q, q_heads, dim] over k, v [tokens, heads,
+    dim]; query j sees the first seen[j] tokens, one that sees none is zero.  mass: the sum of
+    weight |v| of each output, what its error bound is a part of."""
+    n_q, hq, dim = q.shape
+    group = hq // k.shape[1]
+    out, mass = np.zeros((n_q, hq, dim)), np.zeros((n_q, hq, dim))
+    for j in range(n_q):
+        n = min(max(int(seen[j]), 0), k.shape[0])
+        if n == 0:
+            continue
+        for h in range(hq):
+            x = k[:n, h // group] @ q[j, h] * scale
+            if softcap > 0:
+                x = softcap * np.tanh(x / softcap)
+            p = np.exp(x - x.max())
+            p /= p.sum()
+            out[j, h], mass[j, h] = p @ v[:n, h // group], p @ np.abs(v[:n, h // group])
+    return out, mass
+
+
+# ----------------------------------------------------------------------------
 # Balance loss of the router
 # ----------------------------------------------------------------------------
 

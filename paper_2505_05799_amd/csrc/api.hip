@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 
 #include "mxmoe_internal.h"
@@ -666,6 +667,215 @@ mxmoe_status mxmoe_linear_decode(const mxmoe_linear* L, mxmoe_dtype act, const v
   p.k = L->k;
   p.act = act;
   return hip_status(launch_linear_decode(p, kd, stream));
+}
+
+// ------------------------------------- attention of a decode step
+namespace {
+mxmoe_status check_cache(const mxmoe_kv_cache* c, bool buffers) {
+  if (!c || !valid_dtype(c->act) || c->n_pages <= 0 || c->heads <= 0) return MXMOE_ERR_INVALID_ARG;
+  if (c->qmax != 0 && c->qmax != 127 && c->qmax != kQmaxF8) return MXMOE_ERR_UNSUPPORTED;
+  if (c->dim != 64 && c->dim != 128 && c->dim != 256) return MXMOE_ERR_UNSUPPORTED;
+  if (c->page_size < 32 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return MXMOE_ERR_UNSUPPORTED;
+  if (c->heads > 1024 || (int64_t)c->n_pages * c->page_size >= (1LL << 31)) return MXMOE_ERR_UNSUPPORTED;
+  if (!buffers) return MXMOE_OK;
+  if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return MXMOE_ERR_INVALID_ARG;
+  if ((c->qmax != 0) != (c->k_scales != nullptr) || (c->qmax != 0) != (c->v_scales != nullptr)) return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(c->k_scales, 16) || !aligned(c->v_scales, 16)) return MXMOE_ERR_INVALID_ARG;
+  return MXMOE_OK;
+}
+int64_t cache_bytes(const mxmoe_kv_cache& c) { return (int64_t)c.n_pages * c.heads * c.page_size * c.dim * (c.qmax ? 1 : 2); }
+int64_t scale_bytes(const mxmoe_kv_cache& c) { return c.qmax ? (int64_t)c.n_pages * c.heads * c.page_size * 4 : 0; }
+Rows whole(const void* p, int64_t bytes) { return Rows{p, bytes, bytes, p && bytes > 0 ? 1 : 0}; }
+int log2_of(int32_t p) {
+  int l = 0;
+  while ((1 << l) < p) ++l;
+  return l;
+}
+// Whether an output shares a byte with an input or another output.
+bool any_overlap(std::initializer_list<Rows> in, std::initializer_list<Rows> out) {
+  for (const Rows* o = out.begin(); o != out.end(); ++o) {
+    for (const Rows& i : in)
+      if (overlap(*o, i)) return true;
+    for (const Rows* i = out.begin(); i != o; ++i)
+      if (overlap(*o, *i)) return true;
+  }
+  return false;
+}
+}  // namespace
+
+size_t mxmoe_kv_cache_bytes(const mxmoe_kv_cache* cache) {
+  return check_cache(cache, false) == MXMOE_OK ? (size_t)cache_bytes(*cache) : 0;
+}
+
+size_t mxmoe_kv_scale_bytes(const mxmoe_kv_cache* cache) {
+  return check_cache(cache, false) == MXMOE_OK ? (size_t)scale_bytes(*cache) : 0;
+}
+
+mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_tokens, const void* q, int64_t ldq, int32_t q_heads,
+                             const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q_weight,
+                             const void* k_weight, double eps, const int32_t* positions, const double* freqs, int32_t rot,
+                             int32_t interleaved, const int32_t* slots, void* q_out, int64_t ldo, hipStream_t stream) {
+  mxmoe_status st = check_cache(cache, true);
+  if (st != MXMOE_OK) return st;
+  const mxmoe_kv_cache& c = *cache;
+  if (n_tokens < 0 || q_heads < 0 || q_heads > 65536 || (interleaved != 0 && interleaved != 1)) return MXMOE_ERR_INVALID_ARG;
+  if (rot < 0 || rot > c.dim || rot % 16) return MXMOE_ERR_UNSUPPORTED;
+  if ((q_weight || k_weight) && (!(eps >= 1e-30) || !(eps <= 1e30))) return MXMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MXMOE_OK;
+  if (!k || !v || !slots || (q_heads > 0) != (q != nullptr) || (q_heads > 0) != (q_out != nullptr) || (q_weight && !q))
+    return MXMOE_ERR_INVALID_ARG;
+  if ((rot > 0) != (positions != nullptr) || (rot > 0) != (freqs != nullptr)) return MXMOE_ERR_INVALID_ARG;
+  const int64_t qc = (int64_t)q_heads * c.dim, kc = (int64_t)c.heads * c.dim, n = n_tokens;
+  if (!row_stride_ok(ldk, kc, 2, n) || !row_stride_ok(ldv, kc, 2, n) ||
+      (q && (!row_stride_ok(ldq, qc, 2, n) || !row_stride_ok(ldo, qc, 2, n))))
+    return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_weight, 2) || !aligned(k_weight, 2) ||
+      !aligned(q_out, 2) || !aligned(positions, 4) || !aligned(slots, 4) || !aligned(freqs, 8))
+    return MXMOE_ERR_INVALID_ARG;
+  const Rows rq{q, 2 * ldq, 2 * qc, n}, ro{q_out, 2 * ldo, 2 * qc, n};
+  const Rows ck = whole(c.k, cache_bytes(c)), cv = whole(c.v, cache_bytes(c)), cks = whole(c.k_scales, scale_bytes(c)),
+             cvs = whole(c.v_scales, scale_bytes(c));
+  if (any_overlap({{k, 2 * ldk, 2 * kc, n}, {v, 2 * ldv, 2 * kc, n}, whole(q_weight, 2 * c.dim), whole(k_weight, 2 * c.dim),
+                   whole(positions, 4 * n), whole(freqs, 4 * (int64_t)rot), whole(slots, 4 * n)},
+                  {ro, ck, cv, cks, cvs}) ||
+      any_overlap({rq}, {ck, cv, cks, cvs}) || (overlap(ro, rq) && !same_rows(ro, rq)))  // q_out may be q itself
+    return MXMOE_ERR_INVALID_ARG;
+  KvAppendArgs a = {};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.q_out = q_out;
+  a.ck = c.k;
+  a.cv = c.v;
+  a.cks = c.k_scales;
+  a.cvs = c.v_scales;
+  a.positions = positions;
+  a.slots = slots;
+  a.freqs = freqs;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.ldo = ldo;
+  a.eps = eps;
+  a.tokens = n_tokens;
+  a.q_heads = q_heads;
+  a.kv_heads = c.heads;
+  a.rot = rot;
+  a.interleaved = interleaved;
+  a.act = c.act;
+  a.qmax = c.qmax;
+  a.page_log2 = log2_of(c.page_size);
+  a.n_slots = c.n_pages * c.page_size;
+  return hip_status(launch_kv_append(a, c.dim, stream));
+}
+
+mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const int32_t* slots, void* k_out, void* v_out,
+                           hipStream_t stream) {
+  mxmoe_status st = check_cache(cache, true);
+  if (st != MXMOE_OK) return st;
+  const mxmoe_kv_cache& c = *cache;
+  if (n_tokens < 0) return MXMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MXMOE_OK;
+  if (!slots || !k_out || !v_out || !aligned(slots, 4) || !aligned(k_out, 2) || !aligned(v_out, 2)) return MXMOE_ERR_INVALID_ARG;
+  const int64_t ob = 2 * (int64_t)n_tokens * c.heads * c.dim;
+  if (any_overlap({whole(c.k, cache_bytes(c)), whole(c.v, cache_bytes(c)), whole(c.k_scales, scale_bytes(c)),
+                   whole(c.v_scales, scale_bytes(c)), whole(slots, 4 * (int64_t)n_tokens)},
+                  {whole(k_out, ob), whole(v_out, ob)}))
+    return MXMOE_ERR_INVALID_ARG;
+  KvReadArgs a = {};
+  a.ck = c.k;
+  a.cv = c.v;
+  a.cks = c.k_scales;
+  a.cvs = c.v_scales;
+  a.slots = slots;
+  a.k = k_out;
+  a.v = v_out;
+  a.tokens = n_tokens;
+  a.kv_heads = c.heads;
+  a.act = c.act;
+  a.qmax = c.qmax;
+  a.page_log2 = log2_of(c.page_size);
+  a.n_slots = c.n_pages * c.page_size;
+  return hip_status(launch_kv_read(a, c.dim, stream));
+}
+
+namespace {
+mxmoe_status check_attention(const mxmoe_kv_cache& c, int32_t batch, int32_t n_q, int32_t q_heads, int32_t width,
+                             int32_t prefix_len) {
+  if (batch < 0 || n_q <= 0 || q_heads <= 0 || q_heads % c.heads || width < 0 || prefix_len < 0) return MXMOE_ERR_INVALID_ARG;
+  if (n_q > MXMOE_ATTENTION_QUERIES || batch > 65535 || q_heads > 65536 || (int64_t)batch * n_q * q_heads >= (1 << 26) ||
+      (int64_t)width * c.page_size + prefix_len > (1 << 30))
+    return MXMOE_ERR_UNSUPPORTED;
+  return MXMOE_OK;
+}
+AttnArgs attention_args(const mxmoe_kv_cache& c, int32_t batch, int32_t n_q, int32_t q_heads, int32_t width, int32_t prefix_len) {
+  AttnArgs a = {};
+  a.batch = batch;
+  a.n_q = n_q;
+  a.q_heads = q_heads;
+  a.kv_heads = c.heads;
+  a.width = width;
+  a.prefix_len = prefix_len;
+  a.n_pages = c.n_pages;
+  a.page_log2 = log2_of(c.page_size);
+  a.act = c.act;
+  a.qmax = c.qmax;
+  return a;
+}
+}  // namespace
+
+size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, int32_t batch, int32_t n_q, int32_t q_heads,
+                                       int32_t width, int32_t prefix_len) {
+  if (check_cache(cache, false) != MXMOE_OK || check_attention(*cache, batch, n_q, q_heads, width, prefix_len) != MXMOE_OK)
+    return 0;
+  return batch == 0 ? 0 : attention_workspace(attention_args(*cache, batch, n_q, q_heads, width, prefix_len), cache->dim);
+}
+
+mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, int64_t ldq, int32_t batch, int32_t n_q,
+                                    int32_t q_heads, const int32_t* table, int32_t width, const int32_t* lengths,
+                                    const int32_t* prefix, int32_t prefix_len, float scale, float softcap, void* out,
+                                    int64_t ldo, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  mxmoe_status st = check_cache(cache, true);
+  if (st != MXMOE_OK) return st;
+  const mxmoe_kv_cache& c = *cache;
+  st = check_attention(c, batch, n_q, q_heads, width, prefix_len);
+  if (st != MXMOE_OK) return st;
+  if (!(scale - scale == 0.f) || !(softcap >= 0.f) || !(softcap - softcap == 0.f)) return MXMOE_ERR_INVALID_ARG;
+  if (batch == 0) return MXMOE_OK;
+  if (!q || !out || !lengths || (width > 0) != (table != nullptr) || (prefix_len > 0) != (prefix != nullptr))
+    return MXMOE_ERR_INVALID_ARG;
+  const int64_t n = (int64_t)batch * n_q, qc = (int64_t)q_heads * c.dim;
+  if (!row_stride_ok(ldq, qc, 2, n) || !row_stride_ok(ldo, qc, 2, n)) return MXMOE_ERR_INVALID_ARG;
+  if (!aligned(q, 2) || !aligned(out, 2) || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(prefix, 4) ||
+      !aligned(workspace, 256))
+    return MXMOE_ERR_INVALID_ARG;
+  AttnArgs a = attention_args(c, batch, n_q, q_heads, width, prefix_len);
+  const size_t ws = attention_workspace(a, c.dim);
+  if (ws > 0 && !workspace) return MXMOE_ERR_INVALID_ARG;
+  if (workspace_bytes < ws) return MXMOE_ERR_WORKSPACE;
+  const int64_t prefix_pages = ((int64_t)prefix_len + c.page_size - 1) / c.page_size;
+  if (any_overlap({{q, 2 * ldq, 2 * qc, n}, whole(c.k, cache_bytes(c)), whole(c.v, cache_bytes(c)),
+                   whole(c.k_scales, scale_bytes(c)), whole(c.v_scales, scale_bytes(c)), whole(table, 4 * (int64_t)batch * width),
+                   whole(lengths, 4 * (int64_t)batch), whole(prefix, 4 * prefix_pages)},
+                  {{out, 2 * ldo, 2 * qc, n}, whole(workspace, (int64_t)ws)}))
+    return MXMOE_ERR_INVALID_ARG;
+  a.q = q;
+  a.out = out;
+  a.ck = reinterpret_cast<const uint8_t*>(c.k);
+  a.cv = reinterpret_cast<const uint8_t*>(c.v);
+  a.cks = c.k_scales;
+  a.cvs = c.v_scales;
+  a.table = table;
+  a.lengths = lengths;
+  a.prefix = prefix;
+  a.part = reinterpret_cast<float*>(workspace);
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.scale = scale;
+  a.softcap = softcap;
+  return hip_status(launch_attention(a, c.dim, stream));
 }
 
 // ------------------------------------------------------- balance loss

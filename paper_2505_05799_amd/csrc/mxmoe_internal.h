@@ -583,4 +583,44 @@ struct BalanceArgs {
 void balance_shares(int32_t T, int32_t E, int32_t* n_part, int32_t* n_grad);
 hipError_t launch_balance_loss(const BalanceArgs& a, hipStream_t s);
 
+// Heads of new tokens into the paged cache and back (kvcache.hip; layout in kvcache.h).
+// Rows of 16-bit values with token strides in elements, heads side by side; q, the weights,
+// positions and freqs (rot 0) may be null.
+struct KvAppendArgs {
+  const void *q, *k, *v, *q_weight, *k_weight;
+  void* q_out;
+  void *ck, *cv;
+  float *cks, *cvs;
+  const int32_t *positions, *slots;
+  const double* freqs;
+  int64_t ldq, ldk, ldv, ldo;
+  double eps;
+  int32_t tokens, q_heads, kv_heads, rot, interleaved, act, qmax, page_log2, n_slots;
+  int32_t heads, tb;  // set by the launch
+};
+hipError_t launch_kv_append(KvAppendArgs a, int dim, hipStream_t s);
+struct KvReadArgs {
+  const void *ck, *cv;
+  const float *cks, *cvs;
+  const int32_t* slots;
+  void *k, *v;
+  int32_t tokens, kv_heads, act, qmax, page_log2, n_slots;
+};
+hipError_t launch_kv_read(const KvReadArgs& a, int dim, hipStream_t s);
+
+// Attention of a few query tokens a sequence over the cache's pages (attention.hip).
+struct AttnArgs {
+  const void* q;
+  void* out;
+  const uint8_t *ck, *cv;
+  const float *cks, *cvs;
+  const int32_t *table, *lengths, *prefix;
+  float* part;      // workspace: partial sums
+  int64_t ldq, ldo;
+  float scale, softcap;
+  int32_t batch, n_q, q_heads, kv_heads, width, prefix_len, n_pages, page_log2, act, qmax;
+};
+size_t attention_workspace(const AttnArgs& a, int dim);
+hipError_t launch_attention(const AttnArgs& a, int dim, hipStream_t s);
+
 }  // namespace mxmoe

@@ -47,6 +47,12 @@ class ForwardOpts_t(C.Structure):
                 ("shared_w", C.c_void_p), ("fp32_slots", C.c_int32), ("reserved1", C.c_int32)]
 
 
+class KVCache_t(C.Structure):
+    _fields_ = [("n_pages", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("page_size", C.c_int32),
+                ("act", C.c_int), ("qmax", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p),
+                ("v_scales", C.c_void_p)]
+
+
 WS_FIELDS = ["status", "counts", "offsets", "sorted_pair", "inv", "plan", "xq8", "xs8", "xq4", "xs4",
              "h", "h_shared", "hq", "hs", "hq_shared", "hs_shared", "slots", "total", "plan_queue_cap",
              "plan_flat_cap", "partial", "partial_floats", "rsx", "rsh", "rsh_shared", "xq4g", "xs4g", "hsg",
@@ -65,10 +71,13 @@ EXPORTS = [
     "mxmoe_moe_forward_ex", "mxmoe_workspace_layout", "mxmoe_status_string", "mxmoe_version",
     "mxmoe_moe_forward_noalloc", "mxmoe_set_tile_costs", "mxmoe_get_tile_costs",
     "mxmoe_add_rms_norm", "mxmoe_linear_decode", "mxmoe_balance_workspace_bytes", "mxmoe_balance_loss",
+    "mxmoe_kv_cache_bytes", "mxmoe_kv_scale_bytes", "mxmoe_kv_append", "mxmoe_kv_read",
+    "mxmoe_attention_workspace_bytes", "mxmoe_attention_decode",
 ]
 TILE_COST_SHAPE = (2, 11, 4, 4)     # [phase][scheme][configuration][a, bs, bu, h], MXMOE_TILE_COST_ENTRIES
 NOALLOC_SCRATCH_BYTES = 128 << 20   # MXMOE_NOALLOC_SCRATCH_BYTES
 DECODE_ROWS = 64                    # MXMOE_DECODE_ROWS
+ATTENTION_QUERIES = 16              # MXMOE_ATTENTION_QUERIES
 
 _lib = None
 
@@ -82,7 +91,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         raise RuntimeError(f"{path} is missing: build it with `python -m paper_2505_05799_amd.build`")
     lib = C.CDLL(path)
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
-    PL, PB = C.POINTER(Linear_t), C.POINTER(Block_t)
+    PL, PB, PK = C.POINTER(Linear_t), C.POINTER(Block_t), C.POINTER(KVCache_t)
     sig = {
         "mxmoe_packed_bytes": (sz, [PL, C.c_int]),
         "mxmoe_pack_weights": (C.c_int, [PL, C.c_int, C.c_int, vp, vp, vp, vp, sz, vp]),
@@ -110,6 +119,14 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "mxmoe_linear_decode": (C.c_int, [PL, C.c_int, vp, i32, vp, i64, vp, vp, vp, i64, vp]),
         "mxmoe_balance_workspace_bytes": (sz, [i32, i32]),
         "mxmoe_balance_loss": (C.c_int, [vp, vp, vp, i32, i32, i32, C.c_float, vp, vp, vp, vp, vp, sz, vp]),
+        "mxmoe_kv_cache_bytes": (sz, [PK]),
+        "mxmoe_kv_scale_bytes": (sz, [PK]),
+        "mxmoe_kv_append": (C.c_int, [PK, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp, C.c_double, vp, vp, i32, i32, vp, vp, i64,
+                                      vp]),
+        "mxmoe_kv_read": (C.c_int, [PK, i32, vp, vp, vp, vp]),
+        "mxmoe_attention_workspace_bytes": (sz, [PK, i32, i32, i32, i32, i32]),
+        "mxmoe_attention_decode": (C.c_int, [PK, vp, i64, i32, i32, i32, vp, i32, vp, vp, i32, C.c_float, C.c_float, vp, i64, vp,
+                                             sz, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -502,6 +519,182 @@ def balance_loss(logits, topk_ids, alpha: float = 1.0, token_mask=None, want_gra
         return loss, counts, probs, grad
 
     return _run_on(dev, stream, body, (logits, topk_ids, token_mask))
+
+
+# ------------------------------------------- attention of a decode step
+class KVCache:
+    """A paged cache of keys and values on one GPU (mxmoe_kv_cache): n_pages pages of
+    page_size tokens, `heads` kv heads of `dim` elements.  qmax 0 keeps 16-bit rows of the
+    activation dtype, 127 int8 codes and 448 FP8 e4m3 with an fp32 scale per token
+    and head.  k, v [n_pages, heads, page_size * dim] and k_scales, v_scales [n_pages, heads,
+    page_size] start as zeros; rows are in an order of their own inside a page
+    (kv_append writes them, kv_read reads them), pages may be copied whole."""
+
+    def __init__(self, n_pages: int, heads: int, dim: int, page_size: int = 64, act: str = "bf16", qmax: int = 0,
+                 device="cuda"):
+        torch = _torch()
+        lib = load_library()
+        self.n_pages, self.heads, self.dim, self.page_size, self.act, self.qmax = n_pages, heads, dim, page_size, act, qmax
+        self.dtype = {"bf16": torch.bfloat16, "fp16": torch.float16}[act]
+        self.t = KVCache_t(n_pages, heads, dim, page_size, act_code(act), qmax)
+        if lib.mxmoe_kv_cache_bytes(C.byref(self.t)) == 0:
+            raise MxmoeError(ERR_UNSUPPORTED, f"kv_cache({n_pages} pages of {page_size}, {heads} heads of {dim}, qmax {qmax})")
+        rows = torch.int8 if qmax else self.dtype
+        self.k, self.v = (torch.zeros(n_pages, heads, page_size * dim, dtype=rows, device=device) for _ in range(2))
+        self.k_scales = self.v_scales = None
+        if qmax:
+            self.k_scales, self.v_scales = (torch.zeros(n_pages, heads, page_size, dtype=torch.float32, device=device)
+                                            for _ in range(2))
+        self.t.k, self.t.v = self.k.data_ptr(), self.v.data_ptr()
+        if qmax:
+            self.t.k_scales, self.t.v_scales = self.k_scales.data_ptr(), self.v_scales.data_ptr()
+        self._dev = self.k.get_device()
+        if self._dev < 0:
+            raise ValueError(f"device {device}: a cache on a GPU is expected")
+
+    def buffers(self):
+        return self.k, self.v, self.k_scales, self.v_scales
+
+
+def _heads(t, name, dtype, rows, heads, dim, dev):
+    """Raise ValueError unless t is [rows, heads, dim] of the dtype on GPU `dev`, a
+    token's heads side by side; returns its address and the tokens' stride."""
+    if t.dtype is not dtype or tuple(t.shape) != (rows, heads, dim) or t.get_device() != dev:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {(rows, heads, dim)} on GPU {dev}")
+    ld, hs, one = t.stride()
+    if rows and (one != 1 or (hs != dim and heads > 1) or (ld < heads * dim and rows > 1)):
+        raise ValueError(f"{name}: strides {t.stride()}; a token's heads side by side, tokens apart from each other, are expected")
+    return t.data_ptr(), (ld if rows > 1 else heads * dim)
+
+
+def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None, eps: float = 1e-6, positions=None,
+              freqs=None, interleaved: bool = False, q_out=None, stream=None):
+    """Keys and values of new tokens into the cache, normalized per head and rotated on
+    the way, and the queries the same way (mxmoe_kv_append): returns the queries, a
+    new tensor or q_out (which may be q itself), or None without q.
+
+    k, v [tokens, heads, dim], q [tokens, q_heads, dim] in the cache's dtype, tokens of any
+    stride (views of a joint projection); slots int32 [tokens], page * page_size + place
+    (outside the cache: not kept); q_weight, k_weight [dim] or None for no norm;
+    positions int32 [tokens] and freqs float64 [rot / 2], radians a position, or None for no
+    rotation.  A slot must not come twice in a call."""
+    torch = _torch()
+    lib = _lib or load_library()
+    dev, dt, kv, dim = cache._dev, cache.dtype, cache.heads, cache.dim
+    if k.dim() != 3:
+        raise ValueError(f"k: shape {tuple(k.shape)}, expected [tokens, heads, dim]")
+    n = k.shape[0]
+    kp, ldk = _heads(k, "k", dt, n, kv, dim, dev)
+    vp, ldv = _heads(v, "v", dt, n, kv, dim, dev)
+    sp = _dense(slots, "slots", (torch.int32,), (n,), dev)
+    qp, ldq, hq, op, ldo = None, 0, 0, None, 0
+    if q is None:
+        if q_weight is not None or q_out is not None:
+            raise ValueError("q_weight and q_out: there are no queries")
+    else:
+        if q.dim() != 3 or q.shape[1] == 0:
+            raise ValueError(f"q: shape {tuple(q.shape)}, expected [tokens, q_heads, dim]")
+        hq = q.shape[1]
+        qp, ldq = _heads(q, "q", dt, n, hq, dim, dev)
+        ldo = hq * dim
+        if q_out is not None:
+            op, ldo = _heads(q_out, "q_out", dt, n, hq, dim, dev)
+    qw, kw = (None if w is None else _dense(w, name, (dt,), (dim,), dev)
+              for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+    if (positions is None) != (freqs is None):
+        raise ValueError("positions and freqs: a rotation needs both")
+    pp = fp = None
+    rot = 0
+    if freqs is not None:
+        rot = 2 * freqs.numel()
+        pp = _dense(positions, "positions", (torch.int32,), (n,), dev)
+        fp = _dense(freqs, "freqs", (torch.float64,), (rot // 2,), dev)
+        if rot == 0:
+            pp = fp = None
+
+    def body(s):
+        o, p = q_out, op
+        if q is not None and o is None:
+            o = torch.empty(n, hq, dim, dtype=dt, device=q.device)
+            p = o.data_ptr()
+        st = lib.mxmoe_kv_append(C.byref(cache.t), n, qp, ldq, hq, kp, ldk, vp, ldv, qw, kw, eps, pp, fp, rot,
+                                 1 if interleaved else 0, sp, p, ldo, s)
+        if st:
+            raise MxmoeError(st, "mxmoe_kv_append")
+        return o
+
+    return _run_on(dev, stream, body, (q, k, v, slots, q_weight, k_weight, positions, freqs, q_out, *cache.buffers()))
+
+
+def kv_read(cache: KVCache, slots, stream=None):
+    """Rows of the cache back in its activation dtype (mxmoe_kv_read): (k, v), each [tokens,
+    heads, dim]; slots int32 [tokens], zeros for one outside the cache."""
+    torch = _torch()
+    lib = _lib or load_library()
+    dev = cache._dev
+    if slots.dim() != 1:
+        raise ValueError(f"slots: shape {tuple(slots.shape)}, expected [tokens]")
+    n = slots.shape[0]
+    sp = _dense(slots, "slots", (torch.int32,), (n,), dev)
+
+    def body(s):
+        k, v = (torch.empty(n, cache.heads, cache.dim, dtype=cache.dtype, device=cache.k.device) for _ in range(2))
+        st = lib.mxmoe_kv_read(C.byref(cache.t), n, sp, k.data_ptr(), v.data_ptr(), s)
+        if st:
+            raise MxmoeError(st, "mxmoe_kv_read")
+        return k, v
+
+    return _run_on(dev, stream, body, (slots, *cache.buffers()))
+
+
+def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len: int = 0, scale: Optional[float] = None,
+                     softcap: float = 0.0, out=None, stream=None):
+    """Attention of each sequence's last query tokens over its pages of the cache
+    (mxmoe_attention_decode): [batch * n_q, q_heads, dim] in the cache's dtype.
+
+    q [batch * n_q, q_heads, dim], sequence by sequence (n_q at most ATTENTION_QUERIES);
+    table int32 [batch, width], pages of the positions from prefix_len on; lengths int32
+    [batch], all tokens of a sequence (prefix and queries among them), 0 for padding; prefix
+    int32 [ceil(prefix_len / page_size)], pages that every sequence begins with.  scale:
+    1 / sqrt(dim) by default; softcap > 0 caps the scores."""
+    torch = _torch()
+    lib = _lib or load_library()
+    dev, dt, dim = cache._dev, cache.dtype, cache.dim
+    if q.dim() != 3 or table.dim() != 2:
+        raise ValueError(f"q {tuple(q.shape)}, table {tuple(table.shape)}: [batch * n_q, q_heads, dim] and [batch, width] are expected")
+    batch, width = table.shape
+    rows, hq = q.shape[0], q.shape[1]
+    n_q = rows // batch if batch else 1
+    if rows != batch * n_q or (batch and n_q == 0):
+        raise ValueError(f"q: {rows} tokens for {batch} sequences")
+    qp, ldq = _heads(q, "q", dt, rows, hq, dim, dev)
+    tp = _dense(table, "table", (torch.int32,), (batch, width), dev)
+    lp = _dense(lengths, "lengths", (torch.int32,), (batch,), dev)
+    pp = None
+    if prefix is None:
+        if prefix_len:
+            raise ValueError(f"prefix_len {prefix_len} without prefix")
+    else:
+        pp = _dense(prefix, "prefix", (torch.int32,), (-(-prefix_len // cache.page_size),), dev)
+        pp = pp if prefix_len else None
+    op, ldo = (None, hq * dim) if out is None else _heads(out, "out", dt, rows, hq, dim, dev)
+    if scale is None:
+        scale = dim ** -0.5
+    wsb = lib.mxmoe_attention_workspace_bytes(C.byref(cache.t), batch, n_q, hq, width, prefix_len)
+
+    def body(s):
+        o, p = out, op
+        if o is None:
+            o = torch.empty(rows, hq, dim, dtype=dt, device=q.device)
+            p = o.data_ptr()
+        ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
+        st = lib.mxmoe_attention_decode(C.byref(cache.t), qp, ldq, batch, n_q, hq, tp if width else None, width, lp, pp,
+                                        prefix_len, scale, softcap, p, ldo, ws.data_ptr() if wsb else None, wsb, s)
+        if st:
+            raise MxmoeError(st, "mxmoe_attention_decode")
+        return o
+
+    return _run_on(dev, stream, body, (q, table, lengths, prefix, out, *cache.buffers()))
 
 
 # --------------------------------------------------------------- routing
