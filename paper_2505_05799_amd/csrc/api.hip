@@ -870,7 +870,7 @@ mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, 
   a.table = table;
   a.lengths = lengths;
   a.prefix = prefix;
-  a.part = reinterpret_cast<float*>(workspace);
+  a.workspace = workspace;
   a.ldq = ldq;
   a.ldo = ldo;
   a.scale = scale;

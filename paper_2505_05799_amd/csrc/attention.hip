@@ -20,6 +20,8 @@
 // Tokens past a row's last are left out by selection, whatever they hold: their scores
 // become -inf, their values zeros.  Where rows of a tile see different tokens and a value
 // there is not finite, rows are added one by one, each with the values that it sees.
+#include <algorithm>
+
 #include "kvcache.h"
 #include "lanes.h"
 
@@ -71,259 +73,614 @@ LANES_INL float quarters_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-// Keys and values of 32 tokens as a lane holds them.
-template <int KIND, int D> struct Block {
+// Keys (or values) of 32 tokens as a lane holds them, and their scales.
+template <int KIND, int D> struct Frag {
   static constexpr int ES = KIND <= C_F16 ? 2 : 1, N = D * ES / 32;
-  u32x4 k[N], v[N];
-  f32x4 ks[2], vs[2];
-  LANES_INL void load(const AttnArgs& a, int64_t rec, int at, int lane) {
-    const uint8_t* kp = a.ck + ((rec << a.page_log2) + at) * (D * ES) + lane * 16;
-    const uint8_t* vp = a.cv + ((rec << a.page_log2) + at) * (D * ES) + lane * 16;
+  u32x4 w[N];
+  f32x4 s[ES == 1 ? 2 : 1];
+  LANES_INL void load(const uint8_t* base, const float* scales, int64_t token, int lane) {
+    const uint8_t* p = base + token * (D * ES) + lane * 16;
 #pragma unroll
-    for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const u32x4*>(kp + 1024 * i);
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const u32x4*>(vp + 1024 * i);
+    for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const u32x4*>(p + 1024 * i);
     if constexpr (ES == 1) {
-      const int64_t s = (rec << a.page_log2) + at + 4 * (lane >> 4);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        ks[i] = *reinterpret_cast<const f32x4*>(a.cks + s + 16 * i);
-        vs[i] = *reinterpret_cast<const f32x4*>(a.cvs + s + 16 * i);
-      }
+      for (int i = 0; i < 2; ++i) s[i] = *reinterpret_cast<const f32x4*>(scales + token + 4 * (lane >> 4) + 16 * i);
     }
   }
-  LANES_INL u32x4 key(int tile, int step) const {
-    if constexpr (ES == 2) return k[tile * (D / 32) + step];
-    const u32x4 p = k[tile * (D / 64) + (step >> 1)];
+  LANES_INL u32x4 key(int tile, int step) const {  // 16 tokens, 32 elements
+    if constexpr (ES == 2) return w[tile * (D / 32) + step];
+    const u32x4 p = w[tile * (D / 64) + (step >> 1)];
     return step & 1 ? widen8<KIND>(p[2], p[3]) : widen8<KIND>(p[0], p[1]);
   }
-  LANES_INL u32x4 value(int tile) const {
-    if constexpr (ES == 2) return v[tile];
-    const u32x4 p = v[tile >> 1];
+  LANES_INL u32x4 value(int tile) const {  // 16 elements, 32 tokens
+    if constexpr (ES == 2) return w[tile];
+    const u32x4 p = w[tile >> 1];
     return tile & 1 ? widen8<KIND>(p[2], p[3]) : widen8<KIND>(p[0], p[1]);
   }
 };
 
-// 16 query rows of a wavefront: row lane % 16.
-template <int KIND, int D> struct Rows16 {
-  static constexpr int ES = KIND <= C_F16 ? 2 : 1;
-  u32x4 q[D / 32];
-  f32x4 acc[D / 16];   // elements 16 i + 4 (lane / 16) + (0..3)
-  float ref, sum;      // the row's reference, the sum of its weights (this lane's tokens)
-  float mul;           // from a product of codes to a score, in powers of 2 (without a cap)
+// What a block's tokens are to the rows of a wavefront: `some` 1 if a row does not see
+// all 32 or the page is bad (NaN for whoever sees it); most, least: how many the rows see that
+// see most and least of them.
+struct Sight { int some, bad, most, least; };
 
-  LANES_INL void init(const AttnArgs& a, const uint16_t* row, int lane) {
-    const int qd = lane >> 4;
+// MF times 16 query rows of a wavefront: row 16 f + lane % 16.
+template <int KIND, int D, int MF> struct Rows16 {
+  static constexpr int ES = KIND <= C_F16 ? 2 : 1;
+  u32x4 q[MF][D / 32];
+  f32x4 acc[MF][D / 16];   // elements 16 i + 4 (lane / 16) + (0..3)
+  float ref[MF], sum[MF];  // the row's reference, the sum of its weights (this lane's tokens)
+  float mul[MF];           // from a product of codes to a score: in powers of 2, or (with a cap) parts of the cap
+  float w[MF][8];          // scores, then weights of the block in hand
+
+  LANES_INL void clear() {
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    ref = -__builtin_inff();
-    sum = 0.f;
-    mul = a.scale;
+    for (int f = 0; f < MF; ++f) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) acc[f][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      ref[f] = -__builtin_inff();
+      sum[f] = 0.f;
+    }
+  }
+  LANES_INL void load(const AttnArgs& a, int f, const uint16_t* row, int lane) {
+    const int qd = lane >> 4;
+    float m = a.scale;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
       const int c = ES == 2 ? 4 * s + qd : 8 * (s >> 1) + 2 * qd + (s & 1);
-      q[s] = row ? (u32x4) * reinterpret_cast<const u32x4_any*>(row + 8 * c) : u32x4{0u, 0u, 0u, 0u};
+      q[f][s] = row ? (u32x4) * reinterpret_cast<const u32x4_any*>(row + 8 * c) : u32x4{0u, 0u, 0u, 0u};
     }
     if (ES == 1 && a.act == MXMOE_BF16) {
-      uint32_t m = 0u;
+      uint32_t b = 0u;
 #pragma unroll
       for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m = max2(m, q[s][i] & 0x7fff7fffu);
-      m = max2(m, (uint32_t)__shfl_xor((int)m, 16, 64));
-      m = max2(m, (uint32_t)__shfl_xor((int)m, 32, 64));
-      const int e = (int)(max(m & 0xffffu, m >> 16) >> 7);  // exponent of the largest
+        for (int i = 0; i < 4; ++i) b = max2(b, q[f][s][i] & 0x7fff7fffu);
+      b = max2(b, (uint32_t)__shfl_xor((int)b, 16, 64));
+      b = max2(b, (uint32_t)__shfl_xor((int)b, 32, 64));
+      const int e = (int)(max(b & 0xffffu, b >> 16) >> 7);  // exponent of the largest
       const int up = e == 255 ? 0 : min(127, 127 + 14 - max(e, 1));
 #pragma unroll
       for (int s = 0; s < D / 32; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const f32x2 w = unpack2<MXMOE_BF16>(q[s][i]);
-          q[s][i] = pack2<MXMOE_F16>(__builtin_ldexpf(w[0], up), __builtin_ldexpf(w[1], up));
+          const f32x2 v = unpack2<MXMOE_BF16>(q[f][s][i]);
+          q[f][s][i] = pack2<MXMOE_F16>(__builtin_ldexpf(v[0], up), __builtin_ldexpf(v[1], up));
         }
-      mul = __builtin_ldexpf(mul, -up);
+      m = __builtin_ldexpf(m, -up);
     }
-    if (a.softcap > 0.f) mul = mul / a.softcap; else mul *= kLog2e;
+    mul[f] = a.softcap > 0.f ? m / a.softcap : m * kLog2e;
   }
 
-  // 32 tokens; limit: how many of them the lane's row sees.  MASK: some row sees fewer than
-  // 32 (or the page is bad: NaN for whoever sees it); most: what the row that sees most of
-  // them does, least: the real row that sees least.
-  template <bool MASK>
-  LANES_INL void add(const AttnArgs& a, const Block<KIND, D>& b, int lane, int limit, int most, int least, bool bad) {
-    const int t0 = 4 * (lane >> 4);
-    float x[8], w[8];
-    {
-      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  // products of the rows and 32 keys
+  LANES_INL void scores(const Frag<KIND, D>& k) {
+    f32x4 s[MF][2];
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
+    for (int f = 0; f < MF; ++f) s[f][0] = s[f][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) s[t] = mfma<KIND>(b.key(t, i), q[i], s[t]);
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 b = k.key(t, i);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) s[f][t] = mfma<KIND>(b, q[f][i], s[f][t]);
+      }
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = s[i >> 2][i & 3] * mul;
-        if constexpr (ES == 1) x[i] *= b.ks[i >> 2][i & 3];
+        w[f][i] = s[f][i >> 2][i & 3] * mul[f];
+        if constexpr (ES == 1) w[f][i] *= k.s[i >> 2][i & 3];
       }
-    }
-    if (a.softcap > 0.f) {
-      const float c = a.softcap * kLog2e;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)  // tanh y = 1 - 2 / (1 + e^(2 y))
-        x[i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e)));
-    }
+  }
+
+  // weights of the 32 tokens, sums and references; limit: how many of them a row sees
+  LANES_INL void weigh(const AttnArgs& a, const Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
     float vs[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (ES == 1) vs[i] = b.vs[i >> 2][i & 3]; else vs[i] = 1.f;
-      if constexpr (MASK) {
-        const bool in = t0 + (i & 3) + 16 * (i >> 2) < limit;
-        x[i] = in ? (bad ? __builtin_nanf("") : x[i]) : -__builtin_inff();
-        vs[i] = in ? vs[i] : 0.f;
-      }
-    }
-    auto weights = [&](float r, float (&p)[8]) {
-      float most_w = 0.f;
-      const float off = kBase - (r == -__builtin_inff() ? 0.f : r);
+    for (int i = 0; i < 8; ++i)
+      if constexpr (ES == 1) vs[i] = v.s[i >> 2][i & 3]; else vs[i] = 1.f;
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+      float x[8], p[8], s[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(x[i] + off);
-        w[i] = ES == 1 ? p[i] * vs[i] : p[i];
-        most_w = fmaxf(most_w, w[i]);
+        x[i] = w[f][i];
+        s[i] = vs[i];
       }
-      return most_w;
-    };
-    float p[8];
-    const float top = weights(ref, p);
-    // a row without a reference takes one from its first tokens
-    bool move = top > kMostWeight;
-    if (ref == -__builtin_inff()) {
+      if (a.softcap > 0.f) {
+        const float c = a.softcap * kLog2e;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) move |= x[i] > -__builtin_inff();
-    }
-    if (__ballot(move)) {
-      float m = -__builtin_inff();
+        for (int i = 0; i < 8; ++i)  // tanh y = 1 - 2 / (1 + e^(2 y))
+          x[i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e)));
+      }
+      if (g.some) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        m = fmaxf(m, x[i] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i], kLeastScale)) : 0.f));
-      m = quarters_max(m);
-      const float next = fmaxf(ref, m);
-      const float f = ref == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref - next);  // (nothing summed yet)
-      ref = next;
-      sum *= f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) acc[i] *= f;
-      weights(ref, p);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += p[i];
-    u32x4 pw;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) pw[i] = pack2<KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16>(w[2 * i], w[2 * i + 1]);
-    if constexpr (!MASK) {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) acc[i] = mfma<KIND>(b.value(i), pw, acc[i]);
-    } else {
-      // tokens j of the lane's eight that come before a limit, as a mask of 16-bit halves
-      auto cut = [&](u32x4 v, int lim) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 2 * (i & 1) + 16 * (i >> 1);
-          v[i] &= (t < lim ? 0xffffu : 0u) | (t + 1 < lim ? 0xffff0000u : 0u);
+        for (int i = 0; i < 8; ++i) {
+          const bool in = 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f];
+          x[i] = in ? (g.bad ? __builtin_nanf("") : x[i]) : -__builtin_inff();
+          s[i] = in ? s[i] : 0.f;
         }
-        return v;
+      }
+      auto weights = [&](float r) {
+        float top = 0.f;
+        const float off = kBase - (r == -__builtin_inff() ? 0.f : r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(x[i] + off);
+          w[f][i] = ES == 1 ? p[i] * s[i] : p[i];
+          top = fmaxf(top, w[f][i]);
+        }
+        return top;
       };
-      constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u;
+      bool move = weights(ref[f]) > kMostWeight;
+      if (ref[f] == -__builtin_inff()) {  // a row without a reference takes one from its first tokens
+#pragma unroll
+        for (int i = 0; i < 8; ++i) move |= x[i] > -__builtin_inff();
+      }
+      if (__ballot(move)) {
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          m = fmaxf(m, x[i] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(s[i], kLeastScale)) : 0.f));
+        const float next = fmaxf(ref[f], quarters_max(m));
+        const float d = ref[f] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref[f] - next);  // (nothing summed yet)
+        ref[f] = next;
+        sum[f] *= d;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) acc[f][i] *= d;
+        weights(ref[f]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[f] += p[i];
+    }
+  }
+
+  // weights times values
+  LANES_INL void add(const Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
+    u32x4 pw[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pw[f][i] = pack2<KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16>(w[f][2 * i], w[f][2 * i + 1]);
+    if (!g.some) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        const u32x4 v = cut(b.value(i), most);
-        bool odd = false;
-        if (least < most) {
+        const u32x4 b = v.value(i);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) odd |= (v[j] & kInf) == kInf || (v[j] & (kInf << 16)) == kInf << 16;
-        }
-        if (!__ballot(odd)) {
-          acc[i] = mfma<KIND>(v, pw, acc[i]);
-        } else {
-          f32x4 out = acc[i];
-          for (int r = 0; r < 16; ++r) {
-            const f32x4 o = mfma<KIND>(cut(v, __builtin_amdgcn_readlane(limit, r)), pw, acc[i]);
-            if ((lane & 15) == r) out = o;
-          }
-          acc[i] = out;
-        }
+        for (int f = 0; f < MF; ++f) acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
+      }
+      return;
+    }
+    // Values past the last token that any row sees are zeros.  One that is not finite must not reach
+    // the rows that do not see it (0 * inf): it is zero in the products, and rows become
+    // NaN where a second product, of ones, counts such values among the tokens they see.
+    constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
+    auto before = [&](int lim, uint32_t what) {  // `what` in the halves of the tokens before a limit
+      u32x4 m;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = 4 * (lane >> 4) + 2 * (i & 1) + 16 * (i >> 1);
+        m[i] = (t < lim ? what : 0u) | (t + 1 < lim ? what << 16 : 0u);
+      }
+      return m;
+    };
+    const u32x4 any = before(g.most, 0xffffu);
+    u32x4 sees[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) sees[f] = before(limit[f], kOne);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      u32x4 b = v.value(i) & any, odd;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t m = ((b[j] & kInf) == kInf ? 0xffffu : 0u) | ((b[j] & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
+        odd[j] = m & (kOne | kOne << 16);
+        b[j] &= ~m;
+      }
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
+        const f32x4 n = mfma<KIND>(odd, sees[f], f32x4{0.f, 0.f, 0.f, 0.f}), o = mfma<KIND>(b, pw[f], acc[f][i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[f][i][e] = n[e] > 0.f ? __builtin_nanf("") : o[e];
       }
     }
   }
 };
 
-// A wavefront takes 16 query rows of a sequence and kv head, and all tokens they see.
-template <int KIND, int D>
-__global__ void __launch_bounds__(64) attention_kernel(AttnArgs a) {
-  const int lane = threadIdx.x, n = lane & 15, qd = lane >> 4;
-  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, frags = (rows + 15) / 16;
-  const int frag = (int)blockIdx.x % frags, item = (int)blockIdx.x / frags;
-  const int h = item % a.kv_heads, s = item / a.kv_heads;
-  const int page = 1 << a.page_log2;
-  const int length = a.lengths[s];
-  const bool beyond = (int64_t)length > a.prefix_len + (int64_t)a.width * page;
-  const int r = 16 * frag + n, j = r / group;
-  const bool live = r < rows;
-  const int64_t head = (int64_t)h * group + r % group;
-  const int64_t tok = (int64_t)s * a.n_q + j;
-  Rows16<KIND, D> x;
-  x.init(a, live ? reinterpret_cast<const uint16_t*>(a.q) + tok * a.ldq + head * D : nullptr, lane);
-  const int seen = live ? max(0, length - a.n_q + 1 + j) : 0;  // tokens that the row sees
-  const int j0 = (16 * frag) / group, j1 = min(rows - 1, 16 * frag + 15) / group;
-  const int least = max(0, length - a.n_q + 1 + j0), most = beyond ? 0 : max(0, length - a.n_q + 1 + j1);
-  for (int part = 0; part < 2; ++part) {
-    const int first = part ? a.prefix_len : 0;  // position of the part's first token
-    const int end = part ? most - first : min(most, a.prefix_len);
-    const int32_t* pages = part ? a.table + (int64_t)s * a.width : a.prefix;
-    for (int t = 0; t < end; t += 32) {
-      const int id = pages[t >> a.page_log2];
-      const bool bad = id < 0 || id >= a.n_pages;
-      Block<KIND, D> b;
-      b.load(a, (int64_t)(bad ? 0 : id) * a.kv_heads + h, t & (page - 1), lane);
-      // (the prefix may end inside a block)
-      const int full = part ? 1 << 30 : a.prefix_len;
-      const int lo = min(least - first, full) - t, hi = min(end, full) - t;
-      if (lo >= 32 && !bad) x.template add<false>(a, b, lane, 32, 32, 32, false);
-      else x.template add<true>(a, b, lane, min(seen - first, full) - t, hi, lo, bad);
+// How far a partial sum's factor is from the joint reference's
+LANES_INL float join_factor(float ref, float top) { return ref == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref - top); }
+
+LANES_INL void store4(void* out, int64_t at, f32x4 o, int act) {
+  typedef u32x2 u32x2_half __attribute__((aligned(2)));
+  u32x2 w;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    w[e] = act == MXMOE_BF16 ? pack2<MXMOE_BF16>(o[2 * e], o[2 * e + 1]) : pack2<MXMOE_F16>(o[2 * e], o[2 * e + 1]);
+  *reinterpret_cast<u32x2_half*>(reinterpret_cast<uint16_t*>(out) + at) = w;
+}
+
+// Blocks of 32 tokens of a sequence's own pages (0 for a length past its table: its
+// queries are NaN, which the joining launch writes).
+LANES_INL int own_blocks(const AttnArgs& a, int b) {
+  const int own = a.lengths[b] - a.prefix_len;
+  return own <= 0 || own > a.width << a.page_log2 ? 0 : (own + 31) >> 5;
+}
+
+// Sequences' own pages.  The blocks of all items (sequence, row block, kv head) form one
+// list, which the workgroups share evenly: each takes `per` blocks in a row, across items as
+// they come.  An item within a workgroup's share is finished there; pieces of others go to
+// the workspace: slot 2 g of workgroup g for a piece that continues an item, 2 g + 1
+// for one that begins one.  The four wavefronts take an item's blocks in turn and meet in LDS.
+template <int KIND, int D, int MF>
+__global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_kernel(AttnArgs a) {
+  constexpr int RS = D + 4;  // a row in LDS: rows 4 banks apart
+  __shared__ float red[4 * 16 * RS];
+  __shared__ float stat[4][2][16];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
+  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
+  const int per_seq = a.kv_heads * a.row_blocks;  // items of a sequence
+  // this workgroup's share: total blocks, then the sequence in which it begins
+  int64_t total = 0;
+  for (int b = lane; b < a.batch; b += 64) total += own_blocks(a, b);
+  total = (int64_t)lanes_sum<64>((double)total) * per_seq;
+  const int64_t per = max((int64_t)4, (total + gridDim.x - 1) / gridDim.x);
+  int64_t at = per * blockIdx.x;
+  const int64_t stop = min(total, at + per);
+  int seq = 0;
+  int64_t begin = 0;  // of the sequence, in the list
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const int mine = b < a.batch ? own_blocks(a, b) : 0;
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t o = __shfl_up(upto, d, 64);
+      upto += lane >= d ? o : 0;
+    }
+    upto *= per_seq;
+    if (blockIdx.x == 0 && w == 0 && b < a.batch) a.starts[b] = begin + upto - (int64_t)mine * per_seq;
+    // (the first workgroup writes the starts of all sequences, others stop at theirs)
+    const uint64_t beyond = __ballot(begin + upto > at);
+    if (beyond && blockIdx.x) {
+      const int l = __builtin_ctzll(beyond);
+      seq = b0 + l;
+      begin += __shfl(upto - (int64_t)mine * per_seq, l, 64);
+      break;
+    }
+    begin += __shfl(upto, 63, 64);
+  }
+  if (blockIdx.x == 0) {
+    begin = 0;
+    seq = 0;
+    if (tid == 0) {
+      a.starts[a.batch] = total;
+      a.starts[a.batch + 1] = per;
     }
   }
-  const float sum = quarters_sum(x.sum);
-  if (!live) return;
-  const float f = beyond ? __builtin_nanf("") : sum == 0.f ? 0.f : 1.f / sum;
-  uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + tok * a.ldo + head * D + 4 * qd;
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  Rows16<KIND, D, MF> x;
+  while (at < stop) {
+    const int blocks = own_blocks(a, seq);
+    const int64_t in = at - begin;
+    if (in >= (int64_t)blocks * per_seq) {
+      begin += (int64_t)blocks * per_seq;
+      ++seq;
+      continue;
+    }
+    const int item = (int)(in / blocks), first = (int)(in - (int64_t)item * blocks);
+    const int last = (int)min((int64_t)blocks, first + (stop - at));
+    const int h = item % a.kv_heads, rb = item / a.kv_heads;
+    const int length = a.lengths[seq], own = length - a.prefix_len;
+    const int32_t* pages = a.table + (int64_t)seq * a.width;
+    int seen[MF];
+    x.clear();
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const f32x4 o = x.acc[i] * f;
-    u32x2 w;
+    for (int f = 0; f < MF; ++f) {
+      const int r = 16 * (MF * rb + f) + n, j = r / group;
+      const bool live = r < rows;
+      x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)seq * a.n_q + j) * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
+      seen[f] = live ? own - a.n_q + 1 + j : 0;
+    }
+    const int least = own - a.n_q + 1 + 16 * MF * rb / group, most = own - a.n_q + 1 + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
+    auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
+    auto token_of = [&](int i, int id) {
+      const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
+      return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
+    };
+    Frag<KIND, D> k, v;
+    int i = first + w;
+    int id = 0;
+    if (i < last) {
+      id = page_of(i);
+      const int64_t t = token_of(i, id);
+      k.load(a.ck, a.cks, t, lane);
+      v.load(a.cv, a.cvs, t, lane);
+    }
+    while (i < last) {
+      const int next = i + 4;
+      const int next_id = next < last ? page_of(next) : 0;
+      x.scores(k);
+      if (next < last) k.load(a.ck, a.cks, token_of(next, next_id), lane);
+      Sight g;
+      g.bad = (unsigned)id >= (unsigned)a.n_pages;
+      g.least = least - 32 * i;
+      g.most = most - 32 * i;
+      g.some = g.bad || g.least < 32;
+      int limit[MF];
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      w[e] = a.act == MXMOE_BF16 ? pack2<MXMOE_BF16>(o[2 * e], o[2 * e + 1]) : pack2<MXMOE_F16>(o[2 * e], o[2 * e + 1]);
-    typedef u32x2 u32x2_half __attribute__((aligned(2)));
-    *reinterpret_cast<u32x2_half*>(out + 16 * i) = w;
+      for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+      x.weigh(a, v, g, limit, lane);
+      x.add(v, g, limit, lane);
+      if (next < last) v.load(a.cv, a.cvs, token_of(next, next_id), lane);
+      i = next;
+      id = next_id;
+    }
+    // the wavefronts meet
+    const bool whole = first == 0 && last == blocks;
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+      const int r0 = 16 * (MF * rb + f), live = min(16, rows - r0);
+      const float s = quarters_sum(x.sum[f]);
+      __syncthreads();
+      if (n < live) {
+        if (qd == 0) {
+          stat[w][0][n] = x.ref[f];
+          stat[w][1][n] = s;
+        }
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(&red[(w * 16 + n) * RS + 16 * e + 4 * qd]) = x.acc[f][e];
+      }
+      __syncthreads();
+      for (int o = tid; o < live * (D / 4); o += 256) {
+        const int r = o / (D / 4), d = 4 * (o % (D / 4));
+        float top = stat[0][0][r];
+#pragma unroll
+        for (int j = 1; j < 4; ++j) top = fmaxf(top, stat[j][0][r]);
+        f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float c = join_factor(stat[j][0][r], top);
+          v4 += c * *reinterpret_cast<const f32x4*>(&red[(j * 16 + r) * RS + d]);
+          l += c * stat[j][1][r];
+        }
+        const int row = r0 + r, q = row / group;
+        const int64_t tok = (int64_t)seq * a.n_q + q, head = (int64_t)h * group + row % group;
+        if (whole && !a.prefix_len) {
+          store4(a.out, tok * a.ldo + head * D + d, v4 * (l == 0.f ? 0.f : 1.f / l), a.act);
+        } else {
+          float* part = whole ? a.own + (tok * a.q_heads + head) * RS
+                              : a.part + ((2 * (int64_t)blockIdx.x + (first == 0)) * (16 * MF) + 16 * f + r) * RS;
+          *reinterpret_cast<f32x4*>(part + d) = v4;
+          if (d == 0) {
+            part[D] = top;
+            part[D + 1] = l;
+          }
+        }
+      }
+    }
+    __syncthreads();
+    at += last - first;
   }
 }
 
-template <int KIND, int D> hipError_t go(const AttnArgs& a, hipStream_t s) {
-  const int64_t frags = (a.n_q * (a.q_heads / a.kv_heads) + 15) / 16;
-  hipLaunchKernelGGL((attention_kernel<KIND, D>), dim3((unsigned)(frags * a.batch * a.kv_heads)), dim3(64), 0, s, a);
+// The shared prefix: rows of all sequences (sequence by sequence, a query's heads of the kv
+// head side by side) against it.  A workgroup takes one share of the prefix's blocks, its
+// wavefronts 16 MF rows each.
+template <int KIND, int D, int MF>
+__global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_prefix_kernel(AttnArgs a) {
+  constexpr int RS = D + 4;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
+  const int group = a.q_heads / a.kv_heads, rows = a.batch * a.n_q * group;
+  const int h = (int)blockIdx.y, share = (int)blockIdx.z;
+  const int r0 = ((int)blockIdx.x * 4 + w) * 16 * MF;
+  if (r0 >= rows) return;
+  const int blocks = (a.prefix_len + 31) >> 5;
+  const int first = (int)((int64_t)blocks * share / a.shares), last = (int)((int64_t)blocks * (share + 1) / a.shares);
+  Rows16<KIND, D, MF> x;
+  x.clear();
+  int seen[MF], most = 0, least = 1 << 30;
+#pragma unroll
+  for (int f = 0; f < MF; ++f) {
+    const int r = r0 + 16 * f + n, tok = min(r, rows - 1) / group;
+    const bool live = r < rows;
+    x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + tok * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
+    const int b = tok / a.n_q;
+    seen[f] = live ? max(0, min(a.prefix_len, a.lengths[b] - a.n_q + 1 + tok % a.n_q)) : 0;
+    most = max(most, seen[f]);
+    least = min(least, live ? seen[f] : 1 << 30);
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) {
+    most = max(most, __shfl_xor(most, d, 64));
+    least = min(least, __shfl_xor(least, d, 64));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  auto token_of = [&](int i, int id) {
+    const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
+    return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
+  };
+  const int end = min(last, (most + 31) >> 5);
+  Frag<KIND, D> k, v;
+  int id = 0;
+  if (first < end) {
+    id = a.prefix[(32 * first) >> a.page_log2];
+    const int64_t t = token_of(first, id);
+    k.load(a.ck, a.cks, t, lane);
+    v.load(a.cv, a.cvs, t, lane);
+  }
+  for (int i = first; i < end; ++i) {
+    const int next_id = i + 1 < end ? a.prefix[(32 * (i + 1)) >> a.page_log2] : 0;
+    x.scores(k);
+    if (i + 1 < end) k.load(a.ck, a.cks, token_of(i + 1, next_id), lane);
+    Sight g;
+    g.bad = (unsigned)id >= (unsigned)a.n_pages;
+    g.least = least - 32 * i;
+    g.most = most - 32 * i;
+    g.some = g.bad || g.least < 32;
+    int limit[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+    x.weigh(a, v, g, limit, lane);
+    x.add(v, g, limit, lane);
+    if (i + 1 < end) v.load(a.cv, a.cvs, token_of(i + 1, next_id), lane);
+    id = next_id;
+  }
+#pragma unroll
+  for (int f = 0; f < MF; ++f) {
+    const int r = r0 + 16 * f + n;
+    const float s = quarters_sum(x.sum[f]);
+    if (r >= rows) continue;
+    const int tok = r / group;
+    float* part = a.pre + (((int64_t)share * a.batch * a.n_q + tok) * a.q_heads + (int64_t)h * group + r % group) * RS;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(part + 16 * e + 4 * qd) = x.acc[f][e];
+    if (qd == 0) {
+      part[D] = x.ref[f];
+      part[D + 1] = s;
+    }
+  }
+}
+
+// Pieces of a query row joined: of the prefix's shares, of the workgroups that shared its
+// item.  D / 4 lanes hold a row, the groups of lanes take pieces in turn.
+template <int D>
+__global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
+  constexpr int RS = D + 4, L = D / 4, GR = 256 / L;
+  __shared__ float red[GR][RS];
+  const int tid = threadIdx.x, d = 4 * (tid % L), gr = tid / L;
+  const int group = a.q_heads / a.kv_heads;
+  const int64_t tok = blockIdx.x / a.q_heads;
+  const int head = (int)(blockIdx.x - tok * a.q_heads), b = (int)(tok / a.n_q), h = head / group;
+  const int row = (int)(tok - (int64_t)b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
+  const int length = a.lengths[b];
+  const int64_t per = a.starts[a.batch + 1];
+  const int blocks = own_blocks(a, b);
+  const int64_t s0 = a.starts[b] + ((int64_t)rb * a.kv_heads + h) * blocks, e0 = s0 + blocks;
+  int64_t g0 = 0;
+  int pieces = 0;  // of the item
+  if (blocks) {
+    g0 = s0 / per;
+    pieces = (int)((e0 - 1) / per - g0) + 1;
+  }
+  if (pieces == 1 && !a.prefix_len) return;  // written where it was computed
+  const int shares = length > 0 ? a.shares : 0;
+  float top = -__builtin_inff(), l = 0.f;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int i = gr; i < shares + pieces; i += GR) {
+    const int64_t g = g0 + (i - shares);
+    const float* p = i < shares ? a.pre + (((int64_t)i * a.batch * a.n_q + tok) * a.q_heads + head) * RS
+                     : pieces == 1 ? a.own + (tok * a.q_heads + head) * RS
+                                   : a.part + ((2 * g + (i == shares)) * frag_rows + row % frag_rows) * RS;
+    const f32x4 o = *reinterpret_cast<const f32x4*>(p + d);
+    const float r = p[D], s = p[D + 1];
+    const float next = fmaxf(top, r), c = join_factor(top, next), e = join_factor(r, next);
+    v = v * c + o * e;
+    l = l * c + s * e;
+    top = next;
+  }
+  *reinterpret_cast<f32x4*>(&red[gr][d]) = v;
+  if (d == 0) {
+    red[gr][D] = top;
+    red[gr][D + 1] = l;
+  }
+  __syncthreads();
+  if (gr) return;
+  for (int i = 0; i < GR; ++i) top = fmaxf(top, red[i][D]);
+  l = 0.f;
+  v = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < GR; ++i) {
+    const float c = join_factor(red[i][D], top);
+    v += c * *reinterpret_cast<const f32x4*>(&red[i][d]);
+    l += c * red[i][D + 1];
+  }
+  const bool past = (int64_t)length > a.prefix_len + ((int64_t)a.width << a.page_log2);
+  store4(a.out, tok * a.ldo + (int64_t)head * D + d, v * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
+}
+
+constexpr int kGrid = 512;
+
+// Fragments of 16 rows that a wavefront takes
+int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : rows <= 32 || dim == 128 ? 2 : 4; }
+
+struct Plan { int frags, row_blocks, pre_frags, shares, grid; size_t starts, part, own, pre, total; };
+Plan plan_of(const AttnArgs& a, int dim) {
+  Plan p = {};
+  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
+  const int64_t rs = 4 * (int64_t)(dim + 4), all = (int64_t)a.batch * a.n_q * a.q_heads;
+  p.frags = frags_of(rows, dim);
+  p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
+  const int64_t most = (int64_t)a.batch * a.kv_heads * p.row_blocks * ((((int64_t)a.width << a.page_log2) + 31) / 32);
+  p.grid = (int)std::min<int64_t>(kGrid, std::max<int64_t>(1, (most + 3) / 4));
+  if (a.prefix_len) {
+    const int64_t prows = (int64_t)a.batch * rows;
+    p.pre_frags = frags_of(prows, dim);
+    const int64_t wgs = ((prows + 64 * p.pre_frags - 1) / (64 * p.pre_frags)) * a.kv_heads;
+    const int64_t blocks = ((int64_t)a.prefix_len + 31) / 32;
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((blocks + 3) / 4, 64), 512 / wgs));
+  }
+  auto align = [](size_t n) { return (n + 255) / 256 * 256; };
+  size_t o = 0;
+  p.starts = o; o = align(o + 8 * ((size_t)a.batch + 2));
+  p.part = o; o = align(o + 2 * (size_t)p.grid * 16 * p.frags * rs);
+  p.own = o; o = align(o + (a.prefix_len ? (size_t)all * rs : 0));
+  p.pre = o; o = align(o + (size_t)p.shares * all * rs);
+  p.total = o;
+  return p;
+}
+
+template <int KIND, int D, int MF> hipError_t go_own(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  hipLaunchKernelGGL((attention_kernel<KIND, D, MF>), dim3(p.grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
-template <int KIND> hipError_t by_dim(const AttnArgs& a, int dim, hipStream_t s) {
-  return dim == 64 ? go<KIND, 64>(a, s) : dim == 128 ? go<KIND, 128>(a, s) : go<KIND, 256>(a, s);
+template <int KIND, int D, int MF> hipError_t go_prefix(const AttnArgs& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.batch * a.n_q * (a.q_heads / a.kv_heads);
+  hipLaunchKernelGGL((attention_prefix_kernel<KIND, D, MF>), dim3((unsigned)((rows + 64 * MF - 1) / (64 * MF)), a.kv_heads, a.shares),
+                     dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.prefix_len) {
+    if constexpr (D == 64)
+      if (p.pre_frags == 4) e = go_prefix<KIND, D, 4>(a, s);
+    if constexpr (D <= 128)
+      if (p.pre_frags == 2) e = go_prefix<KIND, D, 2>(a, s);
+    if (p.pre_frags == 1) e = go_prefix<KIND, D, 1>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  if constexpr (D == 64)
+    if (p.frags == 4) e = go_own<KIND, D, 4>(a, p, s);
+  if constexpr (D <= 128)
+    if (p.frags == 2) e = go_own<KIND, D, 2>(a, p, s);
+  if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(attention_join_kernel<D>, dim3(a.batch * a.n_q * a.q_heads), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int KIND> hipError_t by_dim(const AttnArgs& a, const Plan& p, int dim, hipStream_t s) {
+  return dim == 64 ? go<KIND, 64>(a, p, s) : dim == 128 ? go<KIND, 128>(a, p, s) : go<KIND, 256>(a, p, s);
 }
 
 }  // namespace
 
-size_t attention_workspace(const AttnArgs&, int) { return 0; }
+size_t attention_workspace(const AttnArgs& a, int dim) { return plan_of(a, dim).total; }
 
-hipError_t launch_attention(const AttnArgs& a, int dim, hipStream_t s) {
-  if (a.qmax == kQmaxF8) return by_dim<C_F8>(a, dim, s);
-  if (a.qmax) return by_dim<C_I8>(a, dim, s);
-  return a.act == MXMOE_BF16 ? by_dim<C_BF16>(a, dim, s) : by_dim<C_F16>(a, dim, s);
+hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s) {
+  const Plan p = plan_of(a, dim);
+  uint8_t* ws = reinterpret_cast<uint8_t*>(a.workspace);
+  a.starts = reinterpret_cast<int64_t*>(ws + p.starts);
+  a.part = reinterpret_cast<float*>(ws + p.part);
+  a.own = reinterpret_cast<float*>(ws + p.own);
+  a.pre = reinterpret_cast<float*>(ws + p.pre);
+  a.frags = p.frags;
+  a.row_blocks = p.row_blocks;
+  a.shares = p.shares;
+  if (a.qmax == kQmaxF8) return by_dim<C_F8>(a, p, dim, s);
+  if (a.qmax) return by_dim<C_I8>(a, p, dim, s);
+  return a.act == MXMOE_BF16 ? by_dim<C_BF16>(a, p, dim, s) : by_dim<C_F16>(a, p, dim, s);
 }
 
 }  // namespace mxmoe

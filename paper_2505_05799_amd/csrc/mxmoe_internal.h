@@ -615,12 +615,17 @@ struct AttnArgs {
   const uint8_t *ck, *cv;
   const float *cks, *cvs;
   const int32_t *table, *lengths, *prefix;
-  float* part;      // workspace: partial sums
+  void* workspace;
   int64_t ldq, ldo;
   float scale, softcap;
   int32_t batch, n_q, q_heads, kv_heads, width, prefix_len, n_pages, page_log2, act, qmax;
+  // set by the launch: parts of the workspace, fragments of 16 rows to a wavefront, row blocks
+  // of an item, shares of the prefix
+  int64_t* starts;          // [batch + 2]: first block of a sequence, all blocks, blocks of a workgroup
+  float *part, *own, *pre;  // rows of dim + 4: sums, reference, sum of weights
+  int32_t frags, row_blocks, shares;
 };
 size_t attention_workspace(const AttnArgs& a, int dim);
-hipError_t launch_attention(const AttnArgs& a, int dim, hipStream_t s);
+hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s);
 
 }  // namespace mxmoe
