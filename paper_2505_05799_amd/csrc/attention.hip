@@ -307,161 +307,159 @@ LANES_INL int own_blocks(const AttnArgs& a, int b) {
   return own <= 0 || own > a.width << a.page_log2 ? 0 : (own + 31) >> 5;
 }
 
-// Sequences' own pages.  The blocks of all items (sequence, row block, kv head) form one
-// list, which the workgroups share evenly: each takes `per` blocks in a row, across items as
-// they come.  An item within a workgroup's share is finished there; pieces of others go to
-// the workspace: slot 2 g of workgroup g for a piece that continues an item, 2 g + 1
-// for one that begins one.  The four wavefronts take an item's blocks in turn and meet in LDS.
+// Sequences' own pages.  The blocks of all items (sequence, row block, kv head) form one list,
+// which the wavefronts share evenly: each takes `per` blocks in a row, across items as they come,
+// on its own (no barrier).  An item within a wavefront's share is finished there; pieces of
+// others go to the workspace: slot 2 g of wavefront g for a piece that continues an item,
+// 2 g + 1 for one that begins one.  The next block's keys are asked for when this one's
+// have made their scores, its values when this one's are added, in the same registers.
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_kernel(AttnArgs a) {
-  constexpr int RS = D + 4;  // a row in LDS: rows 4 banks apart
-  __shared__ float red[4 * 16 * RS];
-  __shared__ float stat[4][2][16];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
-  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
+  constexpr int RS = D + 4;
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, qd = lane >> 4;
+  const int wave = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, piece_rows = min(rows, 16 * MF);
   const int per_seq = a.kv_heads * a.row_blocks;  // items of a sequence
-  // this workgroup's share: total blocks, then the sequence in which it begins
+  // this wavefront's share: all blocks, then the sequence in which it begins
   int64_t total = 0;
   for (int b = lane; b < a.batch; b += 64) total += own_blocks(a, b);
   total = (int64_t)lanes_sum<64>((double)total) * per_seq;
-  const int64_t per = max((int64_t)4, (total + gridDim.x - 1) / gridDim.x);
-  int64_t at = per * blockIdx.x;
-  const int64_t stop = min(total, at + per);
-  int seq = 0;
+  const int64_t waves = (int64_t)gridDim.x * 4, per = max((int64_t)1, (total + waves - 1) / waves);
+  const int64_t at0 = per * wave;
+  int left = (int)(min(total, at0 + per) - at0);  // blocks of the share
+  if (left <= 0 && wave) return;
   int64_t begin = 0;  // of the sequence, in the list
+  int seq = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
-    const int mine = b < a.batch ? own_blocks(a, b) : 0;
+    const int64_t mine = (int64_t)(b < a.batch ? own_blocks(a, b) : 0) * per_seq;
     int64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const int64_t o = __shfl_up(upto, d, 64);
       upto += lane >= d ? o : 0;
     }
-    upto *= per_seq;
-    if (blockIdx.x == 0 && w == 0 && b < a.batch) a.starts[b] = begin + upto - (int64_t)mine * per_seq;
-    // (the first workgroup writes the starts of all sequences, others stop at theirs)
-    const uint64_t beyond = __ballot(begin + upto > at);
-    if (beyond && blockIdx.x) {
-      const int l = __builtin_ctzll(beyond);
-      seq = b0 + l;
-      begin += __shfl(upto - (int64_t)mine * per_seq, l, 64);
-      break;
+    if (wave == 0) {  // (the first wavefront writes all starts, others stop at their sequence)
+      if (b < a.batch) a.starts[b] = begin + upto - mine;
+    } else {
+      const uint64_t past = __ballot(begin + upto > at0);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        seq = b0 + l;
+        begin += __shfl(upto - mine, l, 64);
+        break;
+      }
     }
     begin += __shfl(upto, 63, 64);
   }
-  if (blockIdx.x == 0) {
+  if (wave == 0) {
     begin = 0;
-    seq = 0;
-    if (tid == 0) {
+    while (seq < a.batch && own_blocks(a, seq) == 0) ++seq;
+    if (lane == 0) {
       a.starts[a.batch] = total;
       a.starts[a.batch + 1] = per;
     }
+    if (left <= 0) return;
   }
-  seq = __builtin_amdgcn_readfirstlane(seq);
+  struct Place { int seq, item, i, blocks, h; };  // i: the block in hand of the item's blocks
+  Place c;
+  c.seq = __builtin_amdgcn_readfirstlane(seq);
+  c.blocks = own_blocks(a, c.seq);
+  {
+    const int64_t in = at0 - begin;
+    const int item = (int)(in / c.blocks);
+    c.item = __builtin_amdgcn_readfirstlane(item);
+    c.i = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)item * c.blocks));
+    c.h = c.item % a.kv_heads;
+  }
+  auto page_of = [&](const Place& p) { return a.table[(int64_t)p.seq * a.width + ((32 * p.i) >> a.page_log2)]; };
+  auto token_of = [&](const Place& p, int id) {
+    const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + p.h;
+    return (rec << a.page_log2) + ((32 * p.i) & ((1 << a.page_log2) - 1));
+  };
   Rows16<KIND, D, MF> x;
-  while (at < stop) {
-    const int blocks = own_blocks(a, seq);
-    const int64_t in = at - begin;
-    if (in >= (int64_t)blocks * per_seq) {
-      begin += (int64_t)blocks * per_seq;
-      ++seq;
-      continue;
-    }
-    const int item = (int)(in / blocks), first = (int)(in - (int64_t)item * blocks);
-    const int last = (int)min((int64_t)blocks, first + (stop - at));
-    const int h = item % a.kv_heads, rb = item / a.kv_heads;
-    const int length = a.lengths[seq], own = length - a.prefix_len;
-    const int32_t* pages = a.table + (int64_t)seq * a.width;
-    int seen[MF];
-    x.clear();
+  Frag<KIND, D> k, v;
+  int id = page_of(c);
+  {
+    const int64_t t = token_of(c, id);
+    k.load(a.ck, a.cks, t, lane);
+    v.load(a.cv, a.cvs, t, lane);
+  }
+  int seen[MF], least = 0, most = 0, first = 0;
+  bool fresh = true;
+  while (true) {
+    if (fresh) {  // an item begins here, for this wavefront
+      const int rb = c.item / a.kv_heads, own = a.lengths[c.seq] - a.prefix_len - a.n_q + 1;
+      x.clear();
 #pragma unroll
-    for (int f = 0; f < MF; ++f) {
-      const int r = 16 * (MF * rb + f) + n, j = r / group;
-      const bool live = r < rows;
-      x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)seq * a.n_q + j) * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
-      seen[f] = live ? own - a.n_q + 1 + j : 0;
-    }
-    const int least = own - a.n_q + 1 + 16 * MF * rb / group, most = own - a.n_q + 1 + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
-    auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
-    auto token_of = [&](int i, int id) {
-      const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
-      return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
-    };
-    Frag<KIND, D> k, v;
-    int i = first + w;
-    int id = 0;
-    if (i < last) {
-      id = page_of(i);
-      const int64_t t = token_of(i, id);
-      k.load(a.ck, a.cks, t, lane);
-      v.load(a.cv, a.cvs, t, lane);
-    }
-    while (i < last) {
-      const int next = i + 4;
-      const int next_id = next < last ? page_of(next) : 0;
-      x.scores(k);
-      if (next < last) k.load(a.ck, a.cks, token_of(next, next_id), lane);
-      Sight g;
-      g.bad = (unsigned)id >= (unsigned)a.n_pages;
-      g.least = least - 32 * i;
-      g.most = most - 32 * i;
-      g.some = g.bad || g.least < 32;
-      int limit[MF];
-#pragma unroll
-      for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
-      x.weigh(a, v, g, limit, lane);
-      x.add(v, g, limit, lane);
-      if (next < last) v.load(a.cv, a.cvs, token_of(next, next_id), lane);
-      i = next;
-      id = next_id;
-    }
-    // the wavefronts meet
-    const bool whole = first == 0 && last == blocks;
-#pragma unroll
-    for (int f = 0; f < MF; ++f) {
-      const int r0 = 16 * (MF * rb + f), live = min(16, rows - r0);
-      const float s = quarters_sum(x.sum[f]);
-      __syncthreads();
-      if (n < live) {
-        if (qd == 0) {
-          stat[w][0][n] = x.ref[f];
-          stat[w][1][n] = s;
-        }
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(&red[(w * 16 + n) * RS + 16 * e + 4 * qd]) = x.acc[f][e];
+      for (int f = 0; f < MF; ++f) {
+        const int r = 16 * (MF * rb + f) + n, j = r / group;
+        const bool live = r < rows;
+        x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)c.seq * a.n_q + j) * a.ldq + ((int64_t)c.h * group + r % group) * D : nullptr, lane);
+        seen[f] = live ? own + j : 0;
       }
-      __syncthreads();
-      for (int o = tid; o < live * (D / 4); o += 256) {
-        const int r = o / (D / 4), d = 4 * (o % (D / 4));
-        float top = stat[0][0][r];
+      least = own + 16 * MF * rb / group;
+      most = own + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
+      first = c.i;
+    }
+    Place o = c;  // the next block
+    const bool more = --left > 0;
+    ++o.i;
+    fresh = o.i == c.blocks;
+    if (more && fresh) {
+      o.i = 0;
+      ++o.item;
+      if (o.item == per_seq) {
+        o.item = 0;
+        do ++o.seq;
+        while ((o.blocks = own_blocks(a, o.seq)) == 0);
+      }
+      o.h = o.item % a.kv_heads;
+    }
+    const int next_id = more ? page_of(o) : 0;
+    const int64_t next = token_of(o, next_id);
+    x.scores(k);
+    if (more) k.load(a.ck, a.cks, next, lane);
+    Sight g;
+    g.bad = (unsigned)id >= (unsigned)a.n_pages;
+    g.least = least - 32 * c.i;
+    g.most = most - 32 * c.i;
+    g.some = g.bad || g.least < 32;
+    int limit[MF];
 #pragma unroll
-        for (int j = 1; j < 4; ++j) top = fmaxf(top, stat[j][0][r]);
-        f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
+    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * c.i;
+    x.weigh(a, v, g, limit, lane);
+    x.add(v, g, limit, lane);
+    if (more) v.load(a.cv, a.cvs, next, lane);
+    if (fresh || !more) {
+      const bool whole = first == 0 && fresh;
+      const int rb = c.item / a.kv_heads;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float c = join_factor(stat[j][0][r], top);
-          v4 += c * *reinterpret_cast<const f32x4*>(&red[(j * 16 + r) * RS + d]);
-          l += c * stat[j][1][r];
-        }
-        const int row = r0 + r, q = row / group;
-        const int64_t tok = (int64_t)seq * a.n_q + q, head = (int64_t)h * group + row % group;
-        if (whole && !a.prefix_len) {
-          store4(a.out, tok * a.ldo + head * D + d, v4 * (l == 0.f ? 0.f : 1.f / l), a.act);
-        } else {
-          float* part = whole ? a.own + (tok * a.q_heads + head) * RS
-                              : a.part + ((2 * (int64_t)blockIdx.x + (first == 0)) * (16 * MF) + 16 * f + r) * RS;
-          *reinterpret_cast<f32x4*>(part + d) = v4;
-          if (d == 0) {
-            part[D] = top;
-            part[D + 1] = l;
+      for (int f = 0; f < MF; ++f) {
+        const float l = quarters_sum(x.sum[f]);
+        const int pr = 16 * f + n, row = 16 * MF * rb + pr, q = row / group;
+        if (row < rows) {
+          const int64_t tok = (int64_t)c.seq * a.n_q + q, head = (int64_t)c.h * group + row % group;
+          if (whole && !a.prefix_len) {
+            const float m = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) store4(a.out, tok * a.ldo + head * D + 16 * e + 4 * qd, x.acc[f][e] * m, a.act);
+          } else {
+            float* part = whole ? a.own + (tok * a.q_heads + head) * RS
+                                : a.part + ((2 * (int64_t)wave + (first == 0)) * piece_rows + pr) * RS;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(part + 16 * e + 4 * qd) = x.acc[f][e];
+            if (qd == 0) {
+              part[D] = x.ref[f];
+              part[D + 1] = l;
+            }
           }
         }
       }
+      if (!more) break;
     }
-    __syncthreads();
-    at += last - first;
+    c = o;
+    id = next_id;
   }
 }
 
@@ -544,7 +542,7 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   }
 }
 
-// Pieces of a query row joined: of the prefix's shares, of the workgroups that shared its
+// Pieces of a query row joined: of the prefix's shares, of the wavefronts that shared its
 // item.  D / 4 lanes hold a row, the groups of lanes take pieces in turn.
 template <int D>
 __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
@@ -555,6 +553,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
   const int64_t tok = blockIdx.x / a.q_heads;
   const int head = (int)(blockIdx.x - tok * a.q_heads), b = (int)(tok / a.n_q), h = head / group;
   const int row = (int)(tok - (int64_t)b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
+  const int piece_rows = min(a.n_q * group, frag_rows);
   const int length = a.lengths[b];
   const int64_t per = a.starts[a.batch + 1];
   const int blocks = own_blocks(a, b);
@@ -573,7 +572,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
     const int64_t g = g0 + (i - shares);
     const float* p = i < shares ? a.pre + (((int64_t)i * a.batch * a.n_q + tok) * a.q_heads + head) * RS
                      : pieces == 1 ? a.own + (tok * a.q_heads + head) * RS
-                                   : a.part + ((2 * g + (i == shares)) * frag_rows + row % frag_rows) * RS;
+                                   : a.part + ((2 * g + (i == shares)) * piece_rows + row % frag_rows) * RS;
     const f32x4 o = *reinterpret_cast<const f32x4*>(p + d);
     const float r = p[D], s = p[D + 1];
     const float next = fmaxf(top, r), c = join_factor(top, next), e = join_factor(r, next);
@@ -613,7 +612,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   p.frags = frags_of(rows, dim);
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
   const int64_t most = (int64_t)a.batch * a.kv_heads * p.row_blocks * ((((int64_t)a.width << a.page_log2) + 31) / 32);
-  p.grid = (int)std::min<int64_t>(kGrid, std::max<int64_t>(1, (most + 3) / 4));
+  p.grid = (int)std::min<int64_t>(kGrid, std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront at least
   if (a.prefix_len) {
     const int64_t prows = (int64_t)a.batch * rows;
     p.pre_frags = frags_of(prows, dim);
@@ -624,7 +623,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   auto align = [](size_t n) { return (n + 255) / 256 * 256; };
   size_t o = 0;
   p.starts = o; o = align(o + 8 * ((size_t)a.batch + 2));
-  p.part = o; o = align(o + 2 * (size_t)p.grid * 16 * p.frags * rs);
+  p.part = o; o = align(o + 8 * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
   p.own = o; o = align(o + (a.prefix_len ? (size_t)all * rs : 0));
   p.pre = o; o = align(o + (size_t)p.shares * all * rs);
   p.total = o;
