@@ -321,22 +321,24 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, piece_rows = min(rows, 16 * MF);
   const int per_seq = a.kv_heads * a.row_blocks;  // items of a sequence
   // this wavefront's share: all blocks, then the sequence in which it begins
-  int64_t total = 0;
+  uint32_t total = 0;  // (fewer than 2^31: the host sees to it)
   for (int b = lane; b < a.batch; b += 64) total += own_blocks(a, b);
-  total = (int64_t)lanes_sum<64>((double)total) * per_seq;
-  const int64_t waves = (int64_t)gridDim.x * 4, per = max((int64_t)1, (total + waves - 1) / waves);
-  const int64_t at0 = per * wave;
-  int left = (int)(min(total, at0 + per) - at0);  // blocks of the share
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
+  total = __builtin_amdgcn_readfirstlane(total * per_seq);
+  const uint32_t waves = gridDim.x * 4, per = max(1u, (total + waves - 1) / waves);
+  const uint32_t at0 = min(total, per * wave);
+  int left = (int)min(total - at0, per);  // blocks of the share
   if (left <= 0 && wave) return;
-  int64_t begin = 0;  // of the sequence, in the list
+  uint32_t begin = 0;  // of the sequence, in the list
   int seq = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
-    const int64_t mine = (int64_t)(b < a.batch ? own_blocks(a, b) : 0) * per_seq;
-    int64_t upto = mine;
+    const uint32_t mine = (b < a.batch ? own_blocks(a, b) : 0) * per_seq;
+    uint32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const int64_t o = __shfl_up(upto, d, 64);
+      const uint32_t o = __shfl_up(upto, d, 64);
       upto += lane >= d ? o : 0;
     }
     if (wave == 0) {  // (the first wavefront writes all starts, others stop at their sequence)
@@ -366,10 +368,9 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   c.seq = __builtin_amdgcn_readfirstlane(seq);
   c.blocks = own_blocks(a, c.seq);
   {
-    const int64_t in = at0 - begin;
-    const int item = (int)(in / c.blocks);
-    c.item = __builtin_amdgcn_readfirstlane(item);
-    c.i = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)item * c.blocks));
+    const uint32_t in = __builtin_amdgcn_readfirstlane(at0 - begin);
+    c.item = in / c.blocks;
+    c.i = in - c.item * c.blocks;
     c.h = c.item % a.kv_heads;
   }
   auto page_of = [&](const Place& p) { return a.table[(int64_t)p.seq * a.width + ((32 * p.i) >> a.page_log2)]; };
@@ -463,6 +464,105 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   }
 }
 
+// Items of few blocks: a workgroup of W wavefronts takes an item, its wavefronts every Wth
+// block, and they meet in LDS: one launch, nothing in the workspace (but with a prefix).
+template <int KIND, int D, int MF, int W>
+__global__ void __launch_bounds__(64 * W, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_item_kernel(AttnArgs a) {
+  constexpr int RS = D + 4;  // a row in LDS: rows 4 banks apart
+  __shared__ float red[W * 16 * RS];
+  __shared__ float stat[W][2][16];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
+  const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, per_seq = a.kv_heads * a.row_blocks;
+  const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq, rb = item / a.kv_heads, h = item - rb * a.kv_heads;
+  const int length = a.lengths[seq], own = length - a.prefix_len - a.n_q + 1;
+  const int32_t* pages = a.table + (int64_t)seq * a.width;
+  auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
+  auto token_of = [&](int i, int id) {
+    const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
+    return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
+  };
+  int i = w;
+  int id = 32 * i < a.width << a.page_log2 ? page_of(i) : 0;  // (asked for beside the length)
+  Rows16<KIND, D, MF> x;
+  x.clear();
+  int seen[MF];
+#pragma unroll
+  for (int f = 0; f < MF; ++f) {
+    const int r = 16 * (MF * rb + f) + n, j = r / group;
+    const bool live = r < rows;
+    x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)seq * a.n_q + j) * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
+    seen[f] = live ? own + j : 0;
+  }
+  const int blocks = own_blocks(a, seq);
+  const bool past = (int64_t)length > a.prefix_len + ((int64_t)a.width << a.page_log2);
+  const int least = own + 16 * MF * rb / group, most = own + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
+  Frag<KIND, D> k, v;
+  if (i < blocks) {
+    const int64_t t = token_of(i, id);
+    k.load(a.ck, a.cks, t, lane);
+    v.load(a.cv, a.cvs, t, lane);
+  }
+  while (i < blocks) {
+    const int next = i + W;
+    const int next_id = next < blocks ? page_of(next) : 0;
+    x.scores(k);
+    if (next < blocks) k.load(a.ck, a.cks, token_of(next, next_id), lane);
+    Sight g;
+    g.bad = (unsigned)id >= (unsigned)a.n_pages;
+    g.least = least - 32 * i;
+    g.most = most - 32 * i;
+    g.some = g.bad || g.least < 32;
+    int limit[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+    x.weigh(a, v, g, limit, lane);
+    x.add(v, g, limit, lane);
+    if (next < blocks) v.load(a.cv, a.cvs, token_of(next, next_id), lane);
+    i = next;
+    id = next_id;
+  }
+  const int used = min(W, max(1, blocks));  // wavefronts that have seen a block
+#pragma unroll
+  for (int f = 0; f < MF; ++f) {
+    const int r0 = 16 * (MF * rb + f), live = min(16, rows - r0);
+    const float s = quarters_sum(x.sum[f]);
+    if (f) __syncthreads();
+    if (n < live && w < used) {
+      if (qd == 0) {
+        stat[w][0][n] = x.ref[f];
+        stat[w][1][n] = s;
+      }
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(&red[(w * 16 + n) * RS + 16 * e + 4 * qd]) = x.acc[f][e];
+    }
+    __syncthreads();
+    for (int o = tid; o < live * (D / 4); o += 64 * W) {
+      const int r = o / (D / 4), d = 4 * (o % (D / 4));
+      float top = stat[0][0][r];
+      for (int j = 1; j < used; ++j) top = fmaxf(top, stat[j][0][r]);
+      f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
+      float l = 0.f;
+      for (int j = 0; j < used; ++j) {
+        const float c = join_factor(stat[j][0][r], top);
+        v4 += c * *reinterpret_cast<const f32x4*>(&red[(j * 16 + r) * RS + d]);
+        l += c * stat[j][1][r];
+      }
+      const int row = r0 + r, q = row / group;
+      const int64_t tok = (int64_t)seq * a.n_q + q, head = (int64_t)h * group + row % group;
+      if (!a.prefix_len) {
+        store4(a.out, tok * a.ldo + head * D + d, v4 * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
+      } else {
+        float* part = a.own + (tok * a.q_heads + head) * RS;
+        *reinterpret_cast<f32x4*>(part + d) = v4;
+        if (d == 0) {
+          part[D] = top;
+          part[D + 1] = l;
+        }
+      }
+    }
+  }
+}
+
 // The shared prefix: rows of all sequences (sequence by sequence, a query's heads of the kv
 // head side by side) against it.  A workgroup takes one share of the prefix's blocks, its
 // wavefronts 16 MF rows each.
@@ -543,57 +643,84 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
 }
 
 // Pieces of a query row joined: of the prefix's shares, of the wavefronts that shared its
-// item.  D / 4 lanes hold a row, the groups of lanes take pieces in turn.
-template <int D>
-__global__ void __launch_bounds__(256) attention_join_kernel(AttnArgs a) {
-  constexpr int RS = D + 4, L = D / 4, GR = 256 / L;
-  __shared__ float red[GR][RS];
-  const int tid = threadIdx.x, d = 4 * (tid % L), gr = tid / L;
+// item.  D / 4 lanes hold a row; GP groups of them take the pieces of one row in turn, four at
+// a time, and meet in LDS.
+template <int D, int GP>
+__global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_kernel(AttnArgs a) {
+  constexpr int RS = D + 4, L = D / 4, T = GP == 32 ? 32 * L : 256, R = T / (L * GP);  // rows of a workgroup
+  __shared__ float red[GP > 1 ? GP : 1][RS];
+  const int tid = threadIdx.x, d = 4 * (tid % L), gr = tid / L % GP;
   const int group = a.q_heads / a.kv_heads;
-  const int64_t tok = blockIdx.x / a.q_heads;
-  const int head = (int)(blockIdx.x - tok * a.q_heads), b = (int)(tok / a.n_q), h = head / group;
-  const int row = (int)(tok - (int64_t)b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
+  const int rank = (int)blockIdx.x * R + tid / (L * GP);  // (fewer than 2^26)
+  if (R > 1 && rank >= a.batch * a.n_q * a.q_heads) return;
+  const int64_t tok = rank / a.q_heads;
+  const int head = rank - (int)tok * a.q_heads, b = (int)tok / a.n_q, h = head / group;
+  const int row = ((int)tok - b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
   const int piece_rows = min(a.n_q * group, frag_rows);
   const int length = a.lengths[b];
-  const int64_t per = a.starts[a.batch + 1];
   const int blocks = own_blocks(a, b);
-  const int64_t s0 = a.starts[b] + ((int64_t)rb * a.kv_heads + h) * blocks, e0 = s0 + blocks;
-  int64_t g0 = 0;
-  int pieces = 0;  // of the item
-  if (blocks) {
+  uint32_t g0 = 0;
+  int pieces = blocks > 0;  // of the item
+  if (!a.direct && blocks) {
+    const uint32_t per = a.starts[a.batch + 1], s0 = a.starts[b] + (rb * a.kv_heads + h) * blocks;
     g0 = s0 / per;
-    pieces = (int)((e0 - 1) / per - g0) + 1;
+    pieces = (int)((s0 + blocks - 1) / per - g0) + 1;
   }
   if (pieces == 1 && !a.prefix_len) return;  // written where it was computed
-  const int shares = length > 0 ? a.shares : 0;
+  const int shares = length > 0 ? a.shares : 0, n = shares + pieces;
   float top = -__builtin_inff(), l = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int i = gr; i < shares + pieces; i += GR) {
-    const int64_t g = g0 + (i - shares);
-    const float* p = i < shares ? a.pre + (((int64_t)i * a.batch * a.n_q + tok) * a.q_heads + head) * RS
-                     : pieces == 1 ? a.own + (tok * a.q_heads + head) * RS
-                                   : a.part + ((2 * g + (i == shares)) * piece_rows + row % frag_rows) * RS;
-    const f32x4 o = *reinterpret_cast<const f32x4*>(p + d);
-    const float r = p[D], s = p[D + 1];
-    const float next = fmaxf(top, r), c = join_factor(top, next), e = join_factor(r, next);
-    v = v * c + o * e;
-    l = l * c + s * e;
+  for (int i0 = gr; i0 < n; i0 += 4 * GP) {
+    f32x4 o[4];
+    float r[4], s[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * GP;
+      if (i < n) {
+        const int64_t g = g0 + (uint32_t)(i - shares);
+        const float* p = i < shares ? a.pre + (((int64_t)i * a.batch * a.n_q + tok) * a.q_heads + head) * RS
+                         : pieces == 1 ? a.own + (tok * a.q_heads + head) * RS
+                                       : a.part + ((2 * g + (i == shares)) * piece_rows + row % frag_rows) * RS;
+        o[j] = *reinterpret_cast<const f32x4*>(p + d);
+        r[j] = p[D];
+        s[j] = p[D + 1];
+      } else {
+        o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        r[j] = -__builtin_inff();
+        s[j] = 0.f;
+      }
+    }
+    float next = top;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) next = fmaxf(next, r[j]);
+    const float c = join_factor(top, next);
+    v *= c;
+    l *= c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float e = join_factor(r[j], next);
+      v += o[j] * e;
+      l += s[j] * e;
+    }
     top = next;
   }
-  *reinterpret_cast<f32x4*>(&red[gr][d]) = v;
-  if (d == 0) {
-    red[gr][D] = top;
-    red[gr][D + 1] = l;
-  }
-  __syncthreads();
-  if (gr) return;
-  for (int i = 0; i < GR; ++i) top = fmaxf(top, red[i][D]);
-  l = 0.f;
-  v = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < GR; ++i) {
-    const float c = join_factor(red[i][D], top);
-    v += c * *reinterpret_cast<const f32x4*>(&red[i][d]);
-    l += c * red[i][D + 1];
+  if constexpr (GP > 1) {
+    *reinterpret_cast<f32x4*>(&red[gr][d]) = v;
+    if (d == 0) {
+      red[gr][D] = top;
+      red[gr][D + 1] = l;
+    }
+    __syncthreads();
+    if (gr) return;
+    const int used = min(GP, n);
+    for (int i = 0; i < used; ++i) top = fmaxf(top, red[i][D]);
+    l = 0.f;
+    v = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < used; ++i) {
+      const float c = join_factor(red[i][D], top);
+      v += c * *reinterpret_cast<const f32x4*>(&red[i][d]);
+      l += c * red[i][D + 1];
+    }
   }
   const bool past = (int64_t)length > a.prefix_len + ((int64_t)a.width << a.page_log2);
   store4(a.out, tok * a.ldo + (int64_t)head * D + d, v * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
@@ -604,14 +731,22 @@ constexpr int kGrid = 512;
 // Fragments of 16 rows that a wavefront takes
 int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : rows <= 32 || dim == 128 ? 2 : 4; }
 
-struct Plan { int frags, row_blocks, pre_frags, shares, grid; size_t starts, part, own, pre, total; };
+// Wavefronts to an item, or 0 where the list of blocks is shared
+int direct_of(int64_t items, int64_t most) {
+  if (most <= 64 && items <= 256) return 8;
+  if (most <= 16) return 4;
+  return 0;
+}
+
+struct Plan { int direct, frags, row_blocks, pre_frags, shares, grid, pieces; size_t starts, part, own, pre, total; };
 Plan plan_of(const AttnArgs& a, int dim) {
   Plan p = {};
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
   const int64_t rs = 4 * (int64_t)(dim + 4), all = (int64_t)a.batch * a.n_q * a.q_heads;
   p.frags = frags_of(rows, dim);
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
-  const int64_t most = (int64_t)a.batch * a.kv_heads * p.row_blocks * ((((int64_t)a.width << a.page_log2) + 31) / 32);
+  const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_blocks, longest = ((int64_t)a.width << a.page_log2) / 32, most = items * longest;
+  p.direct = direct_of(items, longest);
   p.grid = (int)std::min<int64_t>(kGrid, std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront at least
   if (a.prefix_len) {
     const int64_t prows = (int64_t)a.batch * rows;
@@ -620,17 +755,28 @@ Plan plan_of(const AttnArgs& a, int dim) {
     const int64_t blocks = ((int64_t)a.prefix_len + 31) / 32;
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((blocks + 3) / 4, 64), 512 / wgs));
   }
+  // pieces of a row at the most, if all sequences are as long as the table allows
+  p.pieces = p.shares + 1 + (p.direct ? 0 : (int)(4 * (int64_t)p.grid / items));
   auto align = [](size_t n) { return (n + 255) / 256 * 256; };
   size_t o = 0;
-  p.starts = o; o = align(o + 8 * ((size_t)a.batch + 2));
-  p.part = o; o = align(o + 8 * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
+  p.starts = o; o = align(o + (p.direct ? 0 : 4 * ((size_t)a.batch + 2)));
+  p.part = o; o = align(o + (p.direct ? 0 : 8) * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
   p.own = o; o = align(o + (a.prefix_len ? (size_t)all * rs : 0));
   p.pre = o; o = align(o + (size_t)p.shares * all * rs);
   p.total = o;
   return p;
 }
 
+template <int KIND, int D, int MF, int W> hipError_t go_item(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  hipLaunchKernelGGL((attention_item_kernel<KIND, D, MF, W>), dim3((unsigned)(a.batch * a.kv_heads * p.row_blocks)), dim3(64 * W), 0, s, a);
+  return hipGetLastError();
+}
 template <int KIND, int D, int MF> hipError_t go_own(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  if (p.direct) {
+    if constexpr (D < 256)  // (8 wavefronts of 256 elements: their rows in LDS are for one workgroup alone)
+      if (p.direct == 8) return go_item<KIND, D, MF, 8>(a, p, s);
+    return go_item<KIND, D, MF, 4>(a, p, s);
+  }
   hipLaunchKernelGGL((attention_kernel<KIND, D, MF>), dim3(p.grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -655,8 +801,14 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
   if constexpr (D <= 128)
     if (p.frags == 2) e = go_own<KIND, D, 2>(a, p, s);
   if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(attention_join_kernel<D>, dim3(a.batch * a.n_q * a.q_heads), dim3(256), 0, s, a);
+  if (e != hipSuccess || (p.direct && !a.prefix_len)) return e;
+  const unsigned all = (unsigned)(a.batch * a.n_q * a.q_heads);
+  if (p.pieces <= 8)
+    hipLaunchKernelGGL((attention_join_kernel<D, 1>), dim3((all * (D / 4) + 255) / 256), dim3(256), 0, s, a);
+  else if (p.pieces <= 32 || D == 256)
+    hipLaunchKernelGGL((attention_join_kernel<D, 1024 / D>), dim3(all), dim3(256), 0, s, a);
+  else if constexpr (D < 256)
+    hipLaunchKernelGGL((attention_join_kernel<D, 32>), dim3(all), dim3(8 * D), 0, s, a);
   return hipGetLastError();
 }
 template <int KIND> hipError_t by_dim(const AttnArgs& a, const Plan& p, int dim, hipStream_t s) {
@@ -670,13 +822,14 @@ size_t attention_workspace(const AttnArgs& a, int dim) { return plan_of(a, dim).
 hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s) {
   const Plan p = plan_of(a, dim);
   uint8_t* ws = reinterpret_cast<uint8_t*>(a.workspace);
-  a.starts = reinterpret_cast<int64_t*>(ws + p.starts);
+  a.starts = reinterpret_cast<uint32_t*>(ws + p.starts);
   a.part = reinterpret_cast<float*>(ws + p.part);
   a.own = reinterpret_cast<float*>(ws + p.own);
   a.pre = reinterpret_cast<float*>(ws + p.pre);
   a.frags = p.frags;
   a.row_blocks = p.row_blocks;
   a.shares = p.shares;
+  a.direct = p.direct;
   if (a.qmax == kQmaxF8) return by_dim<C_F8>(a, p, dim, s);
   if (a.qmax) return by_dim<C_I8>(a, p, dim, s);
   return a.act == MXMOE_BF16 ? by_dim<C_BF16>(a, p, dim, s) : by_dim<C_F16>(a, p, dim, s);
