@@ -236,54 +236,80 @@ template <int KIND, int D, int MF> struct Rows16 {
     }
   }
 
+  // Values for rows that do not see all of them.  Past the last token that any row sees they are
+  // zeros.  One that is not finite must not reach the rows that do not see it (0 * inf): it
+  // becomes zero, and rows become NaN where a product of ones counts such values among
+  // the tokens they see.
+  LANES_INL void sift(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
+    if constexpr (KIND == C_I8) return;  // (every code is finite, the weights of what is not seen are 0)
+    constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
+    const int t0 = 4 * (lane >> 4);
+    auto before = [&](int lim, uint32_t what) {  // `what` in the halves of the tokens before a limit
+      u32x4 m;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + 2 * (i & 1) + 16 * (i >> 1);
+        m[i] = (t < lim ? what : 0u) | (t + 1 < lim ? what << 16 : 0u);
+      }
+      return m;
+    };
+    auto strange = [&](uint32_t w) -> uint32_t {  // ones where a value is not finite
+      if constexpr (ES == 2) return ((w & kInf) == kInf ? 0xffffu : 0u) | ((w & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
+      const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f, 0xff
+      return (top >> 7) * 0xffu;
+    };
+    u32x4 any;
+    if constexpr (ES == 2) {
+      any = before(g.most, 0xffffu);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + 16 * (i & 1);
+        any[i] = (t < g.most ? 0xffu : 0u) | (t + 1 < g.most ? 0xff00u : 0u) | (t + 2 < g.most ? 0xff0000u : 0u) | (t + 3 < g.most ? 0xff000000u : 0u);
+      }
+    }
+    uint32_t odd = 0u;
+#pragma unroll
+    for (int i = 0; i < Frag<KIND, D>::N; ++i) {
+      v.w[i] &= any;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) odd |= strange(v.w[i][j]);
+    }
+    if (__ballot(odd != 0)) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        u32x4 b = v.value(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          b[j] = ((b[j] & kInf) == kInf ? kOne : 0u) | ((b[j] & (kInf << 16)) == kInf << 16 ? kOne << 16 : 0u);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          const f32x4 n = mfma<KIND>(b, before(limit[f], kOne), f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (n[e] > 0.f) acc[f][i][e] = __builtin_nanf("");
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < Frag<KIND, D>::N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v.w[i][j] &= ~strange(v.w[i][j]);
+    }
+  }
+
   // weights times values
-  LANES_INL void add(const Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
+  LANES_INL void add(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
+    if (g.some) sift(v, g, limit, lane);
     u32x4 pw[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) pw[f][i] = pack2<KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16>(w[f][2 * i], w[f][2 * i + 1]);
-    if (!g.some) {
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const u32x4 b = v.value(i);
-#pragma unroll
-        for (int f = 0; f < MF; ++f) acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
-      }
-      return;
-    }
-    // Values past the last token that any row sees are zeros.  One that is not finite must not reach
-    // the rows that do not see it (0 * inf): it is zero in the products, and rows become
-    // NaN where a second product, of ones, counts such values among the tokens they see.
-    constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
-    auto before = [&](int lim, uint32_t what) {  // `what` in the halves of the tokens before a limit
-      u32x4 m;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = 4 * (lane >> 4) + 2 * (i & 1) + 16 * (i >> 1);
-        m[i] = (t < lim ? what : 0u) | (t + 1 < lim ? what << 16 : 0u);
-      }
-      return m;
-    };
-    const u32x4 any = before(g.most, 0xffffu);
-    u32x4 sees[MF];
-#pragma unroll
-    for (int f = 0; f < MF; ++f) sees[f] = before(limit[f], kOne);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      u32x4 b = v.value(i) & any, odd;
+      const u32x4 b = v.value(i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t m = ((b[j] & kInf) == kInf ? 0xffffu : 0u) | ((b[j] & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
-        odd[j] = m & (kOne | kOne << 16);
-        b[j] &= ~m;
-      }
-#pragma unroll
-      for (int f = 0; f < MF; ++f) {
-        const f32x4 n = mfma<KIND>(odd, sees[f], f32x4{0.f, 0.f, 0.f, 0.f}), o = mfma<KIND>(b, pw[f], acc[f][i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[f][i][e] = n[e] > 0.f ? __builtin_nanf("") : o[e];
-      }
+      for (int f = 0; f < MF; ++f) acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
     }
   }
 };
