@@ -398,12 +398,12 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  * length past prefix_len + width * page_size those of its sequence.  What lies in
  * the cache past a query's last token does not reach it, whatever it is.  A query with
  * NaN or inf, and a seen key or value row that is not finite, may make the outputs that depend
- * on it NaN or inf.  Scores, weights and sums are fp32; weights are rounded to fp16 (bf16 with
- * a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
+ * on it NaN or inf.  Scores, weights and sums are fp32; weights are rounded to fp16 (two bf16
+ * parts with a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
  * value's scale is in them (scales below 2^-80 count for less).
  * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
  * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^26,
- * batch * heads * ceil(n_q * q_heads / heads / 16) * width * page_size < 2^36 (UNSUPPORTED beyond).  scale finite, 0 <= softcap finite.  q and out 2-byte
+ * batch * heads * ceil(n_q * q_heads / heads / 16) * (width * page_size + 1024) < 2^36 (UNSUPPORTED beyond).  scale finite, 0 <= softcap finite.  q and out 2-byte
  * aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
  * each other or the inputs.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.  */
 MXMOE_API mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, int64_t ldq, int32_t batch,

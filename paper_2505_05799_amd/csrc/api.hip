@@ -808,9 +808,9 @@ mxmoe_status check_attention(const mxmoe_kv_cache& c, int32_t batch, int32_t n_q
   if (n_q > MXMOE_ATTENTION_QUERIES || batch > 65535 || q_heads > 65536 || (int64_t)batch * n_q * q_heads >= (1 << 26) ||
       (int64_t)width * c.page_size + prefix_len > (1 << 30))
     return MXMOE_ERR_UNSUPPORTED;
-  // blocks of 32 tokens by kv head and 16 query rows: numbered with 32 bits
+  // the kernels number blocks of 32 tokens (and some more for each 16 query rows of a kv head) with 32 bits
   const int64_t items = (int64_t)batch * c.heads * (((int64_t)n_q * (q_heads / c.heads) + 15) / 16);
-  if (items * ((int64_t)width * c.page_size / 32) >= (1LL << 31)) return MXMOE_ERR_UNSUPPORTED;
+  if (items * ((int64_t)width * c.page_size / 32 + 32) >= (1LL << 31)) return MXMOE_ERR_UNSUPPORTED;
   return MXMOE_OK;
 }
 AttnArgs attention_args(const mxmoe_kv_cache& c, int32_t batch, int32_t n_q, int32_t q_heads, int32_t width, int32_t prefix_len) {

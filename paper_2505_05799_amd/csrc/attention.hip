@@ -14,8 +14,9 @@
 // key's scale multiplies its score.  A value's scale multiplies its weight, and the reference
 // is that of the products, so that they keep 11 bits whatever the scales are; scales
 // under 2^-80 do not move it.  The sum of the weights is of fp32 values, before any rounding.
-// 16-bit rows: weights are rounded to the rows' dtype (half a step each, of random
-// sign: the sum over many tokens errs by less than the output's own rounding).
+// 16-bit rows: fp16 weights are rounded once (11 bits), a bf16 weight enters as two, the rounded
+// one and what it lacks (with one, 8 bits, the output's error was 1.4 times its own rounding's;
+// the second product costs 0.5% where memory bounds a call, 5% where it does not).
 //
 // Tokens past a row's last are left out by selection, whatever they hold: their scores
 // become -inf, their values zeros.  Where rows of a tile see different tokens and a value
@@ -32,6 +33,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// Workgroups of 4 wavefronts that a CU holds (registers)
+constexpr int cu_holds(bool wide, int mf_dim) { return wide && mf_dim >= 256 ? 1 : 2; }
 enum CacheKind { C_BF16, C_F16, C_I8, C_F8 };
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kBase = 8.f;              // weights are 2^8 at the reference ..
@@ -305,11 +308,24 @@ template <int KIND, int D, int MF> struct Rows16 {
     for (int f = 0; f < MF; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) pw[f][i] = pack2<KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16>(w[f][2 * i], w[f][2 * i + 1]);
+    u32x4 rest[KIND == C_BF16 ? MF : 1];
+    if constexpr (KIND == C_BF16) {
+#pragma unroll
+      for (int f = 0; f < MF; ++f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x2 r = unpack2<MXMOE_BF16>(pw[f][i]);
+          rest[f][i] = pack2<MXMOE_BF16>(w[f][2 * i] - r[0], w[f][2 * i + 1] - r[1]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       const u32x4 b = v.value(i);
 #pragma unroll
-      for (int f = 0; f < MF; ++f) acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
+      for (int f = 0; f < MF; ++f) {
+        acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
+        if constexpr (KIND == C_BF16) acc[f][i] = mfma<KIND>(b, rest[f], acc[f][i]);
+      }
     }
   }
 };
@@ -326,49 +342,103 @@ LANES_INL void store4(void* out, int64_t at, f32x4 o, int act) {
   *reinterpret_cast<u32x2_half*>(reinterpret_cast<uint16_t*>(out) + at) = w;
 }
 
+// Page ids and lengths: nothing writes them while a kernel runs, so that uniform ones come by
+// scalar loads, whose wait does not wait for the keys and values that are on their way
+// (as vector loads they did, once a block: 32 sequences up to 4000 tokens, 16 kv heads of 128 in bf16, 130 us against 123).
+typedef const __attribute__((address_space(4))) int32_t* Fixed;
+LANES_INL Fixed fixed(const int32_t* p) { return (Fixed)(uintptr_t)p; }
+
 // Blocks of 32 tokens of a sequence's own pages (0 for a length past its table: its
 // queries are NaN, which the joining launch writes).
 LANES_INL int own_blocks(const AttnArgs& a, int b) {
-  const int own = a.lengths[b] - a.prefix_len;
+  const int own = fixed(a.lengths)[b] - a.prefix_len;
   return own <= 0 || own > a.width << a.page_log2 ? 0 : (own + 31) >> 5;
 }
 
-// Sequences' own pages.  The blocks of all items (sequence, row block, kv head) form one list,
-// which the wavefronts share evenly: each takes `per` blocks in a row, across items as they come,
-// on its own (no barrier).  An item within a wavefront's share is finished there; pieces of
-// others go to the workspace: slot 2 g of wavefront g for a piece that continues an item,
-// 2 g + 1 for one that begins one.  The next block's keys are asked for when this one's
-// have made their scores, its values when this one's are added, in the same registers.
-template <int KIND, int D, int MF>
-__global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_kernel(AttnArgs a) {
+// 16 rows of a fragment that the wavefronts of a workgroup have summed, each over its blocks, joined
+// through LDS: red [W][live][D + 4] (rows 4 banks apart) and a flag for each wavefront that has
+// seen a block.  Every thread of the workgroup calls it; done(row, element, sums, weight,
+// reference) gets 4 elements at a time.
+template <int KIND, int D, int MF, int W, class F>
+LANES_INL void meet(const Rows16<KIND, D, MF>& x, int f, int live, bool has, float* red, int* flag, int w, int lane, F done) {
   constexpr int RS = D + 4;
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, qd = lane >> 4;
-  const int wave = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, qd = lane >> 4;
+  const float s = quarters_sum(x.sum[f]);
+  __syncthreads();  // what was there is read
+  if (lane == 0) flag[w] = has;
+  if (has && n < live) {
+    float* row = red + (w * live + n) * RS;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(row + 16 * e + 4 * qd) = x.acc[f][e];
+    if (qd == 0) {
+      row[D] = x.ref[f];
+      row[D + 1] = s;
+    }
+  }
+  __syncthreads();
+  for (int o = w * 64 + lane; o < live * (D / 4); o += 64 * W) {
+    const int r = o / (D / 4), d = 4 * (o % (D / 4));
+    float top = -__builtin_inff(), l = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (flag[j]) top = fmaxf(top, red[(j * live + r) * RS + D]);
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+      if (flag[j]) {
+        const float* row = red + (j * live + r) * RS;
+        const float c = join_factor(row[D], top);
+        v += c * *reinterpret_cast<const f32x4*>(row + d);
+        l += c * row[D + 1];
+      }
+    done(r, d, v, l, top);
+  }
+}
+
+// What an item costs a workgroup beside its blocks (its queries, the wavefronts' meeting), in blocks.
+// us with 4, 8, 16: 64 sequences up to 8192 tokens fp8 110.6, 109.3, 110.0, 16 up to 4000 with 40
+// rows a kv head 37.7, 31.8, 28.1, one of 2000 12.8, 12.4, 14.0 (without: 123, 68, 13.0)
+constexpr uint32_t kItemCost = 8;
+LANES_INL uint32_t item_cost(int blocks) { return blocks ? blocks + kItemCost : 0u; }
+
+// Sequences' own pages.  The costs of all items (sequence, row block, kv head), kItemCost and a unit
+// for each block, form one list, which the workgroups share evenly: each takes `per` units in a
+// row, across items as they come, its wavefronts every fourth block.  An item within a share is finished there; pieces of
+// others go to the workspace: slot 2 g of workgroup g for a piece that continues an item,
+// 2 g + 1 for one that begins one.  A wavefront asks for its next block's keys when this one's
+// have made their scores, for its values when this one's are added, in the same registers, also
+// into the next item, so that they are on their way while the wavefronts meet.
+template <int KIND, int D, int MF>
+__global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attention_kernel(AttnArgs a) {
+  constexpr int RS = D + 4;
+  extern __shared__ float red[];
+  __shared__ int flag[4];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15;
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, piece_rows = min(rows, 16 * MF);
   const int per_seq = a.kv_heads * a.row_blocks;  // items of a sequence
-  // this wavefront's share: all blocks, then the sequence in which it begins
+  // this workgroup's share: all blocks, then the sequence in which it begins
   uint32_t total = 0;  // (fewer than 2^31: the host sees to it)
-  for (int b = lane; b < a.batch; b += 64) total += own_blocks(a, b);
+  for (int b = lane; b < a.batch; b += 64) total += item_cost(own_blocks(a, b));
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d, 64);
   total = __builtin_amdgcn_readfirstlane(total * per_seq);
-  const uint32_t waves = gridDim.x * 4, per = max(1u, (total + waves - 1) / waves);
-  const uint32_t at0 = min(total, per * wave);
-  int left = (int)min(total - at0, per);  // blocks of the share
-  if (left <= 0 && wave) return;
+  const uint32_t per = max(4u + kItemCost, (total + gridDim.x - 1) / gridDim.x);
+  const uint32_t at0 = min(total, per * blockIdx.x);
+  int left = (int)min(total - at0, per);  // units of the share
+  if (left <= 0 && blockIdx.x) return;
   uint32_t begin = 0;  // of the sequence, in the list
   int seq = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const int b = b0 + lane;
-    const uint32_t mine = (b < a.batch ? own_blocks(a, b) : 0) * per_seq;
+    const uint32_t mine = (b < a.batch ? item_cost(own_blocks(a, b)) : 0u) * per_seq;
     uint32_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const uint32_t o = __shfl_up(upto, d, 64);
       upto += lane >= d ? o : 0;
     }
-    if (wave == 0) {  // (the first wavefront writes all starts, others stop at their sequence)
-      if (b < a.batch) a.starts[b] = begin + upto - mine;
+    if (blockIdx.x == 0) {  // (the first workgroup writes all starts, others stop at their sequence)
+      if (w == 0 && b < a.batch) a.starts[b] = begin + upto - mine;
     } else {
       const uint64_t past = __ballot(begin + upto > at0);
       if (past) {
@@ -380,128 +450,154 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
     }
     begin += __shfl(upto, 63, 64);
   }
-  if (wave == 0) {
+  if (blockIdx.x == 0) {
     begin = 0;
     while (seq < a.batch && own_blocks(a, seq) == 0) ++seq;
-    if (lane == 0) {
+    if (tid == 0) {
       a.starts[a.batch] = total;
       a.starts[a.batch + 1] = per;
     }
     if (left <= 0) return;
   }
-  struct Place { int seq, item, i, blocks, h; };  // i: the block in hand of the item's blocks
-  Place c;
-  c.seq = __builtin_amdgcn_readfirstlane(seq);
-  c.blocks = own_blocks(a, c.seq);
+  // item: of the sequence; i: a block of the item's
+  struct Place { int seq, item, i, blocks, h; };
+  auto next_item = [&](Place& p) {
+    if (++p.item == per_seq) {
+      p.item = 0;
+      do ++p.seq;
+      while ((p.blocks = own_blocks(a, p.seq)) == 0);
+    }
+    p.h = p.item % a.kv_heads;
+  };
+  Place s;  // the item in hand, i its first block in this share
+  s.seq = __builtin_amdgcn_readfirstlane(seq);
+  s.blocks = own_blocks(a, s.seq);
   {
-    const uint32_t in = __builtin_amdgcn_readfirstlane(at0 - begin);
-    c.item = in / c.blocks;
-    c.i = in - c.item * c.blocks;
-    c.h = c.item % a.kv_heads;
+    const uint32_t in = __builtin_amdgcn_readfirstlane(at0 - begin), cost = item_cost(s.blocks);
+    s.item = in / cost;
+    s.i = (int)(in - s.item * cost) - (int)kItemCost;
+    s.h = s.item % a.kv_heads;
   }
-  auto page_of = [&](const Place& p) { return a.table[(int64_t)p.seq * a.width + ((32 * p.i) >> a.page_log2)]; };
+  // (a share may end before an item's first block, or begin there: s.i < 0 units are its cost)
+  auto blocks_of = [&](const Place& p, int units) { return min(p.blocks, p.i + units); };  // end of the share's
+  auto page_of = [&](const Place& p) { return fixed(a.table)[(int64_t)p.seq * a.width + ((32 * p.i) >> a.page_log2)]; };
   auto token_of = [&](const Place& p, int id) {
     const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + p.h;
     return (rec << a.page_log2) + ((32 * p.i) & ((1 << a.page_log2) - 1));
   };
   Rows16<KIND, D, MF> x;
   Frag<KIND, D> k, v;
-  int id = page_of(c);
-  {
+  // c: the wavefront's next block, whose keys and values are on their way; ahead: units of the
+  // share from c's item's place on (s.i as that item begins in the share)
+  Place c = s;
+  int ahead = left, id = 0, turn = w;  // turn: blocks to let pass
+  bool mine = true;
+  auto seek = [&]() {  // to the block `turn` further on, if the share has it
+    while (true) {
+      const int from = max(c.i, 0), end = blocks_of(c, ahead);
+      if (from + turn < end) {
+        ahead -= from + turn - c.i;
+        c.i = from + turn;
+        turn = 0;
+        return;
+      }
+      turn -= max(end - from, 0);
+      ahead -= c.blocks - c.i;
+      if (ahead <= (int)kItemCost) {
+        mine = false;
+        return;
+      }
+      next_item(c);
+      c.i = -(int)kItemCost;
+    }
+  };
+  seek();
+  if (mine) {
+    id = page_of(c);
     const int64_t t = token_of(c, id);
     k.load(a.ck, a.cks, t, lane);
     v.load(a.cv, a.cvs, t, lane);
   }
-  int seen[MF], least = 0, most = 0, first = 0;
-  bool fresh = true;
   while (true) {
-    if (fresh) {  // an item begins here, for this wavefront
-      const int rb = c.item / a.kv_heads, own = a.lengths[c.seq] - a.prefix_len - a.n_q + 1;
+    const int first = max(s.i, 0), last = blocks_of(s, left);
+    const int rb = s.item / a.kv_heads, own = fixed(a.lengths)[s.seq] - a.prefix_len - a.n_q + 1;
+    if (first < last) {
+      const bool has = mine && c.seq == s.seq && c.item == s.item;
       x.clear();
+      if (has) {
+        int seen[MF];
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          const int r = 16 * (MF * rb + f) + n, j = r / group;
+          const bool live = r < rows;
+          x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)s.seq * a.n_q + j) * a.ldq + ((int64_t)s.h * group + r % group) * D : nullptr, lane);
+          seen[f] = live ? own + j : 0;
+        }
+        const int least = own + 16 * MF * rb / group, most = own + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
+        bool here = true;
+        while (here) {
+          const int i = c.i;
+          turn = 4;
+          seek();
+          here = mine && c.seq == s.seq && c.item == s.item;
+          const int next_id = mine ? page_of(c) : 0;
+          const int64_t next = token_of(c, next_id);
+          x.scores(k);
+          if (mine) k.load(a.ck, a.cks, next, lane);
+          Sight g;
+          g.bad = (unsigned)id >= (unsigned)a.n_pages;
+          g.least = least - 32 * i;
+          g.most = most - 32 * i;
+          g.some = g.bad || g.least < 32;
+          int limit[MF];
+#pragma unroll
+          for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+          x.weigh(a, v, g, limit, lane);
+          x.add(v, g, limit, lane);
+          if (mine) v.load(a.cv, a.cvs, next, lane);
+          id = next_id;
+        }
+      }
+      const bool whole = first == 0 && last == s.blocks;
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
-        const int r = 16 * (MF * rb + f) + n, j = r / group;
-        const bool live = r < rows;
-        x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)c.seq * a.n_q + j) * a.ldq + ((int64_t)c.h * group + r % group) * D : nullptr, lane);
-        seen[f] = live ? own + j : 0;
-      }
-      least = own + 16 * MF * rb / group;
-      most = own + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
-      first = c.i;
-    }
-    Place o = c;  // the next block
-    const bool more = --left > 0;
-    ++o.i;
-    fresh = o.i == c.blocks;
-    if (more && fresh) {
-      o.i = 0;
-      ++o.item;
-      if (o.item == per_seq) {
-        o.item = 0;
-        do ++o.seq;
-        while ((o.blocks = own_blocks(a, o.seq)) == 0);
-      }
-      o.h = o.item % a.kv_heads;
-    }
-    const int next_id = more ? page_of(o) : 0;
-    const int64_t next = token_of(o, next_id);
-    x.scores(k);
-    if (more) k.load(a.ck, a.cks, next, lane);
-    Sight g;
-    g.bad = (unsigned)id >= (unsigned)a.n_pages;
-    g.least = least - 32 * c.i;
-    g.most = most - 32 * c.i;
-    g.some = g.bad || g.least < 32;
-    int limit[MF];
-#pragma unroll
-    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * c.i;
-    x.weigh(a, v, g, limit, lane);
-    x.add(v, g, limit, lane);
-    if (more) v.load(a.cv, a.cvs, next, lane);
-    if (fresh || !more) {
-      const bool whole = first == 0 && fresh;
-      const int rb = c.item / a.kv_heads;
-#pragma unroll
-      for (int f = 0; f < MF; ++f) {
-        const float l = quarters_sum(x.sum[f]);
-        const int pr = 16 * f + n, row = 16 * MF * rb + pr, q = row / group;
-        if (row < rows) {
-          const int64_t tok = (int64_t)c.seq * a.n_q + q, head = (int64_t)c.h * group + row % group;
+        const int r0 = 16 * (MF * rb + f);
+        meet<KIND, D, MF, 4>(x, f, min(16, rows - r0), has, red, flag, w, lane, [&](int r, int d, f32x4 v4, float l, float top) {
+          const int row = r0 + r, q = row / group;
+          const int64_t tok = (int64_t)s.seq * a.n_q + q, head = (int64_t)s.h * group + row % group;
           if (whole && !a.prefix_len) {
-            const float m = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e) store4(a.out, tok * a.ldo + head * D + 16 * e + 4 * qd, x.acc[f][e] * m, a.act);
+            store4(a.out, tok * a.ldo + head * D + d, v4 * (l == 0.f ? 0.f : 1.f / l), a.act);
           } else {
             float* part = whole ? a.own + (tok * a.q_heads + head) * RS
-                                : a.part + ((2 * (int64_t)wave + (first == 0)) * piece_rows + pr) * RS;
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(part + 16 * e + 4 * qd) = x.acc[f][e];
-            if (qd == 0) {
-              part[D] = x.ref[f];
+                                : a.part + ((2 * (int64_t)blockIdx.x + (first == 0)) * piece_rows + 16 * f + r) * RS;
+            *reinterpret_cast<f32x4*>(part + d) = v4;
+            if (d == 0) {
+              part[D] = top;
               part[D + 1] = l;
             }
           }
-        }
+        });
       }
-      if (!more) break;
     }
-    c = o;
-    id = next_id;
+    left -= s.blocks - s.i;
+    if (left <= (int)kItemCost) break;
+    next_item(s);
+    s.i = -(int)kItemCost;
   }
 }
 
 // Items of few blocks: a workgroup of W wavefronts takes an item, its wavefronts every Wth
 // block, and they meet in LDS: one launch, nothing in the workspace (but with a prefix).
 template <int KIND, int D, int MF, int W>
-__global__ void __launch_bounds__(64 * W, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_item_kernel(AttnArgs a) {
-  constexpr int RS = D + 4;  // a row in LDS: rows 4 banks apart
-  __shared__ float red[W * 16 * RS];
-  __shared__ float stat[W][2][16];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
+__global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) attention_item_kernel(AttnArgs a) {
+  constexpr int RS = D + 4;
+  extern __shared__ float red[];
+  __shared__ int flag[W];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15;
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, per_seq = a.kv_heads * a.row_blocks;
   const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq, rb = item / a.kv_heads, h = item - rb * a.kv_heads;
-  const int length = a.lengths[seq], own = length - a.prefix_len - a.n_q + 1;
-  const int32_t* pages = a.table + (int64_t)seq * a.width;
+  const int length = fixed(a.lengths)[seq], own = length - a.prefix_len - a.n_q + 1;
+  const Fixed pages = fixed(a.table) + (int64_t)seq * a.width;
   auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
   auto token_of = [&](int i, int id) {
     const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
@@ -547,32 +643,10 @@ __global__ void __launch_bounds__(64 * W, KIND <= C_F16 && MF * D >= 256 ? 1 : 2
     i = next;
     id = next_id;
   }
-  const int used = min(W, max(1, blocks));  // wavefronts that have seen a block
 #pragma unroll
   for (int f = 0; f < MF; ++f) {
-    const int r0 = 16 * (MF * rb + f), live = min(16, rows - r0);
-    const float s = quarters_sum(x.sum[f]);
-    if (f) __syncthreads();
-    if (n < live && w < used) {
-      if (qd == 0) {
-        stat[w][0][n] = x.ref[f];
-        stat[w][1][n] = s;
-      }
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) *reinterpret_cast<f32x4*>(&red[(w * 16 + n) * RS + 16 * e + 4 * qd]) = x.acc[f][e];
-    }
-    __syncthreads();
-    for (int o = tid; o < live * (D / 4); o += 64 * W) {
-      const int r = o / (D / 4), d = 4 * (o % (D / 4));
-      float top = stat[0][0][r];
-      for (int j = 1; j < used; ++j) top = fmaxf(top, stat[j][0][r]);
-      f32x4 v4 = {0.f, 0.f, 0.f, 0.f};
-      float l = 0.f;
-      for (int j = 0; j < used; ++j) {
-        const float c = join_factor(stat[j][0][r], top);
-        v4 += c * *reinterpret_cast<const f32x4*>(&red[(j * 16 + r) * RS + d]);
-        l += c * stat[j][1][r];
-      }
+    const int r0 = 16 * (MF * rb + f);
+    meet<KIND, D, MF, W>(x, f, min(16, rows - r0), w < blocks, red, flag, w, lane, [&](int r, int d, f32x4 v4, float l, float top) {
       const int row = r0 + r, q = row / group;
       const int64_t tok = (int64_t)seq * a.n_q + q, head = (int64_t)h * group + row % group;
       if (!a.prefix_len) {
@@ -585,7 +659,7 @@ __global__ void __launch_bounds__(64 * W, KIND <= C_F16 && MF * D >= 256 ? 1 : 2
           part[D + 1] = l;
         }
       }
-    }
+    });
   }
 }
 
@@ -593,7 +667,7 @@ __global__ void __launch_bounds__(64 * W, KIND <= C_F16 && MF * D >= 256 ? 1 : 2
 // head side by side) against it.  A workgroup takes one share of the prefix's blocks, its
 // wavefronts 16 MF rows each.
 template <int KIND, int D, int MF>
-__global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) attention_prefix_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attention_prefix_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
   const int group = a.q_heads / a.kv_heads, rows = a.batch * a.n_q * group;
@@ -630,13 +704,13 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   Frag<KIND, D> k, v;
   int id = 0;
   if (first < end) {
-    id = a.prefix[(32 * first) >> a.page_log2];
+    id = fixed(a.prefix)[(32 * first) >> a.page_log2];
     const int64_t t = token_of(first, id);
     k.load(a.ck, a.cks, t, lane);
     v.load(a.cv, a.cvs, t, lane);
   }
   for (int i = first; i < end; ++i) {
-    const int next_id = i + 1 < end ? a.prefix[(32 * (i + 1)) >> a.page_log2] : 0;
+    const int next_id = i + 1 < end ? fixed(a.prefix)[(32 * (i + 1)) >> a.page_log2] : 0;
     x.scores(k);
     if (i + 1 < end) k.load(a.ck, a.cks, token_of(i + 1, next_id), lane);
     Sight g;
@@ -668,7 +742,7 @@ __global__ void __launch_bounds__(256, KIND <= C_F16 && MF * D >= 256 ? 1 : 2) a
   }
 }
 
-// Pieces of a query row joined: of the prefix's shares, of the wavefronts that shared its
+// Pieces of a query row joined: of the prefix's shares, of the workgroups that shared its
 // item.  D / 4 lanes hold a row; GP groups of them take the pieces of one row in turn, four at
 // a time, and meet in LDS.
 template <int D, int GP>
@@ -683,12 +757,12 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
   const int head = rank - (int)tok * a.q_heads, b = (int)tok / a.n_q, h = head / group;
   const int row = ((int)tok - b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
   const int piece_rows = min(a.n_q * group, frag_rows);
-  const int length = a.lengths[b];
+  const int length = fixed(a.lengths)[b];
   const int blocks = own_blocks(a, b);
   uint32_t g0 = 0;
   int pieces = blocks > 0;  // of the item
   if (!a.direct && blocks) {
-    const uint32_t per = a.starts[a.batch + 1], s0 = a.starts[b] + (rb * a.kv_heads + h) * blocks;
+    const uint32_t per = a.starts[a.batch + 1], s0 = a.starts[b] + (rb * a.kv_heads + h) * item_cost(blocks) + kItemCost;
     g0 = s0 / per;
     pieces = (int)((s0 + blocks - 1) / per - g0) + 1;
   }
@@ -752,16 +826,18 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
   store4(a.out, tok * a.ldo + (int64_t)head * D + d, v * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
 }
 
-constexpr int kGrid = 512;
 
 // Fragments of 16 rows that a wavefront takes
 int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : rows <= 32 || dim == 128 ? 2 : 4; }
 
-// Wavefronts to an item, or 0 where the list of blocks is shared
-int direct_of(int64_t items, int64_t most) {
-  if (most <= 64 && items <= 256) return 8;
-  if (most <= 16) return 4;
-  return 0;
+// Wavefronts to an item, or 0 where the list of costs is shared.  An item to a workgroup is one launch
+// and needs no search for its place; from 64 blocks on its length is what the launch waits for, and
+// few long items leave CUs idle.  us with 4 wavefronts to an item, 8, shared (int8, dim 128, 4 rows; sequences of
+// 3/4 to all of the length): 8 items of 4 blocks 4.6, 4.4, 9.0; 8 of 63 16.1, 13.7, 11.6; 128 of 63 19.4, 15.9,
+// 21.0; 512 of 4 6.8, 8.9, 13.0; 512 of 63 46.4, 47.6, 56.3; 2048 of 16 50.6, 62.8, 65.0
+int direct_of(int64_t items, int64_t longest) {
+  if (longest > 64 || (longest > 48 && items < 16)) return 0;
+  return items <= 256 ? 8 : 4;
 }
 
 struct Plan { int direct, frags, row_blocks, pre_frags, shares, grid, pieces; size_t starts, part, own, pre, total; };
@@ -773,7 +849,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_blocks, longest = ((int64_t)a.width << a.page_log2) / 32, most = items * longest;
   p.direct = direct_of(items, longest);
-  p.grid = (int)std::min<int64_t>(kGrid, std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront at least
+  p.grid = (int)std::min<int64_t>(256 * cu_holds(a.qmax == 0, p.frags * dim), std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront
   if (a.prefix_len) {
     const int64_t prows = (int64_t)a.batch * rows;
     p.pre_frags = frags_of(prows, dim);
@@ -782,19 +858,23 @@ Plan plan_of(const AttnArgs& a, int dim) {
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((blocks + 3) / 4, 64), 512 / wgs));
   }
   // pieces of a row at the most, if all sequences are as long as the table allows
-  p.pieces = p.shares + 1 + (p.direct ? 0 : (int)(4 * (int64_t)p.grid / items));
+  p.pieces = p.shares + 1 + (p.direct ? 0 : (int)(p.grid / items));
   auto align = [](size_t n) { return (n + 255) / 256 * 256; };
   size_t o = 0;
   p.starts = o; o = align(o + (p.direct ? 0 : 4 * ((size_t)a.batch + 2)));
-  p.part = o; o = align(o + (p.direct ? 0 : 8) * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
+  p.part = o; o = align(o + (p.direct ? 0 : 2) * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
   p.own = o; o = align(o + (a.prefix_len ? (size_t)all * rs : 0));
   p.pre = o; o = align(o + (size_t)p.shares * all * rs);
   p.total = o;
   return p;
 }
 
+// LDS of meet
+size_t meet_bytes(const AttnArgs& a, int dim, int w) { return 4 * (size_t)w * std::min(16, a.n_q * (a.q_heads / a.kv_heads)) * (dim + 4); }
+
 template <int KIND, int D, int MF, int W> hipError_t go_item(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  hipLaunchKernelGGL((attention_item_kernel<KIND, D, MF, W>), dim3((unsigned)(a.batch * a.kv_heads * p.row_blocks)), dim3(64 * W), 0, s, a);
+  hipLaunchKernelGGL((attention_item_kernel<KIND, D, MF, W>), dim3((unsigned)(a.batch * a.kv_heads * p.row_blocks)), dim3(64 * W),
+                     meet_bytes(a, D, W), s, a);
   return hipGetLastError();
 }
 template <int KIND, int D, int MF> hipError_t go_own(const AttnArgs& a, const Plan& p, hipStream_t s) {
@@ -803,7 +883,7 @@ template <int KIND, int D, int MF> hipError_t go_own(const AttnArgs& a, const Pl
       if (p.direct == 8) return go_item<KIND, D, MF, 8>(a, p, s);
     return go_item<KIND, D, MF, 4>(a, p, s);
   }
-  hipLaunchKernelGGL((attention_kernel<KIND, D, MF>), dim3(p.grid), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((attention_kernel<KIND, D, MF>), dim3(p.grid), dim3(256), meet_bytes(a, D, 4), s, a);
   return hipGetLastError();
 }
 template <int KIND, int D, int MF> hipError_t go_prefix(const AttnArgs& a, hipStream_t s) {
