@@ -38,7 +38,7 @@ constexpr int cu_holds(bool wide, int mf_dim) { return wide && mf_dim >= 256 ? 1
 enum CacheKind { C_BF16, C_F16, C_I8, C_F8 };
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kBase = 8.f;              // weights are 2^8 at the reference ..
-constexpr float kMostWeight = 0x1p15f;    // .. and move it past 2^15 (fp16 ends at 2^16)
+constexpr uint32_t kMostF16 = 0x7800u, kMostBf16 = 0x4700u;  // .. and move it past 2^15 (fp16 ends at 2^16)
 constexpr float kLeastScale = 0x1p-80f;
 
 template <int KIND> LANES_INL f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -114,7 +114,8 @@ template <int KIND, int D, int MF> struct Rows16 {
   f32x4 acc[MF][D / 16];   // elements 16 i + 4 (lane / 16) + (0..3)
   float ref[MF], sum[MF];  // the row's reference, the sum of its weights (this lane's tokens)
   float mul[MF];           // from a product of codes to a score: in powers of 2, or (with a cap) parts of the cap
-  float w[MF][8];          // scores, then weights of the block in hand
+  float w[MF][8];          // products, then weights of the block in hand
+  u32x4 pw[MF];            // weights as the second product takes them
 
   LANES_INL void clear() {
 #pragma unroll
@@ -143,20 +144,19 @@ template <int KIND, int D, int MF> struct Rows16 {
       b = max2(b, (uint32_t)__shfl_xor((int)b, 32, 64));
       const int e = (int)(max(b & 0xffffu, b >> 16) >> 7);  // exponent of the largest
       const int up = e == 255 ? 0 : min(127, 127 + 14 - max(e, 1));
+      auto turned = [&](uint32_t b) {
+        const f32x2 v = unpack2<MXMOE_BF16>(b);
+        return pack2<MXMOE_F16>(__builtin_ldexpf(v[0], up), __builtin_ldexpf(v[1], up));
+      };
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 v = unpack2<MXMOE_BF16>(q[f][s][i]);
-          q[f][s][i] = pack2<MXMOE_F16>(__builtin_ldexpf(v[0], up), __builtin_ldexpf(v[1], up));
-        }
+      for (int s = 0; s < D / 32; ++s) q[f][s] = u32x4{turned(q[f][s][0]), turned(q[f][s][1]), turned(q[f][s][2]), turned(q[f][s][3])};
       m = __builtin_ldexpf(m, -up);
     }
     mul[f] = a.softcap > 0.f ? m / a.softcap : m * kLog2e;
   }
 
-  // products of the rows and 32 keys
-  LANES_INL void scores(const Frag<KIND, D>& k) {
+  // products of the rows and 32 keys: 16 keys of a tile, 32 elements of a step at a time
+  template <class K> LANES_INL void scores(K key) {
     f32x4 s[MF][2];
 #pragma unroll
     for (int f = 0; f < MF; ++f) s[f][0] = s[f][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -164,69 +164,69 @@ template <int KIND, int D, int MF> struct Rows16 {
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const u32x4 b = k.key(t, i);
+        const u32x4 b = key(t, i);
 #pragma unroll
         for (int f = 0; f < MF; ++f) s[f][t] = mfma<KIND>(b, q[f][i], s[f][t]);
       }
 #pragma unroll
     for (int f = 0; f < MF; ++f)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[f][i] = s[f][i >> 2][i & 3] * mul[f];
-        if constexpr (ES == 1) w[f][i] *= k.s[i >> 2][i & 3];
-      }
+      for (int i = 0; i < 8; ++i) w[f][i] = s[f][i >> 2][i & 3];
   }
 
-  // weights of the 32 tokens, sums and references; limit: how many of them a row sees
-  LANES_INL void weigh(const AttnArgs& a, const Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
-    float vs[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if constexpr (ES == 1) vs[i] = v.s[i >> 2][i & 3]; else vs[i] = 1.f;
+  // weights of the 32 tokens, sums and references; ks, vs: the tokens' scales, limit: how many of
+  // the tokens a row sees
+  LANES_INL void weigh(const AttnArgs& a, const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Sight& g, const int (&limit)[MF], int lane) {
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
       float x[8], p[8], s[8];
+      float m = mul[f];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = w[f][i];
-        s[i] = vs[i];
+        x[i] = ES == 1 ? w[f][i] * ks[i >> 2][i & 3] : w[f][i];
+        s[i] = ES == 1 ? vs[i >> 2][i & 3] : 1.f;
       }
       if (a.softcap > 0.f) {
         const float c = a.softcap * kLog2e;
 #pragma unroll
         for (int i = 0; i < 8; ++i)  // tanh y = 1 - 2 / (1 + e^(2 y))
-          x[i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * (2.f * kLog2e)));
+          x[i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * m * (2.f * kLog2e)));
+        m = 1.f;
       }
       if (g.some) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const bool in = 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f];
-          x[i] = in ? (g.bad ? __builtin_nanf("") : x[i]) : -__builtin_inff();
+          x[i] = in ? (g.bad ? __builtin_nanf("") : x[i] * m) : -__builtin_inff();
           s[i] = in ? s[i] : 0.f;
         }
+        m = 1.f;
       }
       auto weights = [&](float r) {
-        float top = 0.f;
         const float off = kBase - (r == -__builtin_inff() ? 0.f : r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(x[i] + off);
+          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], m, off));
           w[f][i] = ES == 1 ? p[i] * s[i] : p[i];
-          top = fmaxf(top, w[f][i]);
         }
-        return top;
+        constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
+        const u32x4 o = {pack2<P>(w[f][0], w[f][1]), pack2<P>(w[f][2], w[f][3]), pack2<P>(w[f][4], w[f][5]), pack2<P>(w[f][6], w[f][7])};
+        pw[f] = o;
+        const uint32_t top = max2(max2(o[0], o[1]), max2(o[2], o[3]));
+        return max(top & 0xffffu, top >> 16);
       };
-      bool move = weights(ref[f]) > kMostWeight;
+      // (weights are not negative: the order of their bits is theirs, and inf and NaN come last)
+      bool move = weights(ref[f]) > (KIND == C_BF16 ? kMostBf16 : kMostF16);
       if (ref[f] == -__builtin_inff()) {  // a row without a reference takes one from its first tokens
 #pragma unroll
-        for (int i = 0; i < 8; ++i) move |= x[i] > -__builtin_inff();
+        for (int i = 0; i < 8; ++i) move |= x[i] * m > -__builtin_inff();
       }
       if (__ballot(move)) {
-        float m = -__builtin_inff();
+        float r = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          m = fmaxf(m, x[i] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(s[i], kLeastScale)) : 0.f));
-        const float next = fmaxf(ref[f], quarters_max(m));
+          r = fmaxf(r, x[i] * m + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(s[i], kLeastScale)) : 0.f));
+        const float next = fmaxf(ref[f], quarters_max(r));
         const float d = ref[f] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref[f] - next);  // (nothing summed yet)
         ref[f] = next;
         sum[f] *= d;
@@ -239,37 +239,43 @@ template <int KIND, int D, int MF> struct Rows16 {
     }
   }
 
+  // `what` in the 16-bit halves of the lane's tokens that come before a limit
+  static LANES_INL u32x4 before(int lim, uint32_t what, int lane) {
+    auto half = [&](int i) {
+      const int t = 4 * (lane >> 4) + 2 * (i & 1) + 16 * (i >> 1);
+      return (t < lim ? what : 0u) | (t + 1 < lim ? what << 16 : 0u);
+    };
+    const u32x4 m = {half(0), half(1), half(2), half(3)};
+    return m;
+  }
+  static constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
+  // ones in the halves that are not finite.  (Fragments are changed whole: element by element, hipcc
+  // (clang 22, ROCm 7.2) has given a part of one's registers to other values while it was in use.)
+  static LANES_INL uint32_t odd_half(uint32_t w) {
+    return ((w & kInf) == kInf ? 0xffffu : 0u) | ((w & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
+  }
+  static LANES_INL u32x4 odd_halves(u32x4 v) { return u32x4{odd_half(v[0]), odd_half(v[1]), odd_half(v[2]), odd_half(v[3])}; }
+
   // Values for rows that do not see all of them.  Past the last token that any row sees they are
   // zeros.  One that is not finite must not reach the rows that do not see it (0 * inf): it
   // becomes zero, and rows become NaN where a product of ones counts such values among
   // the tokens they see.
   LANES_INL void sift(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
     if constexpr (KIND == C_I8) return;  // (every code is finite, the weights of what is not seen are 0)
-    constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
-    const int t0 = 4 * (lane >> 4);
-    auto before = [&](int lim, uint32_t what) {  // `what` in the halves of the tokens before a limit
-      u32x4 m;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + 2 * (i & 1) + 16 * (i >> 1);
-        m[i] = (t < lim ? what : 0u) | (t + 1 < lim ? what << 16 : 0u);
-      }
-      return m;
-    };
     auto strange = [&](uint32_t w) -> uint32_t {  // ones where a value is not finite
-      if constexpr (ES == 2) return ((w & kInf) == kInf ? 0xffffu : 0u) | ((w & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
+      if constexpr (ES == 2) return odd_half(w);
       const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f, 0xff
       return (top >> 7) * 0xffu;
     };
     u32x4 any;
     if constexpr (ES == 2) {
-      any = before(g.most, 0xffffu);
+      any = before(g.most, 0xffffu, lane);
     } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int t = t0 + 16 * (i & 1);
-        any[i] = (t < g.most ? 0xffu : 0u) | (t + 1 < g.most ? 0xff00u : 0u) | (t + 2 < g.most ? 0xff0000u : 0u) | (t + 3 < g.most ? 0xff000000u : 0u);
-      }
+      auto four = [&](int t) {
+        return (t < g.most ? 0xffu : 0u) | (t + 1 < g.most ? 0xff00u : 0u) | (t + 2 < g.most ? 0xff0000u : 0u) | (t + 3 < g.most ? 0xff000000u : 0u);
+      };
+      const uint32_t lo = four(4 * (lane >> 4)), hi = four(4 * (lane >> 4) + 16);
+      any = u32x4{lo, hi, lo, hi};
     }
     uint32_t odd = 0u;
 #pragma unroll
@@ -280,53 +286,61 @@ template <int KIND, int D, int MF> struct Rows16 {
     }
     if (__ballot(odd != 0)) {
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        u32x4 b = v.value(i);
+      for (int i = 0; i < D / 16; ++i) count(v.value(i), i, limit, lane);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          b[j] = ((b[j] & kInf) == kInf ? kOne : 0u) | ((b[j] & (kInf << 16)) == kInf << 16 ? kOne << 16 : 0u);
-#pragma unroll
-        for (int f = 0; f < MF; ++f) {
-          const f32x4 n = mfma<KIND>(b, before(limit[f], kOne), f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n[e] > 0.f) acc[f][i][e] = __builtin_nanf("");
-        }
+      for (int i = 0; i < Frag<KIND, D>::N; ++i) {
+        const u32x4 o = v.w[i];
+        v.w[i] = o & ~u32x4{strange(o[0]), strange(o[1]), strange(o[2]), strange(o[3])};
       }
+    }
+  }
+  // NaN for the rows that see a value of tile i that is not finite
+  LANES_INL void count(u32x4 b, int i, const int (&limit)[MF], int lane) {
+    b = odd_halves(b) & (kOne | kOne << 16);
+    constexpr float nan = __builtin_nanf("");
 #pragma unroll
-      for (int i = 0; i < Frag<KIND, D>::N; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v.w[i][j] &= ~strange(v.w[i][j]);
+    for (int f = 0; f < MF; ++f) {
+      const f32x4 n = mfma<KIND>(b, before(limit[f], kOne, lane), f32x4{0.f, 0.f, 0.f, 0.f}), o = acc[f][i];
+      acc[f][i] = f32x4{n[0] > 0.f ? nan : o[0], n[1] > 0.f ? nan : o[1], n[2] > 0.f ? nan : o[2], n[3] > 0.f ? nan : o[3]};
     }
   }
 
-  // weights times values
-  LANES_INL void add(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
-    if (g.some) sift(v, g, limit, lane);
-    u32x4 pw[MF];
-#pragma unroll
-    for (int f = 0; f < MF; ++f)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pw[f][i] = pack2<KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16>(w[f][2 * i], w[f][2 * i + 1]);
+  // weights times values, 16 elements of a tile at a time
+  template <class V> LANES_INL void add(V value) {
     u32x4 rest[KIND == C_BF16 ? MF : 1];
     if constexpr (KIND == C_BF16) {
 #pragma unroll
-      for (int f = 0; f < MF; ++f)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+      for (int f = 0; f < MF; ++f) {
+        auto lack = [&](int i) {
           const f32x2 r = unpack2<MXMOE_BF16>(pw[f][i]);
-          rest[f][i] = pack2<MXMOE_BF16>(w[f][2 * i] - r[0], w[f][2 * i + 1] - r[1]);
-        }
+          return pack2<MXMOE_BF16>(w[f][2 * i] - r[0], w[f][2 * i + 1] - r[1]);
+        };
+        rest[f] = u32x4{lack(0), lack(1), lack(2), lack(3)};
+      }
     }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      const u32x4 b = v.value(i);
+      const u32x4 b = value(i);
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
         if constexpr (KIND == C_BF16) acc[f][i] = mfma<KIND>(b, rest[f], acc[f][i]);
       }
     }
+  }
+
+  // a block whose keys and values the lane holds; between: what is done when the keys are used
+  template <class F>
+  LANES_INL void block(const AttnArgs& a, Frag<KIND, D>& k, Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane, F between) {
+    scores([&](int t, int i) { return k.key(t, i); });
+    f32x4 ks[2];
+    if constexpr (ES == 1) { ks[0] = k.s[0]; ks[1] = k.s[1]; }
+    between();
+    f32x4 vs[2];
+    if constexpr (ES == 1) { vs[0] = v.s[0]; vs[1] = v.s[1]; }
+    weigh(a, ks, vs, g, limit, lane);
+    if (g.some) sift(v, g, limit, lane);
+    add([&](int i) { return v.value(i); });
   }
 };
 
@@ -347,11 +361,12 @@ LANES_INL void store4(void* out, int64_t at, f32x4 o, int act) {
 // (as vector loads they did, once a block: 32 sequences up to 4000 tokens, 16 kv heads of 128 in bf16, 130 us against 123).
 typedef const __attribute__((address_space(4))) int32_t* Fixed;
 LANES_INL Fixed fixed(const int32_t* p) { return (Fixed)(uintptr_t)p; }
+LANES_INL int length_of(const AttnArgs& a, int b) { return max(0, fixed(a.lengths)[b]); }
 
 // Blocks of 32 tokens of a sequence's own pages (0 for a length past its table: its
 // queries are NaN, which the joining launch writes).
 LANES_INL int own_blocks(const AttnArgs& a, int b) {
-  const int own = fixed(a.lengths)[b] - a.prefix_len;
+  const int own = length_of(a, b) - a.prefix_len;
   return own <= 0 || own > a.width << a.page_log2 ? 0 : (own + 31) >> 5;
 }
 
@@ -520,7 +535,7 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
   }
   while (true) {
     const int first = max(s.i, 0), last = blocks_of(s, left);
-    const int rb = s.item / a.kv_heads, own = fixed(a.lengths)[s.seq] - a.prefix_len - a.n_q + 1;
+    const int rb = s.item / a.kv_heads, own = length_of(a, s.seq) - a.prefix_len - a.n_q + 1;
     if (first < last) {
       const bool has = mine && c.seq == s.seq && c.item == s.item;
       x.clear();
@@ -542,8 +557,6 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
           here = mine && c.seq == s.seq && c.item == s.item;
           const int next_id = mine ? page_of(c) : 0;
           const int64_t next = token_of(c, next_id);
-          x.scores(k);
-          if (mine) k.load(a.ck, a.cks, next, lane);
           Sight g;
           g.bad = (unsigned)id >= (unsigned)a.n_pages;
           g.least = least - 32 * i;
@@ -552,8 +565,9 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
           int limit[MF];
 #pragma unroll
           for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
-          x.weigh(a, v, g, limit, lane);
-          x.add(v, g, limit, lane);
+          x.block(a, k, v, g, limit, lane, [&]() {
+            if (mine) k.load(a.ck, a.cks, next, lane);
+          });
           if (mine) v.load(a.cv, a.cvs, next, lane);
           id = next_id;
         }
@@ -596,7 +610,7 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15;
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group, per_seq = a.kv_heads * a.row_blocks;
   const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq, rb = item / a.kv_heads, h = item - rb * a.kv_heads;
-  const int length = fixed(a.lengths)[seq], own = length - a.prefix_len - a.n_q + 1;
+  const int length = length_of(a, seq), own = length - a.prefix_len - a.n_q + 1;
   const Fixed pages = fixed(a.table) + (int64_t)seq * a.width;
   auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
   auto token_of = [&](int i, int id) {
@@ -627,8 +641,6 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
   while (i < blocks) {
     const int next = i + W;
     const int next_id = next < blocks ? page_of(next) : 0;
-    x.scores(k);
-    if (next < blocks) k.load(a.ck, a.cks, token_of(next, next_id), lane);
     Sight g;
     g.bad = (unsigned)id >= (unsigned)a.n_pages;
     g.least = least - 32 * i;
@@ -637,8 +649,9 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
     int limit[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
-    x.weigh(a, v, g, limit, lane);
-    x.add(v, g, limit, lane);
+    x.block(a, k, v, g, limit, lane, [&]() {
+      if (next < blocks) k.load(a.ck, a.cks, token_of(next, next_id), lane);
+    });
     if (next < blocks) v.load(a.cv, a.cvs, token_of(next, next_id), lane);
     i = next;
     id = next_id;
@@ -663,17 +676,34 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
   }
 }
 
+// Keys and values of a stage in LDS, as the products take them (codes widened to fp16): fragments of
+// 1 KB that a wavefront reads side by side.
+template <int KIND, int D> struct Stage {
+  static constexpr int ES = KIND <= C_F16 ? 2 : 1;
+  static constexpr int NB = D == 256 ? 1 : 2;                       // blocks of a stage
+  static constexpr int KF = NB * 2 * (D / 32), VF = NB * (D / 16);  // fragments of keys, of values
+  static constexpr int LP = NB * D * ES / 64;                       // 1 KB loads of a wavefront (keys and values)
+  u32x4 k[KF][64], v[VF][64];
+  float s[ES == 1 ? 2 : 1][NB * 32];
+};
+
 // The shared prefix: rows of all sequences (sequence by sequence, a query's heads of the kv
-// head side by side) against it.  A workgroup takes one share of the prefix's blocks, its
-// wavefronts 16 MF rows each.
+// head side by side) against it.  A workgroup takes one share of the prefix's blocks, its four
+// wavefronts 16 MF rows each; keys and values go through LDS, two stages of them, where they come
+// once for all wavefronts and codes are widened once.  Workgroups with the same blocks, for other
+// rows, have indexes 8 apart: one XCD's, so that its L2 has them.
 template <int KIND, int D, int MF>
-__global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attention_prefix_kernel(AttnArgs a) {
-  constexpr int RS = D + 4;
+__global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
+  using S = Stage<KIND, D>;
+  constexpr int RS = D + 4, ES = S::ES, NB = S::NB;
+  __shared__ S stage[2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
   const int group = a.q_heads / a.kv_heads, rows = a.batch * a.n_q * group;
-  const int h = (int)blockIdx.y, share = (int)blockIdx.z;
-  const int r0 = ((int)blockIdx.x * 4 + w) * 16 * MF;
-  if (r0 >= rows) return;
+  const int teams = (rows + 64 * MF - 1) / (64 * MF);  // workgroups with the same blocks
+  const int of8 = (int)blockIdx.x / (8 * teams), rem = (int)blockIdx.x - of8 * 8 * teams, pair = of8 * 8 + (rem & 7);
+  if (pair >= a.kv_heads * a.shares) return;
+  const int h = pair % a.kv_heads, share = pair / a.kv_heads;
+  const int r0 = ((rem >> 3) * 4 + w) * 16 * MF;
   const int blocks = (a.prefix_len + 31) >> 5;
   const int first = (int)((int64_t)blocks * share / a.shares), last = (int)((int64_t)blocks * (share + 1) / a.shares);
   Rows16<KIND, D, MF> x;
@@ -685,7 +715,7 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
     const bool live = r < rows;
     x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + tok * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
     const int b = tok / a.n_q;
-    seen[f] = live ? max(0, min(a.prefix_len, a.lengths[b] - a.n_q + 1 + tok % a.n_q)) : 0;
+    seen[f] = live ? max(0, min(a.prefix_len, length_of(a, b) - a.n_q + 1 + tok % a.n_q)) : 0;
     most = max(most, seen[f]);
     least = min(least, live ? seen[f] : 1 << 30);
   }
@@ -696,35 +726,102 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
+  auto id_of = [&](int i) { return fixed(a.prefix)[(32 * i) >> a.page_log2]; };
   auto token_of = [&](int i, int id) {
     const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
     return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
   };
-  const int end = min(last, (most + 31) >> 5);
-  Frag<KIND, D> k, v;
-  int id = 0;
-  if (first < end) {
-    id = fixed(a.prefix)[(32 * first) >> a.page_log2];
-    const int64_t t = token_of(first, id);
-    k.load(a.ck, a.cks, t, lane);
-    v.load(a.cv, a.cvs, t, lane);
-  }
-  for (int i = first; i < end; ++i) {
-    const int next_id = i + 1 < end ? fixed(a.prefix)[(32 * (i + 1)) >> a.page_log2] : 0;
-    x.scores(k);
-    if (i + 1 < end) k.load(a.ck, a.cks, token_of(i + 1, next_id), lane);
-    Sight g;
-    g.bad = (unsigned)id >= (unsigned)a.n_pages;
-    g.least = least - 32 * i;
-    g.most = most - 32 * i;
-    g.some = g.bad || g.least < 32;
-    int limit[MF];
+  // A stage's keys, then its values: load j of wavefront w is the KB 4 j + w of either.
+  constexpr int KB = NB * D * ES / 32;  // KB of keys (and of values) in a stage
+  static_assert(KB % 4 == 0 && KB / 4 * 2 == S::LP, "every wavefront brings as much");
+  u32x4 in[S::LP];
+  f32x4 in_s;
+  int ids[NB];
+  auto ask = [&](int i0) {  // blocks i0 .. (the last one again past the share's end)
+    int64_t t[NB];
 #pragma unroll
-    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
-    x.weigh(a, v, g, limit, lane);
-    x.add(v, g, limit, lane);
-    if (i + 1 < end) v.load(a.cv, a.cvs, token_of(i + 1, next_id), lane);
-    id = next_id;
+    for (int b = 0; b < NB; ++b) {
+      const int i = min(i0 + b, last - 1);
+      t[b] = token_of(i, ids[b] = id_of(i));
+    }
+#pragma unroll
+    for (int j = 0; j < S::LP; ++j) {
+      const int p = 4 * (j % (S::LP / 2)) + w, b = p / (KB / NB);
+      const uint8_t* base = j < S::LP / 2 ? a.ck : a.cv;
+      in[j] = *reinterpret_cast<const u32x4*>(base + (NB > 1 && b ? t[NB - 1] : t[0]) * (D * ES) + (p % (KB / NB)) * 1024 + lane * 16);
+    }
+    if constexpr (ES == 1)
+      if (tid < 16 * NB) {
+        const int j = tid & 7, b = NB > 1 ? (tid >> 3) & 1 : 0;
+        const float* base = tid < 8 * NB ? a.cks : a.cvs;
+        in_s = *reinterpret_cast<const f32x4*>(base + (NB > 1 && b ? t[NB - 1] : t[0]) + 4 * j);
+      }
+  };
+  auto put = [&](S& to) {
+#pragma unroll
+    for (int j = 0; j < S::LP; ++j) {
+      const int p = 4 * (j % (S::LP / 2)) + w;
+      u32x4(*dst)[64] = j < S::LP / 2 ? to.k : to.v;
+      if constexpr (ES == 2) {
+        dst[p][lane] = in[j];
+      } else {
+        dst[2 * p][lane] = widen8<KIND>(in[j][0], in[j][1]);
+        dst[2 * p + 1][lane] = widen8<KIND>(in[j][2], in[j][3]);
+      }
+    }
+    if constexpr (ES == 1)
+      if (tid < 16 * NB) *reinterpret_cast<f32x4*>(&to.s[tid / (8 * NB)][4 * (tid % (8 * NB))]) = in_s;
+  };
+  if (first < last) {
+    ask(first);
+    put(stage[0]);
+  }
+  __syncthreads();
+  for (int i0 = first, at = 0; i0 < last; i0 += NB, at ^= 1) {
+    const S& st = stage[at];
+    bool bad[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) bad[b] = (unsigned)ids[b] >= (unsigned)a.n_pages;
+    if (i0 + NB < last) ask(i0 + NB);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int i = i0 + b;
+      Sight g;
+      g.bad = bad[b];
+      g.least = least - 32 * i;
+      g.most = most - 32 * i;
+      g.some = g.bad || g.least < 32;
+      if (i >= last || g.most <= 0) continue;
+      int limit[MF];
+#pragma unroll
+      for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+      x.scores([&](int t, int s) { return st.k[(b * 2 + t) * (D / 32) + s][lane]; });
+      f32x4 ks[2], vs[2];
+      if constexpr (ES == 1) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          ks[t] = *reinterpret_cast<const f32x4*>(&st.s[0][32 * b + 16 * t + 4 * qd]);
+          vs[t] = *reinterpret_cast<const f32x4*>(&st.s[1][32 * b + 16 * t + 4 * qd]);
+        }
+      }
+      x.weigh(a, ks, vs, g, limit, lane);
+      if (!g.some) {
+        x.add([&](int e) { return st.v[b * (D / 16) + e][lane]; });
+      } else {
+        const u32x4 any = x.before(g.most, 0xffffu, lane);
+        x.add([&](int e) {
+          u32x4 v = st.v[b * (D / 16) + e][lane] & any;
+          const u32x4 odd = x.odd_halves(v);
+          if (__ballot((odd[0] | odd[1] | odd[2] | odd[3]) != 0)) {
+            x.count(v, e, limit, lane);
+            v = v & ~odd;
+          }
+          return v;
+        });
+      }
+    }
+    if (i0 + NB < last) put(stage[at ^ 1]);
+    __syncthreads();
   }
 #pragma unroll
   for (int f = 0; f < MF; ++f) {
@@ -757,7 +854,7 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
   const int head = rank - (int)tok * a.q_heads, b = (int)tok / a.n_q, h = head / group;
   const int row = ((int)tok - b * a.n_q) * group + head % group, frag_rows = 16 * a.frags, rb = row / frag_rows;
   const int piece_rows = min(a.n_q * group, frag_rows);
-  const int length = fixed(a.lengths)[b];
+  const int length = length_of(a, b);
   const int blocks = own_blocks(a, b);
   uint32_t g0 = 0;
   int pieces = blocks > 0;  // of the item
@@ -852,7 +949,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   p.grid = (int)std::min<int64_t>(256 * cu_holds(a.qmax == 0, p.frags * dim), std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront
   if (a.prefix_len) {
     const int64_t prows = (int64_t)a.batch * rows;
-    p.pre_frags = frags_of(prows, dim);
+    p.pre_frags = prows <= 64 || dim == 256 ? 1 : 2;
     const int64_t wgs = ((prows + 64 * p.pre_frags - 1) / (64 * p.pre_frags)) * a.kv_heads;
     const int64_t blocks = ((int64_t)a.prefix_len + 31) / 32;
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((blocks + 3) / 4, 64), 512 / wgs));
@@ -888,15 +985,13 @@ template <int KIND, int D, int MF> hipError_t go_own(const AttnArgs& a, const Pl
 }
 template <int KIND, int D, int MF> hipError_t go_prefix(const AttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.batch * a.n_q * (a.q_heads / a.kv_heads);
-  hipLaunchKernelGGL((attention_prefix_kernel<KIND, D, MF>), dim3((unsigned)((rows + 64 * MF - 1) / (64 * MF)), a.kv_heads, a.shares),
-                     dim3(256), 0, s, a);
+  const unsigned teams = (unsigned)((rows + 64 * MF - 1) / (64 * MF)), pairs = (unsigned)(a.kv_heads * a.shares);
+  hipLaunchKernelGGL((attention_prefix_kernel<KIND, D, MF>), dim3((pairs + 7) / 8 * 8 * teams), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.prefix_len) {
-    if constexpr (D == 64)
-      if (p.pre_frags == 4) e = go_prefix<KIND, D, 4>(a, s);
     if constexpr (D <= 128)
       if (p.pre_frags == 2) e = go_prefix<KIND, D, 2>(a, s);
     if (p.pre_frags == 1) e = go_prefix<KIND, D, 1>(a, s);
