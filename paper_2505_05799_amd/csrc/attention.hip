@@ -40,6 +40,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kBase = 8.f;              // weights are 2^8 at the reference ..
 constexpr uint32_t kMostF16 = 0x7800u, kMostBf16 = 0x4700u;  // .. and move it past 2^15 (fp16 ends at 2^16)
 constexpr float kLeastScale = 0x1p-80f;
+constexpr float kNoReference = -0x1p126f;  // of a row that has seen nothing: below any, and against it every weight is inf
 
 template <int KIND> LANES_INL f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   if constexpr (KIND == C_BF16)
@@ -122,7 +123,7 @@ template <int KIND, int D, int MF> struct Rows16 {
     for (int f = 0; f < MF; ++f) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) acc[f][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      ref[f] = -__builtin_inff();
+      ref[f] = kNoReference;
       sum[f] = 0.f;
     }
   }
@@ -177,66 +178,71 @@ template <int KIND, int D, int MF> struct Rows16 {
   // weights of the 32 tokens, sums and references; ks, vs: the tokens' scales, limit: how many of
   // the tokens a row sees
   LANES_INL void weigh(const AttnArgs& a, const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Sight& g, const int (&limit)[MF], int lane) {
+    float x[MF][8], p[MF][8], m[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
-      float x[8], p[8], s[8];
-      float m = mul[f];
+      m[f] = mul[f];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = ES == 1 ? w[f][i] * ks[i >> 2][i & 3] : w[f][i];
-        s[i] = ES == 1 ? vs[i >> 2][i & 3] : 1.f;
-      }
-      if (a.softcap > 0.f) {
-        const float c = a.softcap * kLog2e;
+      for (int i = 0; i < 8; ++i) x[f][i] = ES == 1 ? w[f][i] * ks[i >> 2][i & 3] : w[f][i];
+    }
+    if (a.softcap > 0.f) {
+      const float c = a.softcap * kLog2e;
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)  // tanh y = 1 - 2 / (1 + e^(2 y))
-          x[i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[i] * m * (2.f * kLog2e)));
-        m = 1.f;
+          x[f][i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[f][i] * m[f] * (2.f * kLog2e)));
+        m[f] = 1.f;
       }
-      if (g.some) {
+    }
+    auto sees = [&](int f, int i) { return 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f]; };
+    if (g.some) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const bool in = 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f];
-          x[i] = in ? (g.bad ? __builtin_nanf("") : x[i] * m) : -__builtin_inff();
-          s[i] = in ? s[i] : 0.f;
-        }
-        m = 1.f;
+      for (int f = 0; f < MF; ++f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[f][i] = sees(f, i) ? (g.bad ? __builtin_nanf("") : x[f][i] * m[f]) : -__builtin_inff();
+        m[f] = 1.f;
       }
-      auto weights = [&](float r) {
-        const float off = kBase - (r == -__builtin_inff() ? 0.f : r);
+    }
+    auto weights = [&](int f) {
+      const float off = kBase - ref[f];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], m, off));
-          w[f][i] = ES == 1 ? p[i] * s[i] : p[i];
-        }
-        constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
-        const u32x4 o = {pack2<P>(w[f][0], w[f][1]), pack2<P>(w[f][2], w[f][3]), pack2<P>(w[f][4], w[f][5]), pack2<P>(w[f][6], w[f][7])};
-        pw[f] = o;
-        const uint32_t top = max2(max2(o[0], o[1]), max2(o[2], o[3]));
-        return max(top & 0xffffu, top >> 16);
-      };
-      // (weights are not negative: the order of their bits is theirs, and inf and NaN come last)
-      bool move = weights(ref[f]) > (KIND == C_BF16 ? kMostBf16 : kMostF16);
-      if (ref[f] == -__builtin_inff()) {  // a row without a reference takes one from its first tokens
-#pragma unroll
-        for (int i = 0; i < 8; ++i) move |= x[i] * m > -__builtin_inff();
+      for (int i = 0; i < 8; ++i) {
+        p[f][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[f][i], m[f], off));
+        w[f][i] = ES == 1 ? p[f][i] * vs[i >> 2][i & 3] : p[f][i];
       }
-      if (__ballot(move)) {
-        float r = -__builtin_inff();
+      if (ES == 1 && g.some) {  // (whatever the scale of a token that is not seen)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[f][i] = sees(f, i) ? w[f][i] : 0.f;
+      }
+      constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
+      const u32x4 o = {pack2<P>(w[f][0], w[f][1]), pack2<P>(w[f][2], w[f][3]), pack2<P>(w[f][4], w[f][5]), pack2<P>(w[f][6], w[f][7])};
+      pw[f] = o;
+      return max2(max2(o[0], o[1]), max2(o[2], o[3]));
+    };
+    // (weights are not negative: the order of their bits is theirs, and inf and NaN come last; a
+    // row without a reference has inf for its first tokens)
+    uint32_t top = 0u;
+#pragma unroll
+    for (int f = 0; f < MF; ++f) top = max2(top, weights(f));
+    if (__ballot(max(top & 0xffffu, top >> 16) > (KIND == C_BF16 ? kMostBf16 : kMostF16))) {
+#pragma unroll
+      for (int f = 0; f < MF; ++f) {
+        float r = kNoReference;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          r = fmaxf(r, x[i] * m + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(s[i], kLeastScale)) : 0.f));
-        const float next = fmaxf(ref[f], quarters_max(r));
-        const float d = ref[f] == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref[f] - next);  // (nothing summed yet)
+          r = fmaxf(r, x[f][i] * m[f] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i >> 2][i & 3], kLeastScale)) : 0.f));
+        const float next = fmaxf(ref[f], quarters_max(r)), d = __builtin_amdgcn_exp2f(ref[f] - next);
         ref[f] = next;
         sum[f] *= d;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) acc[f][i] *= d;
-        weights(ref[f]);
+        weights(f);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[f] += p[i];
     }
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+      sum[f] += ((p[f][0] + p[f][1]) + (p[f][2] + p[f][3])) + ((p[f][4] + p[f][5]) + (p[f][6] + p[f][7]));
   }
 
   // `what` in the 16-bit halves of the lane's tokens that come before a limit
@@ -256,27 +262,29 @@ template <int KIND, int D, int MF> struct Rows16 {
   }
   static LANES_INL u32x4 odd_halves(u32x4 v) { return u32x4{odd_half(v[0]), odd_half(v[1]), odd_half(v[2]), odd_half(v[3])}; }
 
+  // ones where a value of a 16-byte piece is not finite
+  static LANES_INL uint32_t strange(uint32_t w) {
+    if constexpr (ES == 2) return odd_half(w);
+    const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f, 0xff
+    return (top >> 7) * 0xffu;
+  }
+  // ones for the values of a 16-byte piece whose tokens come before a limit
+  static LANES_INL u32x4 kept(int lim, int lane) {
+    if constexpr (ES == 2) return before(lim, 0xffffu, lane);
+    auto four = [&](int t) {
+      return (t < lim ? 0xffu : 0u) | (t + 1 < lim ? 0xff00u : 0u) | (t + 2 < lim ? 0xff0000u : 0u) | (t + 3 < lim ? 0xff000000u : 0u);
+    };
+    const uint32_t lo = four(4 * (lane >> 4)), hi = four(4 * (lane >> 4) + 16);
+    return u32x4{lo, hi, lo, hi};
+  }
+
   // Values for rows that do not see all of them.  Past the last token that any row sees they are
   // zeros.  One that is not finite must not reach the rows that do not see it (0 * inf): it
   // becomes zero, and rows become NaN where a product of ones counts such values among
   // the tokens they see.
   LANES_INL void sift(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
     if constexpr (KIND == C_I8) return;  // (every code is finite, the weights of what is not seen are 0)
-    auto strange = [&](uint32_t w) -> uint32_t {  // ones where a value is not finite
-      if constexpr (ES == 2) return odd_half(w);
-      const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes 0x7f, 0xff
-      return (top >> 7) * 0xffu;
-    };
-    u32x4 any;
-    if constexpr (ES == 2) {
-      any = before(g.most, 0xffffu, lane);
-    } else {
-      auto four = [&](int t) {
-        return (t < g.most ? 0xffu : 0u) | (t + 1 < g.most ? 0xff00u : 0u) | (t + 2 < g.most ? 0xff0000u : 0u) | (t + 3 < g.most ? 0xff000000u : 0u);
-      };
-      const uint32_t lo = four(4 * (lane >> 4)), hi = four(4 * (lane >> 4) + 16);
-      any = u32x4{lo, hi, lo, hi};
-    }
+    const u32x4 any = kept(g.most, lane);
     uint32_t odd = 0u;
 #pragma unroll
     for (int i = 0; i < Frag<KIND, D>::N; ++i) {
@@ -296,6 +304,7 @@ template <int KIND, int D, int MF> struct Rows16 {
   }
   // NaN for the rows that see a value of tile i that is not finite
   LANES_INL void count(u32x4 b, int i, const int (&limit)[MF], int lane) {
+    __builtin_amdgcn_sched_barrier(0);  // (rare: one tile after another, in few registers)
     b = odd_halves(b) & (kOne | kOne << 16);
     constexpr float nan = __builtin_nanf("");
 #pragma unroll
@@ -345,7 +354,7 @@ template <int KIND, int D, int MF> struct Rows16 {
 };
 
 // How far a partial sum's factor is from the joint reference's
-LANES_INL float join_factor(float ref, float top) { return ref == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(ref - top); }
+LANES_INL float join_factor(float ref, float top) { return __builtin_amdgcn_exp2f(ref - top); }
 
 LANES_INL void store4(void* out, int64_t at, f32x4 o, int act) {
   typedef u32x2 u32x2_half __attribute__((aligned(2)));
@@ -393,7 +402,7 @@ LANES_INL void meet(const Rows16<KIND, D, MF>& x, int f, int live, bool has, flo
   __syncthreads();
   for (int o = w * 64 + lane; o < live * (D / 4); o += 64 * W) {
     const int r = o / (D / 4), d = 4 * (o % (D / 4));
-    float top = -__builtin_inff(), l = 0.f;
+    float top = kNoReference, l = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < W; ++j)
@@ -695,8 +704,10 @@ template <int KIND, int D> struct Stage {
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
   using S = Stage<KIND, D>;
+  using R = Rows16<KIND, D, MF>;
   constexpr int RS = D + 4, ES = S::ES, NB = S::NB;
   __shared__ S stage[2];
+  __shared__ uint32_t odd_values;  // 1: some were not finite (in LDS they are zeros)
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, qd = lane >> 4;
   const int group = a.q_heads / a.kv_heads, rows = a.batch * a.n_q * group;
   const int teams = (rows + 64 * MF - 1) / (64 * MF);  // workgroups with the same blocks
@@ -757,7 +768,35 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
         in_s = *reinterpret_cast<const f32x4*>(base + (NB > 1 && b ? t[NB - 1] : t[0]) + 4 * j);
       }
   };
-  auto put = [&](S& to) {
+  // Values enter LDS as finite ones, tokens past the prefix as zeros: rows that do not see a token
+  // then need no more than a weight of 0.
+  auto put = [&](S& to, int i0) {
+    if constexpr (KIND != C_I8) {
+      uint32_t seen16 = 0u, any = 0u;
+      if (32 * (i0 + NB) > a.prefix_len) {
+#pragma unroll
+        for (int j = S::LP / 2; j < S::LP; ++j) {
+          const int p = 4 * (j % (S::LP / 2)) + w;
+          in[j] &= R::kept(a.prefix_len - 32 * (i0 + p / (KB / NB)), lane);
+        }
+      }
+#pragma unroll
+      for (int j = S::LP / 2; j < S::LP; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (ES == 2) seen16 = max2(seen16, in[j][e] & 0x7fff7fffu);
+          else any |= (in[j][e] & 0x7f7f7f7fu) + 0x01010101u;
+        }
+      const bool odd = ES == 2 ? max(seen16 & 0xffffu, seen16 >> 16) >= R::kInf : (any & 0x80808080u) != 0;
+      if (__ballot(odd)) {
+#pragma unroll
+        for (int j = S::LP / 2; j < S::LP; ++j) {
+          const u32x4 o = in[j];
+          in[j] = o & ~u32x4{R::strange(o[0]), R::strange(o[1]), R::strange(o[2]), R::strange(o[3])};
+        }
+        if (lane == 0) odd_values = 1u;
+      }
+    }
 #pragma unroll
     for (int j = 0; j < S::LP; ++j) {
       const int p = 4 * (j % (S::LP / 2)) + w;
@@ -772,9 +811,11 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
     if constexpr (ES == 1)
       if (tid < 16 * NB) *reinterpret_cast<f32x4*>(&to.s[tid / (8 * NB)][4 * (tid % (8 * NB))]) = in_s;
   };
+  if (tid == 0) odd_values = 0u;
+  __syncthreads();
   if (first < last) {
     ask(first);
-    put(stage[0]);
+    put(stage[0], first);
   }
   __syncthreads();
   for (int i0 = first, at = 0; i0 < last; i0 += NB, at ^= 1) {
@@ -805,23 +846,25 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
         }
       }
       x.weigh(a, ks, vs, g, limit, lane);
-      if (!g.some) {
-        x.add([&](int e) { return st.v[b * (D / 16) + e][lane]; });
-      } else {
-        const u32x4 any = x.before(g.most, 0xffffu, lane);
-        x.add([&](int e) {
-          u32x4 v = st.v[b * (D / 16) + e][lane] & any;
-          const u32x4 odd = x.odd_halves(v);
-          if (__ballot((odd[0] | odd[1] | odd[2] | odd[3]) != 0)) {
-            x.count(v, e, limit, lane);
-            v = v & ~odd;
-          }
-          return v;
-        });
+      x.add([&](int e) { return st.v[b * (D / 16) + e][lane]; });
+    }
+    if (i0 + NB < last) put(stage[at ^ 1], i0 + NB);
+    __syncthreads();
+  }
+  if (KIND != C_I8 && odd_values) {  // (rare: the values once more, as memory has them)
+    for (int i = first; i < min(last, (most + 31) >> 5); ++i) {
+      const int64_t t = token_of(i, id_of(i));
+      const u32x4 any = R::kept(a.prefix_len - 32 * i, lane);
+      int limit[MF];
+#pragma unroll
+      for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) {
+        __builtin_amdgcn_sched_barrier(0);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(a.cv + t * (D * ES) + (ES == 2 ? e : e >> 1) * 1024 + lane * 16) & any;
+        x.count(ES == 2 ? v : e & 1 ? widen8<KIND>(v[2], v[3]) : widen8<KIND>(v[0], v[1]), e, limit, lane);
       }
     }
-    if (i0 + NB < last) put(stage[at ^ 1]);
-    __syncthreads();
   }
 #pragma unroll
   for (int f = 0; f < MF; ++f) {
@@ -865,7 +908,7 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
   }
   if (pieces == 1 && !a.prefix_len) return;  // written where it was computed
   const int shares = length > 0 ? a.shares : 0, n = shares + pieces;
-  float top = -__builtin_inff(), l = 0.f;
+  float top = kNoReference, l = 0.f;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int i0 = gr; i0 < n; i0 += 4 * GP) {
     f32x4 o[4];
@@ -883,7 +926,7 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
         s[j] = p[D + 1];
       } else {
         o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        r[j] = -__builtin_inff();
+        r[j] = kNoReference;
         s[j] = 0.f;
       }
     }
@@ -925,7 +968,7 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
 
 
 // Fragments of 16 rows that a wavefront takes
-int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : rows <= 32 || dim == 128 ? 2 : 4; }
+int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : 2; }
 
 // Wavefronts to an item, or 0 where the list of costs is shared.  An item to a workgroup is one launch
 // and needs no search for its place; from 64 blocks on its length is what the launch waits for, and
@@ -997,8 +1040,6 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
     if (p.pre_frags == 1) e = go_prefix<KIND, D, 1>(a, s);
     if (e != hipSuccess) return e;
   }
-  if constexpr (D == 64)
-    if (p.frags == 4) e = go_own<KIND, D, 4>(a, p, s);
   if constexpr (D <= 128)
     if (p.frags == 2) e = go_own<KIND, D, 2>(a, p, s);
   if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
