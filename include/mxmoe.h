@@ -355,7 +355,8 @@ MXMOE_API size_t mxmoe_kv_scale_bytes(const mxmoe_kv_cache* cache);
  *              q_out is written).  A slot given twice in a call holds either token's
  *              bytes or some of both: what is read from it is undefined, other slots are not
  *              affected.
- * `act` is the cache's.  rot: a multiple of 16 up to dim (UNSUPPORTED otherwise).
+ * `act` is the cache's.  rot: a multiple of 16 up to dim, n_tokens <= 2^24 (UNSUPPORTED
+ * otherwise).
  * 2-byte aligned rows, 4-byte positions and slots, 8-byte freqs.  Outputs share no
  * byte with inputs (but q_out with q) or each other.  1e-30 <= eps <= 1e30 where there is a
  * weight; q_heads <= 65536.
@@ -369,7 +370,7 @@ MXMOE_API mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_to
 
 /* Rows of the cache back: k_out, v_out `act` [n_tokens, heads, dim] dense, code * scale
  * rounded once (16-bit rows as they are); slots int32 [n_tokens], zeros for a slot outside the
- * cache.  Outputs 2-byte aligned; they share no byte with the cache, slots or each
+ * cache.  n_tokens <= 2^24 (UNSUPPORTED beyond).  Outputs 2-byte aligned; they share no byte with the cache, slots or each
  * other.  Errors: INVALID_ARG, UNSUPPORTED, HIP.                             */
 MXMOE_API mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const int32_t* slots,
                            void* k_out, void* v_out, hipStream_t stream);

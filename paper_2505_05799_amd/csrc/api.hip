@@ -683,6 +683,7 @@ mxmoe_status check_cache(const mxmoe_kv_cache* c, bool buffers) {
   if (!aligned(c->k_scales, 16) || !aligned(c->v_scales, 16)) return MXMOE_ERR_INVALID_ARG;
   return MXMOE_OK;
 }
+constexpr int32_t kMaxKvTokens = 1 << 24;  // of a call
 int64_t cache_bytes(const mxmoe_kv_cache& c) { return (int64_t)c.n_pages * c.heads * c.page_size * c.dim * (c.qmax ? 1 : 2); }
 int64_t scale_bytes(const mxmoe_kv_cache& c) { return c.qmax ? (int64_t)c.n_pages * c.heads * c.page_size * 4 : 0; }
 Rows whole(const void* p, int64_t bytes) { return Rows{p, bytes, bytes, p && bytes > 0 ? 1 : 0}; }
@@ -719,7 +720,7 @@ mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_tokens, cons
   if (st != MXMOE_OK) return st;
   const mxmoe_kv_cache& c = *cache;
   if (n_tokens < 0 || q_heads < 0 || q_heads > 65536 || (interleaved != 0 && interleaved != 1)) return MXMOE_ERR_INVALID_ARG;
-  if (rot < 0 || rot > c.dim || rot % 16) return MXMOE_ERR_UNSUPPORTED;
+  if (rot < 0 || rot > c.dim || rot % 16 || n_tokens > kMaxKvTokens) return MXMOE_ERR_UNSUPPORTED;
   if ((q_weight || k_weight) && (!(eps >= 1e-30) || !(eps <= 1e30))) return MXMOE_ERR_INVALID_ARG;
   if (n_tokens == 0) return MXMOE_OK;
   if (!k || !v || !slots || (q_heads > 0) != (q != nullptr) || (q_heads > 0) != (q_out != nullptr) || (q_weight && !q))
@@ -777,6 +778,7 @@ mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const 
   if (st != MXMOE_OK) return st;
   const mxmoe_kv_cache& c = *cache;
   if (n_tokens < 0) return MXMOE_ERR_INVALID_ARG;
+  if (n_tokens > kMaxKvTokens) return MXMOE_ERR_UNSUPPORTED;
   if (n_tokens == 0) return MXMOE_OK;
   if (!slots || !k_out || !v_out || !aligned(slots, 4) || !aligned(k_out, 2) || !aligned(v_out, 2)) return MXMOE_ERR_INVALID_ARG;
   const int64_t ob = 2 * (int64_t)n_tokens * c.heads * c.dim;

@@ -5,21 +5,56 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin)        angle = position * frequency, in 64 bits
 //   codes, scale: the per-token recipe of rowquant.h on the fp32 values of a head's row
 //
-// dim / 8 lanes hold a head's row, 8 elements each.
+// dim / 8 lanes hold a head's row, 8 elements each.  Keys are written in the 16-byte pieces that a
+// row consists of.  A value's elements lie 16 bytes apart there, next to those of other tokens:
+// 32 tokens whose slots are one block of the cache go through LDS and leave as whole pieces (and come
+// back that way), others element by element.
 #include "kvcache.h"
 #include "lanes.h"
 
 namespace mxmoe {
 namespace {
 
-LANES_INL void store_act(uint16_t* p, const float (&v)[8], int act) {
-  u32x4 o;
+// The row's factor of the norm: 1 / sqrt(mean + eps) in 64 bits, by an approximate root and one step
+// of Newton's (relative error below 2^-40), rounded to fp32.
+template <int D> LANES_INL float norm_factor(const float (&v)[8], double eps) {
+  double ss = 0.0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = act == MXMOE_BF16 ? pack2<MXMOE_BF16>(v[2 * i], v[2 * i + 1]) : pack2<MXMOE_F16>(v[2 * i], v[2 * i + 1]);
-  *reinterpret_cast<u32x4_any*>(p) = o;
+  for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+  const double m = __builtin_fma(lanes_sum<D / 8>(ss), 1.0 / D, eps);
+  double r = __builtin_amdgcn_rsq(m);
+  const double e = __builtin_fma(-m * r, r, 1.0);
+  r = __builtin_fma(0.5 * r, e, r);
+  // (the step turns the root of inf, 0, into NaN)
+  return m < __builtin_inf() ? (float)r : m != m ? __builtin_nanf("") : 0.f;
 }
-LANES_INL void load_act(const uint16_t* p, float (&v)[8], int act) {
-  const u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+
+// Codes and scale of a head's row that dim / 8 lanes hold
+struct Coded { u32x2 q; float scale; };
+template <int D> LANES_INL Coded encode(const float (&v)[8], int qmax) {
+  uint32_t mb = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mb = max(mb, __float_as_uint(v[i]) & 0x7fffffffu);
+  mb = lanes_umax<D / 8>(mb);
+  const float amax = __uint_as_float(mb), qm = (float)qmax;
+  Coded c = {{0u, 0u}, 0.f};
+  if (mb >= 0x7f800000u) {
+    c.scale = __builtin_nanf("");
+  } else if (amax >= kTinyAmax) {
+    const float inv = __fdiv_rn(qm, amax);
+    const bool f8 = qmax == kQmaxF8;
+    c.scale = __fdiv_rn(amax, qm);
+    c.q = u32x2{codes4(v[0], v[1], v[2], v[3], inv, f8), codes4(v[4], v[5], v[6], v[7], inv, f8)};
+  }
+  return c;
+}
+LANES_INL u32x4 rounded(const float (&v)[8], int act) {
+  u32x4 o;
+  if (act == MXMOE_BF16) o = u32x4{pack2<MXMOE_BF16>(v[0], v[1]), pack2<MXMOE_BF16>(v[2], v[3]), pack2<MXMOE_BF16>(v[4], v[5]), pack2<MXMOE_BF16>(v[6], v[7])};
+  else o = u32x4{pack2<MXMOE_F16>(v[0], v[1]), pack2<MXMOE_F16>(v[2], v[3]), pack2<MXMOE_F16>(v[4], v[5]), pack2<MXMOE_F16>(v[6], v[7])};
+  return o;
+}
+LANES_INL void widened(u32x4 w, float (&v)[8], int act) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const f32x2 a = act == MXMOE_BF16 ? unpack2<MXMOE_BF16>(w[i]) : unpack2<MXMOE_F16>(w[i]);
@@ -27,193 +62,337 @@ LANES_INL void load_act(const uint16_t* p, float (&v)[8], int act) {
     v[2 * i + 1] = a[1];
   }
 }
+LANES_INL u32x4 row_piece(const void* p, int64_t at) { return *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const uint16_t*>(p) + at); }
 
-// A workgroup takes `tb` tokens and the heads hs .. he of a token's q | k | v heads.  The
-// rotations' cosines and sines of its tokens are in LDS, one pair of a token to a thread.
+// The slots of 32 tokens of a call from t0 on: whether they are one block of the cache, from its first
+// slot on (every wavefront finds out for itself)
+LANES_INL int block_of(const int32_t* slots, int t0, int tokens, int n_slots) {
+  const int l = threadIdx.x & 31, t = t0 + l;
+  const int slot = t >= 0 && t < tokens ? slots[t] : -1, first = __builtin_amdgcn_readfirstlane(slot);
+  const bool in = first >= 0 && first < n_slots && first % 32 == 0 && slot == first + l;
+  return __ballot(!in) ? -1 : first;
+}
+
+// Pieces of values in LDS: 256 bytes of (dim tile, q), 16 bytes further apart than in the cache, so that
+// lanes that read different tiles meet different banks.
+constexpr int kTile = 256 + 16;
+template <int ES> LANES_INL int lds_at(int t, int d) {
+  const int q = (t >> 2) & 3, j = (t & 3) + ((t >> 4) & 1) * 4;
+  if (ES == 2) return ((d >> 4) * 4 + q) * kTile + (d & 15) * 16 + 2 * j;
+  return ((d >> 5) * 4 + q) * kTile + (d & 15) * 16 + ((d >> 4) & 1) * 8 + j;
+}
+
+// 32 tokens' values of one head into the cache
+template <int D, int ES> LANES_INL void append_values(const KvAppendArgs& a, int t0, int h, uint8_t* lds) {
+  constexpr int GL = D / 8, RP = 256 / GL;
+  const int tid = threadIdx.x, c = tid % GL;
+  const int first = block_of(a.slots, t0, a.tokens, a.n_slots);
+  const int page = (1 << a.page_log2) - 1;
+  const int64_t rec0 = first < 0 ? 0 : ((int64_t)(first >> a.page_log2) * a.kv_heads + h) << a.page_log2;
+#pragma unroll
+  for (int r0 = 0; r0 < 32; r0 += RP) {
+    const int i = r0 + tid / GL, t = t0 + i;
+    const bool live = i < 32 && t >= 0 && t < a.tokens;
+    const u32x4 w = live ? row_piece(a.v, t * a.ldv + h * D + 8 * c) : u32x4{0u, 0u, 0u, 0u};
+    const int slot = live ? a.slots[t] : -1;
+    const bool keep = slot >= 0 && slot < a.n_slots;
+    const int64_t rec = keep ? ((int64_t)(slot >> a.page_log2) * a.kv_heads + h) << a.page_log2 : 0;
+    uint8_t* to = first >= 0 ? lds : reinterpret_cast<uint8_t*>(a.cv) + rec * (D * ES);
+    auto place = [&](int e) { return first >= 0 ? lds_at<ES>(i, 8 * c + e) : value_at<ES>(slot & page, 8 * c + e, D); };
+    if constexpr (ES == 1) {
+      float v[8];
+      widened(w, v, a.act);
+      const Coded q = encode<D>(v, a.qmax);
+      if (keep) {
+        if (c == 0) a.cvs[rec + (slot & page)] = q.scale;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[place(e)] = (uint8_t)(q.q[e >> 2] >> (8 * (e & 3)));
+      }
+    } else if (keep) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *reinterpret_cast<uint16_t*>(to + place(e)) = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+  if (first < 0) return;
+  __syncthreads();
+  uint8_t* base = reinterpret_cast<uint8_t*>(a.cv) + (rec0 + (first & page)) * (D * ES);
+#pragma unroll
+  for (int o = tid; o < 2 * D * ES; o += 256)
+    *reinterpret_cast<u32x4*>(base + 16 * o) = *reinterpret_cast<const u32x4*>(lds + (o >> 4) * kTile + (o & 15) * 16);
+}
+
+// The first `value_jobs` workgroups take 32 tokens' values of one head each.  The others take `tb`
+// tokens and every `parts`-th set of heads of a token's q | k (and v, where values have no jobs of
+// their own): the groups of dim / 8 lanes share the tokens and take heads in turn, the next
+// row on its way meanwhile.  The rotations' cosines and sines go through LDS, one pair of a
+// token to a thread, into the registers of the lanes that need them for all heads.
 template <int D>
 __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL;
-  extern __shared__ float2 turn[];  // [tb][rot / 2]
-  const int tid = threadIdx.x, c = tid % GL, half = a.rot / 2;
-  const int t0 = (int)blockIdx.x * a.tb, nt = min(a.tb, a.tokens - t0);
-  for (int i = tid; i < nt * half; i += 256) {
-    const int t = i / half, p = i - t * half;
-    const double turns = (double)a.positions[t0 + t] * a.freqs[p] * 0.15915494309189533577;
-    const float f = 2.f * (float)(turns - rint(turns));
-    float sn, cs;
-    sincospif(f, &sn, &cs);
-    turn[i] = make_float2(cs, sn);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[D / 4 * kTile > RP * D / 2 * 8 ? D / 4 * kTile : RP * D / 2 * 8];
+  if ((int)blockIdx.x < a.value_jobs) {
+    // (blocks begin where the first token's slot says, so that the tokens of one sequence fall into them)
+    const int job = (int)blockIdx.x / a.kv_heads, h = (int)blockIdx.x - job * a.kv_heads;
+    const int t0 = 32 * job - (a.slots[0] & 31);
+    if (t0 >= a.tokens) return;
+    if (a.qmax) append_values<D, 1>(a, t0, h, lds);
+    else append_values<D, 2>(a, t0, h, lds);
+    return;
   }
-  __syncthreads();
-  const int per = (a.heads + (int)gridDim.y - 1) / (int)gridDim.y;
-  const int h0 = (int)blockIdx.y * per, nh = min(per, a.heads - h0);
-  const int rows = nt * nh;
-  for (int r0 = 0; r0 < rows; r0 += RP) {
-    const int r = r0 + tid / GL;
-    const bool live = r < rows;  // (lanes of no row go along: the cross-lane moves take whole groups)
-    const int tl = live ? r / nh : 0, h = h0 + (live ? r - tl * nh : 0), t = t0 + tl;
-    const int what = h < a.q_heads ? 0 : h < a.q_heads + a.kv_heads ? 1 : 2;
-    const int hk = h - a.q_heads - (what == 2 ? a.kv_heads : 0);
-    const uint16_t* src = what == 0 ? reinterpret_cast<const uint16_t*>(a.q) + t * a.ldq + h * D
-                        : reinterpret_cast<const uint16_t*>(what == 1 ? a.k : a.v) + t * (what == 1 ? a.ldk : a.ldv) + hk * D;
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (live) load_act(src + 8 * c, v, a.act);
-    const void* w = what == 0 ? a.q_weight : what == 1 ? a.k_weight : nullptr;
-    if (w) {
-      float g[8];
-      load_act(reinterpret_cast<const uint16_t*>(w) + 8 * c, g, a.act);
-      double ss = 0.0;
+  float2* turn = reinterpret_cast<float2*>(lds);  // [tb][rot / 2]
+  const int tid = threadIdx.x, c = tid % GL, half = a.rot / 2, job = (int)blockIdx.x - a.value_jobs;
+  const int part = job % a.parts, t0 = job / a.parts * a.tb;
+  const int per = RP / a.tb, tl = tid / GL / per, t = t0 + tl;  // groups to a token, this group's token
+  const bool live = t < a.tokens;
+  const int step = per * a.parts;
+  int h = part * per + tid / GL % per;
+  auto row_of = [&](int h) {
+    return h < a.q_heads ? row_piece(a.q, t * a.ldq + h * D + 8 * c)
+           : h < a.q_heads + a.kv_heads ? row_piece(a.k, t * a.ldk + (h - a.q_heads) * D + 8 * c)
+                                        : row_piece(a.v, t * a.ldv + (h - a.q_heads - a.kv_heads) * D + 8 * c);
+  };
+  u32x4 next = live && h < a.heads ? row_of(h) : u32x4{0u, 0u, 0u, 0u};
+  const int slot = live ? a.slots[t] : -1;
+  // own and partner's cosines, sines and weights
+  float cs[8], sn[8];
+  const int hc = a.rot / 16;
+  const bool in = 8 * c < a.rot, low = c < hc;
+  const int pc = !in || a.interleaved ? c : low ? c + hc : c - hc;
+  if (a.rot) {
+    for (int i = tid; i < a.tb * half; i += 256) {
+      const int k = i / half, p = i - k * half;
+      if (t0 + k < a.tokens) {
+        const double turns = (double)a.positions[t0 + k] * a.freqs[p] * 0.15915494309189533577;
+        float s1, c1;
+        sincospif(2.f * (float)(turns - rint(turns)), &s1, &c1);
+        turn[i] = make_float2(c1, s1);
+      }
+    }
+    __syncthreads();
+    if (in) {
+      const float2* z = turn + tl * half + (a.interleaved ? 4 * c : 8 * (low ? c : c - hc));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
-      ss = lanes_sum<GL>(ss);
-      const float f = (float)(1.0 / __builtin_sqrt(ss / D + a.eps));
+      for (int i = 0; i < 8; ++i) {
+        const float2 w = z[a.interleaved ? i >> 1 : i];
+        cs[i] = w.x;
+        sn[i] = (a.interleaved ? (i & 1) == 0 : low) ? -w.y : w.y;
+      }
+    }
+  }
+  u32x4 wq = {0u, 0u, 0u, 0u}, wk = wq, wqp = wq, wkp = wq;
+  if (a.q_weight) wq = row_piece(a.q_weight, 8 * c), wqp = row_piece(a.q_weight, 8 * pc);
+  if (a.k_weight) wk = row_piece(a.k_weight, 8 * c), wkp = row_piece(a.k_weight, 8 * pc);
+  const int other = (tid & 63) - c + pc;
+  const bool keep = slot >= 0 && slot < a.n_slots;
+  const int page = (1 << a.page_log2) - 1, at = slot & page;
+  // (all groups go round as often: the cross-lane moves take whole wavefronts)
+  for (int h0 = part * per; h0 < a.heads; h0 += step, h += step) {
+    const bool here = live && h < a.heads;
+    const u32x4 w = next;
+    if (live && h + step < a.heads) next = row_of(h + step);
+    const int what = h < a.q_heads ? 0 : h < a.q_heads + a.kv_heads ? 1 : 2;
+    float v[8];
+    widened(w, v, a.act);
+    float f = 1.f;
+    const bool norm = (what == 0 && a.q_weight) || (what == 1 && a.k_weight);
+    if (norm) {
+      float g[8];
+      f = norm_factor<D>(v, a.eps);
+      widened(what ? wk : wq, g, a.act);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = v[i] * f * g[i];
     }
-    if (a.rot) {  // (q, k and v rows may share a wavefront: every lane moves, v keeps its own)
-      const float2* cs = turn + tl * half;
+    if (a.rot) {
+      float o[8];
       if (a.interleaved) {
-        if (what < 2 && 8 * c < a.rot) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 z = cs[4 * c + i];
-            const float x = v[2 * i], y = v[2 * i + 1];
-            v[2 * i] = x * z.x - y * z.y;
-            v[2 * i + 1] = y * z.x + x * z.y;
-          }
-        }
+        for (int i = 0; i < 8; ++i) o[i] = v[i ^ 1];
       } else {
-        const int hc = a.rot / 16;
-        const bool first = c < hc, in = c < 2 * hc;
-        const int other = (int)(threadIdx.x & 63) + (in ? (first ? hc : -hc) : 0);
-        float o[8];
+        u32x4 pw;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __shfl(v[i], other, 64);
-        if (what < 2 && in) {
+        for (int i = 0; i < 4; ++i) pw[i] = (uint32_t)__shfl((int)w[i], other, 64);
+        widened(pw, o, a.act);
+        if (norm) {
+          float g[8];
+          widened(what ? wkp : wqp, g, a.act);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 z = cs[8 * (first ? c : c - hc) + i];
-            v[i] = first ? v[i] * z.x - o[i] * z.y : v[i] * z.x + o[i] * z.y;
-          }
+          for (int i = 0; i < 8; ++i) o[i] = o[i] * f * g[i];
         }
+      }
+      if (in && what < 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * cs[i] + o[i] * sn[i];
       }
     }
     if (what == 0) {
-      if (live) store_act(reinterpret_cast<uint16_t*>(a.q_out) + t * a.ldo + h * D + 8 * c, v, a.act);
+      if (here) *reinterpret_cast<u32x4_any*>(reinterpret_cast<uint16_t*>(a.q_out) + t * a.ldo + h * D + 8 * c) = rounded(v, a.act);
+      continue;
     }
-    const int slot = live && what ? a.slots[t] : -1;
-    const bool keep = slot >= 0 && slot < a.n_slots;
-    const int64_t rec = (int64_t)(keep ? slot >> a.page_log2 : 0) * a.kv_heads + (what ? hk : 0);
-    const int at = keep ? slot & ((1 << a.page_log2) - 1) : 0;
+    const int hk = h - a.q_heads - (what == 2 ? a.kv_heads : 0);
+    const int64_t rec = (int64_t)((keep ? slot >> a.page_log2 : 0) * (int64_t)a.kv_heads + hk) << a.page_log2;
     if (a.qmax) {
-      uint32_t mb = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) mb = max(mb, __float_as_uint(v[i]) & 0x7fffffffu);
-      mb = lanes_umax<GL>(mb);
-      const float amax = __uint_as_float(mb), qm = (float)a.qmax;
-      float inv = 0.f, scale = 0.f;
-      if (mb >= 0x7f800000u) {
-        scale = __builtin_nanf("");
-      } else if (amax >= kTinyAmax) {
-        inv = __fdiv_rn(qm, amax);
-        scale = __fdiv_rn(amax, qm);
-      }
-      if (keep) {
-        const bool f8 = a.qmax == kQmaxF8;
-        u32x2 q = {0u, 0u};
-        if (inv > 0.f) q = u32x2{codes4(v[0], v[1], v[2], v[3], inv, f8), codes4(v[4], v[5], v[6], v[7], inv, f8)};
-        uint8_t* base = reinterpret_cast<uint8_t*>(what == 1 ? a.ck : a.cv) + (rec << a.page_log2) * D;
-        float* sc = (what == 1 ? a.cks : a.cvs) + (rec << a.page_log2) + at;
-        if (c == 0) *sc = scale;
+      const Coded q = encode<D>(v, a.qmax);
+      if (here && keep) {
+        uint8_t* base = reinterpret_cast<uint8_t*>(what == 1 ? a.ck : a.cv) + rec * D;
+        if (c == 0) (what == 1 ? a.cks : a.cvs)[rec + at] = q.scale;
         if (what == 1) {
-          *reinterpret_cast<u32x2*>(base + key_at<1>(at, c, D)) = q;
+          *reinterpret_cast<u32x2*>(base + key_at<1>(at, c, D)) = q.q;
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) base[value_at<1>(at, 8 * c + i, D)] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
+          for (int e = 0; e < 8; ++e) base[value_at<1>(at, 8 * c + e, D)] = (uint8_t)(q.q[e >> 2] >> (8 * (e & 3)));
         }
       }
-    } else if (keep) {
-      uint8_t* base = reinterpret_cast<uint8_t*>(what == 1 ? a.ck : a.cv) + (rec << a.page_log2) * (2 * D);
-      uint16_t o[8];
-      store_act(o, v, a.act);
+    } else if (here && keep) {
+      uint8_t* base = reinterpret_cast<uint8_t*>(what == 1 ? a.ck : a.cv) + rec * (2 * D);
       if (what == 1) {
-        *reinterpret_cast<u32x4*>(base + key_at<2>(at, c, D)) = *reinterpret_cast<const u32x4_any*>(o);
+        *reinterpret_cast<u32x4*>(base + key_at<2>(at, c, D)) = rounded(v, a.act);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint16_t*>(base + value_at<2>(at, 8 * c + i, D)) = o[i];
+        for (int e = 0; e < 8; ++e) *reinterpret_cast<uint16_t*>(base + value_at<2>(at, 8 * c + e, D)) = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
       }
     }
   }
 }
 
-// Rows at slots back in 16 bits: a row of one head (keys, then values) to dim / 8 lanes.
-template <int D>
+LANES_INL void decoded(u32x2 q, float s, int qmax, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t b = q[i >> 2] >> (8 * (i & 3)) & 0xffu;
+    v[i] = (qmax == kQmaxF8 ? __builtin_amdgcn_cvt_f32_fp8((int)b, 0) : (float)(int8_t)b) * s;
+  }
+}
+
+// Rows at slots back in 16 bits.  32 tokens of one head to a workgroup (keys, then values): whole
+// pieces where their slots are one block, else piece by piece and element by element.
+template <int D, int ES>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL;
-  const int c = threadIdx.x % GL;
-  const int64_t rows = (int64_t)a.tokens * a.kv_heads * 2;
-  for (int64_t r = (int64_t)blockIdx.x * RP + threadIdx.x / GL; r < rows; r += (int64_t)gridDim.x * RP) {
-    const int64_t t = r / (2 * a.kv_heads);
-    const int j = (int)(r - t * (2 * a.kv_heads)), what = j >= a.kv_heads, h = j - (what ? a.kv_heads : 0);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[D * ES / 8 * kTile];
+  const int tid = threadIdx.x, c = tid % GL;
+  const int job = (int)blockIdx.x / a.kv_heads, h = (int)blockIdx.x - job * a.kv_heads;
+  const int t0 = 32 * job - (a.slots[0] & 31);
+  if (t0 >= a.tokens) return;
+  const int first = block_of(a.slots, t0, a.tokens, a.n_slots);
+  const int page = (1 << a.page_log2) - 1;
+  if (first >= 0) {
+    const int64_t rec = (((int64_t)(first >> a.page_log2) * a.kv_heads + h) << a.page_log2) + (first & page);
+    const uint8_t* kb = reinterpret_cast<const uint8_t*>(a.ck) + rec * (D * ES);
+    const uint8_t* vb = reinterpret_cast<const uint8_t*>(a.cv) + rec * (D * ES);
+    constexpr int N = (2 * D * ES + 255) / 256;  // 16-byte pieces of keys (and of values) to a thread
+    u32x4 k[N], v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (tid + 256 * j < 2 * D * ES) {
+        k[j] = *reinterpret_cast<const u32x4*>(kb + 16 * (tid + 256 * j));
+        v[j] = *reinterpret_cast<const u32x4*>(vb + 16 * (tid + 256 * j));
+      }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int o = tid + 256 * j;
+      if (o >= 2 * D * ES) break;
+      *reinterpret_cast<u32x4*>(lds + (o >> 4) * kTile + (o & 15) * 16) = v[j];
+      // a key's piece: token o % 16 of tile o / (16 pieces a row), 8 or 16 elements
+      const int i = (o & 15) + 16 * (o / (D * ES)), p = o % (D * ES) / 16;
+      uint16_t* out = reinterpret_cast<uint16_t*>(a.k) + ((int64_t)(t0 + i) * a.kv_heads + h) * D;
+      if constexpr (ES == 2) {
+        *reinterpret_cast<u32x4_any*>(out + 8 * p) = k[j];
+      } else {
+        const float s = a.cks[rec + i];
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          decoded(u32x2{k[j][2 * e], k[j][2 * e + 1]}, s, a.qmax, f);
+          *reinterpret_cast<u32x4_any*>(out + 16 * p + 8 * e) = rounded(f, a.act);
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RP) {
+      const int i = r0 + tid / GL;
+      if (i >= 32) break;
+      uint16_t* out = reinterpret_cast<uint16_t*>(a.v) + ((int64_t)(t0 + i) * a.kv_heads + h) * D + 8 * c;
+      if constexpr (ES == 2) {
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = *reinterpret_cast<const uint16_t*>(lds + lds_at<2>(i, 8 * c + j));
+        *reinterpret_cast<u32x4_any*>(out) = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+      } else {
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = lds[lds_at<1>(i, 8 * c + j)];
+        float f[8];
+        decoded(u32x2{e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24}, a.cvs[rec + i], a.qmax, f);
+        *reinterpret_cast<u32x4_any*>(out) = rounded(f, a.act);
+      }
+    }
+    return;
+  }
+  for (int r = tid / GL; r < 64; r += RP) {  // 32 rows of keys, 32 of values
+    const int i = r & 31, what = r >> 5, t = t0 + i;
+    if (t < 0 || t >= a.tokens) continue;
     const int slot = a.slots[t];
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    uint16_t* out = reinterpret_cast<uint16_t*>(what ? a.v : a.k) + (t * a.kv_heads + h) * D + 8 * c;
+    uint16_t* out = reinterpret_cast<uint16_t*>(what ? a.v : a.k) + ((int64_t)t * a.kv_heads + h) * D + 8 * c;
     if (slot < 0 || slot >= a.n_slots) {
-      store_act(out, v, a.act);
+      *reinterpret_cast<u32x4_any*>(out) = u32x4{0u, 0u, 0u, 0u};
       continue;
     }
-    const int64_t rec = (int64_t)(slot >> a.page_log2) * a.kv_heads + h;
-    const int at = slot & ((1 << a.page_log2) - 1);
-    if (a.qmax) {
-      const uint8_t* base = reinterpret_cast<const uint8_t*>(what ? a.cv : a.ck) + (rec << a.page_log2) * D;
-      const float s = (what ? a.cvs : a.cks)[(rec << a.page_log2) + at];
-      uint8_t q[8];
+    const int64_t rec = ((int64_t)(slot >> a.page_log2) * a.kv_heads + h) << a.page_log2;
+    const int at = slot & page;
+    const uint8_t* base = reinterpret_cast<const uint8_t*>(what ? a.cv : a.ck) + rec * (D * ES);
+    if constexpr (ES == 1) {
+      u32x2 q;
       if (!what) {
-        *reinterpret_cast<u32x2_any*>(q) = *reinterpret_cast<const u32x2*>(base + key_at<1>(at, c, D));
+        q = *reinterpret_cast<const u32x2*>(base + key_at<1>(at, c, D));
       } else {
+        uint32_t e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = base[value_at<1>(at, 8 * c + i, D)];
+        for (int j = 0; j < 8; ++j) e[j] = base[value_at<1>(at, 8 * c + j, D)];
+        q = u32x2{e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24};
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        v[i] = (a.qmax == kQmaxF8 ? __builtin_amdgcn_cvt_f32_fp8((int)q[i], 0) : (float)(int8_t)q[i]) * s;
-      store_act(out, v, a.act);
+      float f[8];
+      decoded(q, (what ? a.cvs : a.cks)[rec + at], a.qmax, f);
+      *reinterpret_cast<u32x4_any*>(out) = rounded(f, a.act);
+    } else if (!what) {
+      *reinterpret_cast<u32x4_any*>(out) = *reinterpret_cast<const u32x4*>(base + key_at<2>(at, c, D));
     } else {
-      const uint8_t* base = reinterpret_cast<const uint8_t*>(what ? a.cv : a.ck) + (rec << a.page_log2) * (2 * D);
-      if (!what) {
-        *reinterpret_cast<u32x4_any*>(out) = *reinterpret_cast<const u32x4*>(base + key_at<2>(at, c, D));
-      } else {
+      uint32_t e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = *reinterpret_cast<const uint16_t*>(base + value_at<2>(at, 8 * c + i, D));
-      }
+      for (int j = 0; j < 8; ++j) e[j] = *reinterpret_cast<const uint16_t*>(base + value_at<2>(at, 8 * c + j, D));
+      *reinterpret_cast<u32x4_any*>(out) = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
     }
   }
+}
+
+template <int D> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
+  constexpr int RP = 2048 / D;
+  // 32 tokens and more: values by blocks
+  const int blocks = a.tokens >= 32 ? (a.tokens + 31) / 32 + 1 : 0;  // (they may begin anywhere in one)
+  a.value_jobs = blocks * a.kv_heads;
+  a.heads = a.q_heads + (blocks ? 1 : 2) * a.kv_heads;
+  // tokens to a workgroup: one pair of angles to a thread, more where there are many tokens
+  a.tb = a.tokens >= 4096 ? RP : a.tokens >= 4 ? (RP < 4 ? RP : 4) : 1;
+  const int teams = (a.tokens + a.tb - 1) / a.tb, per = RP / a.tb;
+  const int most = (a.heads + per - 1) / per, want = (512 + teams - 1) / teams;
+  a.parts = want < most ? want : most;
+  const int64_t grid = a.value_jobs + (int64_t)teams * a.parts;
+  hipLaunchKernelGGL(kv_append_kernel<D>, dim3((unsigned)grid), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int D> hipError_t go_read(const KvReadArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(((a.tokens + 31) / 32 + 1) * a.kv_heads));
+  if (a.qmax) hipLaunchKernelGGL((kv_read_kernel<D, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_read_kernel<D, 2>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_kv_append(KvAppendArgs a, int dim, hipStream_t s) {
-  a.heads = a.q_heads + 2 * a.kv_heads;
-  a.tb = 4;
-  const dim3 grid((a.tokens + a.tb - 1) / a.tb, a.tokens <= 256 ? (a.heads * dim / 8 + 255) / 256 : 1);
-  const size_t lds = sizeof(float2) * a.tb * (a.rot / 2);
-  switch (dim) {
-    case 64: hipLaunchKernelGGL(kv_append_kernel<64>, grid, dim3(256), lds, s, a); break;
-    case 128: hipLaunchKernelGGL(kv_append_kernel<128>, grid, dim3(256), lds, s, a); break;
-    default: hipLaunchKernelGGL(kv_append_kernel<256>, grid, dim3(256), lds, s, a); break;
-  }
-  return hipGetLastError();
+hipError_t launch_kv_append(const KvAppendArgs& a, int dim, hipStream_t s) {
+  return dim == 64 ? go_append<64>(a, s) : dim == 128 ? go_append<128>(a, s) : go_append<256>(a, s);
 }
-
 hipError_t launch_kv_read(const KvReadArgs& a, int dim, hipStream_t s) {
-  const int64_t rows = (int64_t)a.tokens * a.kv_heads * 2, rp = 2048 / dim, grid = (rows + rp - 1) / rp;
-  const dim3 g((unsigned)(grid < (1 << 20) ? grid : 1 << 20));
-  switch (dim) {
-    case 64: hipLaunchKernelGGL(kv_read_kernel<64>, g, dim3(256), 0, s, a); break;
-    case 128: hipLaunchKernelGGL(kv_read_kernel<128>, g, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL(kv_read_kernel<256>, g, dim3(256), 0, s, a); break;
-  }
-  return hipGetLastError();
+  return dim == 64 ? go_read<64>(a, s) : dim == 128 ? go_read<128>(a, s) : go_read<256>(a, s);
 }
 
 }  // namespace mxmoe

@@ -596,9 +596,9 @@ struct KvAppendArgs {
   int64_t ldq, ldk, ldv, ldo;
   double eps;
   int32_t tokens, q_heads, kv_heads, rot, interleaved, act, qmax, page_log2, n_slots;
-  int32_t heads, tb;  // set by the launch
+  int32_t heads, tb, parts, value_jobs;  // set by the launch
 };
-hipError_t launch_kv_append(KvAppendArgs a, int dim, hipStream_t s);
+hipError_t launch_kv_append(const KvAppendArgs& a, int dim, hipStream_t s);
 struct KvReadArgs {
   const void *ck, *cv;
   const float *cks, *cvs;

@@ -140,6 +140,7 @@ def test_append_refuses_caches_and_unsupported(lib):
     assert append(lib, cache(vs=at(3))) == M.ERR_INVALID_ARG
     for rot in (8, 24, 80, -16):
         assert append(lib, rot=rot) == M.ERR_UNSUPPORTED
+    assert append(lib, n=(1 << 24) + 1) == M.ERR_UNSUPPORTED and read(lib, n=(1 << 24) + 1) == M.ERR_UNSUPPORTED
     assert append(lib, n=0, q=None, out=None, k=None, v=None, slots=None) == M.OK
     assert lib.mxmoe_kv_append(None, 0, None, 0, 0, None, 0, None, 0, None, None, 1e-6, None, None, 0, 0, None, None, 0, None) \
         == M.ERR_INVALID_ARG
