@@ -48,16 +48,13 @@ template <int D> LANES_INL Coded encode(const float (&v)[8], int qmax) {
   }
   return c;
 }
-LANES_INL u32x4 rounded(const float (&v)[8], int act) {
-  u32x4 o;
-  if (act == MXMOE_BF16) o = u32x4{pack2<MXMOE_BF16>(v[0], v[1]), pack2<MXMOE_BF16>(v[2], v[3]), pack2<MXMOE_BF16>(v[4], v[5]), pack2<MXMOE_BF16>(v[6], v[7])};
-  else o = u32x4{pack2<MXMOE_F16>(v[0], v[1]), pack2<MXMOE_F16>(v[2], v[3]), pack2<MXMOE_F16>(v[4], v[5]), pack2<MXMOE_F16>(v[6], v[7])};
-  return o;
+template <int ACT> LANES_INL u32x4 rounded(const float (&v)[8]) {
+  return u32x4{pack2<ACT>(v[0], v[1]), pack2<ACT>(v[2], v[3]), pack2<ACT>(v[4], v[5]), pack2<ACT>(v[6], v[7])};
 }
-LANES_INL void widened(u32x4 w, float (&v)[8], int act) {
+template <int ACT> LANES_INL void widened(u32x4 w, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const f32x2 a = act == MXMOE_BF16 ? unpack2<MXMOE_BF16>(w[i]) : unpack2<MXMOE_F16>(w[i]);
+    const f32x2 a = unpack2<ACT>(w[i]);
     v[2 * i] = a[0];
     v[2 * i + 1] = a[1];
   }
@@ -83,7 +80,7 @@ template <int ES> LANES_INL int lds_at(int t, int d) {
 }
 
 // 32 tokens' values of one head into the cache
-template <int D, int ES> LANES_INL void append_values(const KvAppendArgs& a, int t0, int h, uint8_t* lds) {
+template <int D, int ES, int ACT> LANES_INL void append_values(const KvAppendArgs& a, int t0, int h, uint8_t* lds) {
   constexpr int GL = D / 8, RP = 256 / GL;
   const int tid = threadIdx.x, c = tid % GL;
   const int first = block_of(a.slots, t0, a.tokens, a.n_slots);
@@ -101,7 +98,7 @@ template <int D, int ES> LANES_INL void append_values(const KvAppendArgs& a, int
     auto place = [&](int e) { return first >= 0 ? lds_at<ES>(i, 8 * c + e) : value_at<ES>(slot & page, 8 * c + e, D); };
     if constexpr (ES == 1) {
       float v[8];
-      widened(w, v, a.act);
+      widened<ACT>(w, v);
       const Coded q = encode<D>(v, a.qmax);
       if (keep) {
         if (c == 0) a.cvs[rec + (slot & page)] = q.scale;
@@ -126,7 +123,7 @@ template <int D, int ES> LANES_INL void append_values(const KvAppendArgs& a, int
 // their own): the groups of dim / 8 lanes share the tokens and take heads in turn, the next
 // row on its way meanwhile.  The rotations' cosines and sines go through LDS, one pair of a
 // token to a thread, into the registers of the lanes that need them for all heads.
-template <int D>
+template <int D, int ACT>
 __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL;
   __shared__ __attribute__((aligned(16))) uint8_t lds[D / 4 * kTile > RP * D / 2 * 8 ? D / 4 * kTile : RP * D / 2 * 8];
@@ -135,8 +132,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
     const int job = (int)blockIdx.x / a.kv_heads, h = (int)blockIdx.x - job * a.kv_heads;
     const int t0 = 32 * job - (a.slots[0] & 31);
     if (t0 >= a.tokens) return;
-    if (a.qmax) append_values<D, 1>(a, t0, h, lds);
-    else append_values<D, 2>(a, t0, h, lds);
+    if (a.qmax) append_values<D, 1, ACT>(a, t0, h, lds);
+    else append_values<D, 2, ACT>(a, t0, h, lds);
     return;
   }
   float2* turn = reinterpret_cast<float2*>(lds);  // [tb][rot / 2]
@@ -153,11 +150,28 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
   };
   u32x4 next = live && h < a.heads ? row_of(h) : u32x4{0u, 0u, 0u, 0u};
   const int slot = live ? a.slots[t] : -1;
-  // own and partner's cosines, sines and weights
-  float cs[8], sn[8];
+  // Row element i becomes (x own[i] + partner turned[i]) times the row's factor: weight times cosine,
+  // partner's weight times sine (with its sign), of queries first, of keys when they come.
+  float own[8], turned[8];
+  int kind = -1;
   const int hc = a.rot / 16;
   const bool in = 8 * c < a.rot, low = c < hc;
   const int pc = !in || a.interleaved ? c : low ? c + hc : c - hc;
+  u32x4 weights[2][2] = {};  // (asked for before the angles)
+  if (a.q_weight) {
+    weights[0][0] = row_piece(a.q_weight, 8 * c);
+    weights[0][1] = row_piece(a.q_weight, 8 * pc);
+  }
+  if (a.k_weight) {
+    weights[1][0] = row_piece(a.k_weight, 8 * c);
+    weights[1][1] = row_piece(a.k_weight, 8 * pc);
+  }
+  float cs[8], sn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    cs[i] = 1.f;
+    sn[i] = 0.f;
+  }
   if (a.rot) {
     for (int i = tid; i < a.tb * half; i += 256) {
       const int k = i / half, p = i - k * half;
@@ -179,9 +193,6 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
       }
     }
   }
-  u32x4 wq = {0u, 0u, 0u, 0u}, wk = wq, wqp = wq, wkp = wq;
-  if (a.q_weight) wq = row_piece(a.q_weight, 8 * c), wqp = row_piece(a.q_weight, 8 * pc);
-  if (a.k_weight) wk = row_piece(a.k_weight, 8 * c), wkp = row_piece(a.k_weight, 8 * pc);
   const int other = (tid & 63) - c + pc;
   const bool keep = slot >= 0 && slot < a.n_slots;
   const int page = (1 << a.page_log2) - 1, at = slot & page;
@@ -192,18 +203,26 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
     if (live && h + step < a.heads) next = row_of(h + step);
     const int what = h < a.q_heads ? 0 : h < a.q_heads + a.kv_heads ? 1 : 2;
     float v[8];
-    widened(w, v, a.act);
-    float f = 1.f;
-    const bool norm = (what == 0 && a.q_weight) || (what == 1 && a.k_weight);
-    if (norm) {
-      float g[8];
-      f = norm_factor<D>(v, a.eps);
-      widened(what ? wk : wq, g, a.act);
+    widened<ACT>(w, v);
+    if (what < 2 && what != kind) {
+      kind = what;
+      float g[8], o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * f * g[i];
+      for (int i = 0; i < 8; ++i) g[i] = o[i] = 1.f;
+      if (what ? a.k_weight : a.q_weight) {
+        widened<ACT>(what ? weights[1][0] : weights[0][0], g);
+        widened<ACT>(what ? weights[1][1] : weights[0][1], o);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        own[i] = g[i] * cs[i];
+        turned[i] = (a.interleaved ? o[i ^ 1] : o[i]) * sn[i];
+      }
     }
+    const bool norm = (what == 0 && a.q_weight) || (what == 1 && a.k_weight);
+    const float f = norm ? norm_factor<D>(v, a.eps) : 1.f;
+    float o[8];
     if (a.rot) {
-      float o[8];
       if (a.interleaved) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = v[i ^ 1];
@@ -211,21 +230,18 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
         u32x4 pw;
 #pragma unroll
         for (int i = 0; i < 4; ++i) pw[i] = (uint32_t)__shfl((int)w[i], other, 64);
-        widened(pw, o, a.act);
-        if (norm) {
-          float g[8];
-          widened(what ? wkp : wqp, g, a.act);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = o[i] * f * g[i];
-        }
+        widened<ACT>(pw, o);
       }
-      if (in && what < 2) {
+    }
+    if (what < 2 && (norm || a.rot)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v[i] * cs[i] + o[i] * sn[i];
+      for (int i = 0; i < 8; ++i) {
+        const float y = v[i] * own[i];
+        v[i] = (in ? __builtin_fmaf(o[i], turned[i], y) : y) * f;
       }
     }
     if (what == 0) {
-      if (here) *reinterpret_cast<u32x4_any*>(reinterpret_cast<uint16_t*>(a.q_out) + t * a.ldo + h * D + 8 * c) = rounded(v, a.act);
+      if (here) *reinterpret_cast<u32x4_any*>(reinterpret_cast<uint16_t*>(a.q_out) + t * a.ldo + h * D + 8 * c) = rounded<ACT>(v);
       continue;
     }
     const int hk = h - a.q_heads - (what == 2 ? a.kv_heads : 0);
@@ -245,7 +261,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
     } else if (here && keep) {
       uint8_t* base = reinterpret_cast<uint8_t*>(what == 1 ? a.ck : a.cv) + rec * (2 * D);
       if (what == 1) {
-        *reinterpret_cast<u32x4*>(base + key_at<2>(at, c, D)) = rounded(v, a.act);
+        *reinterpret_cast<u32x4*>(base + key_at<2>(at, c, D)) = rounded<ACT>(v);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) *reinterpret_cast<uint16_t*>(base + value_at<2>(at, 8 * c + e, D)) = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
@@ -262,84 +278,84 @@ LANES_INL void decoded(u32x2 q, float s, int qmax, float (&v)[8]) {
   }
 }
 
-// Rows at slots back in 16 bits.  32 tokens of one head to a workgroup (keys, then values): whole
-// pieces where their slots are one block, else piece by piece and element by element.
-template <int D, int ES>
+// Rows at slots back in 16 bits.  32 tokens' keys or values of one head to a workgroup: whole pieces
+// where their slots are one block, else piece by piece and element by element.
+template <int D, int ES, int ACT>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
-  constexpr int GL = D / 8, RP = 256 / GL;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[D * ES / 8 * kTile];
+  constexpr int GL = D / 8, RP = 256 / GL, kRow = D * ES + 16;  // (rows of keys 16 bytes apart)
+  __shared__ __attribute__((aligned(16))) uint8_t lds[D * ES / 8 * kTile > 32 * kRow ? D * ES / 8 * kTile : 32 * kRow];
   const int tid = threadIdx.x, c = tid % GL;
-  const int job = (int)blockIdx.x / a.kv_heads, h = (int)blockIdx.x - job * a.kv_heads;
+  const int job = (int)blockIdx.x / (2 * a.kv_heads), row = (int)blockIdx.x - job * (2 * a.kv_heads);
+  const bool what = row >= a.kv_heads;
+  const int h = row - (what ? a.kv_heads : 0);
   const int t0 = 32 * job - (a.slots[0] & 31);
   if (t0 >= a.tokens) return;
   const int first = block_of(a.slots, t0, a.tokens, a.n_slots);
   const int page = (1 << a.page_log2) - 1;
+  const uint8_t* from = reinterpret_cast<const uint8_t*>(what ? a.cv : a.ck);
+  const float* scales = what ? a.cvs : a.cks;
+  uint16_t* to = reinterpret_cast<uint16_t*>(what ? a.v : a.k);
   if (first >= 0) {
     const int64_t rec = (((int64_t)(first >> a.page_log2) * a.kv_heads + h) << a.page_log2) + (first & page);
-    const uint8_t* kb = reinterpret_cast<const uint8_t*>(a.ck) + rec * (D * ES);
-    const uint8_t* vb = reinterpret_cast<const uint8_t*>(a.cv) + rec * (D * ES);
-    constexpr int N = (2 * D * ES + 255) / 256;  // 16-byte pieces of keys (and of values) to a thread
-    u32x4 k[N], v[N];
+    const uint8_t* base = from + rec * (D * ES);
+    constexpr int N = (2 * D * ES + 255) / 256;  // 16-byte pieces to a thread
+    u32x4 w[N];
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (tid + 256 * j < 2 * D * ES) {
-        k[j] = *reinterpret_cast<const u32x4*>(kb + 16 * (tid + 256 * j));
-        v[j] = *reinterpret_cast<const u32x4*>(vb + 16 * (tid + 256 * j));
-      }
+      if (tid + 256 * j < 2 * D * ES) w[j] = *reinterpret_cast<const u32x4*>(base + 16 * (tid + 256 * j));
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int o = tid + 256 * j;
-      if (o >= 2 * D * ES) break;
-      *reinterpret_cast<u32x4*>(lds + (o >> 4) * kTile + (o & 15) * 16) = v[j];
-      // a key's piece: token o % 16 of tile o / (16 pieces a row), 8 or 16 elements
-      const int i = (o & 15) + 16 * (o / (D * ES)), p = o % (D * ES) / 16;
-      uint16_t* out = reinterpret_cast<uint16_t*>(a.k) + ((int64_t)(t0 + i) * a.kv_heads + h) * D;
-      if constexpr (ES == 2) {
-        *reinterpret_cast<u32x4_any*>(out + 8 * p) = k[j];
-      } else {
-        const float s = a.cks[rec + i];
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          decoded(u32x2{k[j][2 * e], k[j][2 * e + 1]}, s, a.qmax, f);
-          *reinterpret_cast<u32x4_any*>(out + 16 * p + 8 * e) = rounded(f, a.act);
-        }
-      }
+      // (a key's piece: token o % 16 of tile o / (16 pieces a row))
+      const int at = what ? (o >> 4) * kTile + (o & 15) * 16 : ((o & 15) + 16 * (o / (D * ES))) * kRow + o % (D * ES) / 16 * 16;
+      if (o < 2 * D * ES) *reinterpret_cast<u32x4*>(lds + at) = w[j];
     }
     __syncthreads();
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += RP) {
       const int i = r0 + tid / GL;
       if (i >= 32) break;
-      uint16_t* out = reinterpret_cast<uint16_t*>(a.v) + ((int64_t)(t0 + i) * a.kv_heads + h) * D + 8 * c;
+      uint16_t* out = to + ((int64_t)(t0 + i) * a.kv_heads + h) * D + 8 * c;
       if constexpr (ES == 2) {
-        uint32_t e[8];
+        u32x4 v;
+        if (!what) {
+          v = *reinterpret_cast<const u32x4*>(lds + i * kRow + 16 * c);
+        } else {
+          uint32_t e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = *reinterpret_cast<const uint16_t*>(lds + lds_at<2>(i, 8 * c + j));
-        *reinterpret_cast<u32x4_any*>(out) = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+          for (int j = 0; j < 8; ++j) e[j] = *reinterpret_cast<const uint16_t*>(lds + lds_at<2>(i, 8 * c + j));
+          v = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+        }
+        *reinterpret_cast<u32x4_any*>(out) = v;
       } else {
-        uint32_t e[8];
+        u32x2 q;
+        if (!what) {
+          q = *reinterpret_cast<const u32x2*>(lds + i * kRow + 8 * c);
+        } else {
+          uint32_t e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = lds[lds_at<1>(i, 8 * c + j)];
+          for (int j = 0; j < 8; ++j) e[j] = lds[lds_at<1>(i, 8 * c + j)];
+          q = u32x2{e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24};
+        }
         float f[8];
-        decoded(u32x2{e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24}, a.cvs[rec + i], a.qmax, f);
-        *reinterpret_cast<u32x4_any*>(out) = rounded(f, a.act);
+        decoded(q, scales[rec + i], a.qmax, f);
+        *reinterpret_cast<u32x4_any*>(out) = rounded<ACT>(f);
       }
     }
     return;
   }
-  for (int r = tid / GL; r < 64; r += RP) {  // 32 rows of keys, 32 of values
-    const int i = r & 31, what = r >> 5, t = t0 + i;
+  for (int i = tid / GL; i < 32; i += RP) {
+    const int t = t0 + i;
     if (t < 0 || t >= a.tokens) continue;
     const int slot = a.slots[t];
-    uint16_t* out = reinterpret_cast<uint16_t*>(what ? a.v : a.k) + ((int64_t)t * a.kv_heads + h) * D + 8 * c;
+    uint16_t* out = to + ((int64_t)t * a.kv_heads + h) * D + 8 * c;
     if (slot < 0 || slot >= a.n_slots) {
       *reinterpret_cast<u32x4_any*>(out) = u32x4{0u, 0u, 0u, 0u};
       continue;
     }
     const int64_t rec = ((int64_t)(slot >> a.page_log2) * a.kv_heads + h) << a.page_log2;
     const int at = slot & page;
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(what ? a.cv : a.ck) + rec * (D * ES);
+    const uint8_t* base = from + rec * (D * ES);
     if constexpr (ES == 1) {
       u32x2 q;
       if (!what) {
@@ -351,8 +367,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
         q = u32x2{e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24, e[4] | e[5] << 8 | e[6] << 16 | e[7] << 24};
       }
       float f[8];
-      decoded(q, (what ? a.cvs : a.cks)[rec + at], a.qmax, f);
-      *reinterpret_cast<u32x4_any*>(out) = rounded(f, a.act);
+      decoded(q, scales[rec + at], a.qmax, f);
+      *reinterpret_cast<u32x4_any*>(out) = rounded<ACT>(f);
     } else if (!what) {
       *reinterpret_cast<u32x4_any*>(out) = *reinterpret_cast<const u32x4*>(base + key_at<2>(at, c, D));
     } else {
@@ -364,7 +380,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
   }
 }
 
-template <int D> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
+template <int D, int ACT> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
   constexpr int RP = 2048 / D;
   // 32 tokens and more: values by blocks
   const int blocks = a.tokens >= 32 ? (a.tokens + 31) / 32 + 1 : 0;  // (they may begin anywhere in one)
@@ -376,23 +392,27 @@ template <int D> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
   const int most = (a.heads + per - 1) / per, want = (512 + teams - 1) / teams;
   a.parts = want < most ? want : most;
   const int64_t grid = a.value_jobs + (int64_t)teams * a.parts;
-  hipLaunchKernelGGL(kv_append_kernel<D>, dim3((unsigned)grid), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((kv_append_kernel<D, ACT>), dim3((unsigned)grid), dim3(256), 0, s, a);
   return hipGetLastError();
 }
-template <int D> hipError_t go_read(const KvReadArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(((a.tokens + 31) / 32 + 1) * a.kv_heads));
-  if (a.qmax) hipLaunchKernelGGL((kv_read_kernel<D, 1>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((kv_read_kernel<D, 2>), grid, dim3(256), 0, s, a);
+template <int D, int ACT> hipError_t go_read(const KvReadArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(((a.tokens + 31) / 32 + 1) * 2 * a.kv_heads));
+  if (a.qmax) hipLaunchKernelGGL((kv_read_kernel<D, 1, ACT>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((kv_read_kernel<D, 2, ACT>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendArgs& a, int dim, hipStream_t s) {
-  return dim == 64 ? go_append<64>(a, s) : dim == 128 ? go_append<128>(a, s) : go_append<256>(a, s);
+  if (a.act == MXMOE_BF16)
+    return dim == 64 ? go_append<64, MXMOE_BF16>(a, s) : dim == 128 ? go_append<128, MXMOE_BF16>(a, s) : go_append<256, MXMOE_BF16>(a, s);
+  return dim == 64 ? go_append<64, MXMOE_F16>(a, s) : dim == 128 ? go_append<128, MXMOE_F16>(a, s) : go_append<256, MXMOE_F16>(a, s);
 }
 hipError_t launch_kv_read(const KvReadArgs& a, int dim, hipStream_t s) {
-  return dim == 64 ? go_read<64>(a, s) : dim == 128 ? go_read<128>(a, s) : go_read<256>(a, s);
+  if (a.act == MXMOE_BF16)
+    return dim == 64 ? go_read<64, MXMOE_BF16>(a, s) : dim == 128 ? go_read<128, MXMOE_BF16>(a, s) : go_read<256, MXMOE_BF16>(a, s);
+  return dim == 64 ? go_read<64, MXMOE_F16>(a, s) : dim == 128 ? go_read<128, MXMOE_F16>(a, s) : go_read<256, MXMOE_F16>(a, s);
 }
 
 }  // namespace mxmoe
