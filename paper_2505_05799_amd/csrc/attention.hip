@@ -196,19 +196,17 @@ template <int KIND, int D, int MF> struct Rows16 {
       }
     }
     auto sees = [&](int f, int i) { return 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f]; };
-    if (g.some) {
-#pragma unroll
-      for (int f = 0; f < MF; ++f) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[f][i] = sees(f, i) ? (g.bad ? __builtin_nanf("") : x[f][i] * m[f]) : -__builtin_inff();
-        m[f] = 1.f;
-      }
-    }
     auto weights = [&](int f) {
       const float off = kBase - ref[f];
 #pragma unroll
+      for (int i = 0; i < 8; ++i) p[f][i] = __builtin_fmaf(x[f][i], m[f], off);
+      if (g.some) {  // (after the same arithmetic: a row's result does not hang on what others see)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[f][i] = sees(f, i) ? (g.bad ? __builtin_nanf("") : p[f][i]) : -__builtin_inff();
+      }
+#pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[f][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[f][i], m[f], off));
+        p[f][i] = __builtin_amdgcn_exp2f(p[f][i]);
         w[f][i] = ES == 1 ? p[f][i] * vs[i >> 2][i & 3] : p[f][i];
       }
       if (ES == 1 && g.some) {  // (whatever the scale of a token that is not seen)
@@ -222,17 +220,23 @@ template <int KIND, int D, int MF> struct Rows16 {
     };
     // (weights are not negative: the order of their bits is theirs, and inf and NaN come last; a
     // row without a reference has inf for its first tokens)
-    uint32_t top = 0u;
+    constexpr uint32_t kMost = KIND == C_BF16 ? kMostBf16 : kMostF16;
+    uint32_t top[MF], any = 0u;
 #pragma unroll
-    for (int f = 0; f < MF; ++f) top = max2(top, weights(f));
-    if (__ballot(max(top & 0xffffu, top >> 16) > (KIND == C_BF16 ? kMostBf16 : kMostF16))) {
+    for (int f = 0; f < MF; ++f) any = max2(any, top[f] = weights(f));
+    if (__ballot(max(any & 0xffffu, any >> 16) > kMost)) {
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
+        // (a row moves for its own weights' sake alone: what it comes to does not hang on the others)
+        uint32_t t = max(top[f] & 0xffffu, top[f] >> 16);
+        t = max(t, (uint32_t)__shfl_xor((int)t, 16, 64));
+        t = max(t, (uint32_t)__shfl_xor((int)t, 32, 64));
         float r = kNoReference;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          r = fmaxf(r, x[f][i] * m[f] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i >> 2][i & 3], kLeastScale)) : 0.f));
-        const float next = fmaxf(ref[f], quarters_max(r)), d = __builtin_amdgcn_exp2f(ref[f] - next);
+          if (!g.some || sees(f, i)) r = fmaxf(r, x[f][i] * m[f] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i >> 2][i & 3], kLeastScale)) : 0.f));
+        r = quarters_max(r);
+        const float next = t > kMost ? fmaxf(ref[f], r) : ref[f], d = t > kMost ? __builtin_amdgcn_exp2f(ref[f] - next) : 1.f;
         ref[f] = next;
         sum[f] *= d;
 #pragma unroll
@@ -610,7 +614,8 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
 }
 
 // Items of few blocks: a workgroup of W wavefronts takes an item, its wavefronts every Wth
-// block, and they meet in LDS: one launch, nothing in the workspace (but with a prefix).
+// block, and they meet in LDS: one launch, nothing in the workspace.  A short prefix is taken along
+// (a.fold), block by block in front of the item's own; beside a long one the sums go to the workspace.
 template <int KIND, int D, int MF, int W>
 __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) attention_item_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
@@ -621,13 +626,17 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
   const int seq = (int)blockIdx.x / per_seq, item = (int)blockIdx.x - seq * per_seq, rb = item / a.kv_heads, h = item - rb * a.kv_heads;
   const int length = length_of(a, seq), own = length - a.prefix_len - a.n_q + 1;
   const Fixed pages = fixed(a.table) + (int64_t)seq * a.width;
-  auto page_of = [&](int i) { return pages[(32 * i) >> a.page_log2]; };
+  const int pre = a.fold ? (min(length, a.prefix_len) + 31) >> 5 : 0;  // blocks of the prefix
+  auto page_of = [&](int i) {
+    const int t = 32 * (i < pre ? i : i - pre);
+    return (i < pre ? fixed(a.prefix) : pages)[t >> a.page_log2];
+  };
   auto token_of = [&](int i, int id) {
     const int64_t rec = (int64_t)((unsigned)id < (unsigned)a.n_pages ? id : 0) * a.kv_heads + h;
-    return (rec << a.page_log2) + ((32 * i) & ((1 << a.page_log2) - 1));
+    return (rec << a.page_log2) + ((32 * (i < pre ? i : i - pre)) & ((1 << a.page_log2) - 1));
   };
   int i = w;
-  int id = 32 * i < a.width << a.page_log2 ? page_of(i) : 0;  // (asked for beside the length)
+  int id = !a.fold && 32 * i < a.width << a.page_log2 ? page_of(i) : 0;  // (asked for beside the length)
   Rows16<KIND, D, MF> x;
   x.clear();
   int seen[MF];
@@ -636,9 +645,10 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
     const int r = 16 * (MF * rb + f) + n, j = r / group;
     const bool live = r < rows;
     x.load(a, f, live ? reinterpret_cast<const uint16_t*>(a.q) + ((int64_t)seq * a.n_q + j) * a.ldq + ((int64_t)h * group + r % group) * D : nullptr, lane);
-    seen[f] = live ? own + j : 0;
+    seen[f] = live ? own + j : -(1 << 30);
   }
-  const int blocks = own_blocks(a, seq);
+  const int blocks = pre + own_blocks(a, seq);
+  if (a.fold && i < blocks) id = page_of(i);
   const bool past = (int64_t)length > a.prefix_len + ((int64_t)a.width << a.page_log2);
   const int least = own + 16 * MF * rb / group, most = own + min(rows - 1, 16 * MF * rb + 16 * MF - 1) / group;
   Frag<KIND, D> k, v;
@@ -650,14 +660,16 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
   while (i < blocks) {
     const int next = i + W;
     const int next_id = next < blocks ? page_of(next) : 0;
+    // what lies before the block, and how many tokens of its part there are
+    const int from = i < pre ? 32 * i - a.prefix_len : 32 * (i - pre), part = i < pre ? a.prefix_len - 32 * i : 1 << 30;
     Sight g;
     g.bad = (unsigned)id >= (unsigned)a.n_pages;
-    g.least = least - 32 * i;
-    g.most = most - 32 * i;
+    g.least = min(least - from, part);
+    g.most = min(most - from, part);
     g.some = g.bad || g.least < 32;
     int limit[MF];
 #pragma unroll
-    for (int f = 0; f < MF; ++f) limit[f] = seen[f] - 32 * i;
+    for (int f = 0; f < MF; ++f) limit[f] = min(seen[f] - from, part);
     x.block(a, k, v, g, limit, lane, [&]() {
       if (next < blocks) k.load(a.ck, a.cks, token_of(next, next_id), lane);
     });
@@ -671,7 +683,7 @@ __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) atten
     meet<KIND, D, MF, W>(x, f, min(16, rows - r0), w < blocks, red, flag, w, lane, [&](int r, int d, f32x4 v4, float l, float top) {
       const int row = r0 + r, q = row / group;
       const int64_t tok = (int64_t)seq * a.n_q + q, head = (int64_t)h * group + row % group;
-      if (!a.prefix_len) {
+      if (!a.prefix_len || a.fold) {
         store4(a.out, tok * a.ldo + head * D + d, v4 * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
       } else {
         float* part = a.own + (tok * a.q_heads + head) * RS;
@@ -980,7 +992,7 @@ int direct_of(int64_t items, int64_t longest) {
   return items <= 256 ? 8 : 4;
 }
 
-struct Plan { int direct, frags, row_blocks, pre_frags, shares, grid, pieces; size_t starts, part, own, pre, total; };
+struct Plan { int fold, direct, frags, row_blocks, pre_frags, shares, grid, pieces; size_t starts, part, own, pre, total; };
 Plan plan_of(const AttnArgs& a, int dim) {
   Plan p = {};
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
@@ -988,9 +1000,13 @@ Plan plan_of(const AttnArgs& a, int dim) {
   p.frags = frags_of(rows, dim);
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_blocks, longest = ((int64_t)a.width << a.page_log2) / 32, most = items * longest;
-  p.direct = direct_of(items, longest);
+  const int64_t pre = ((int64_t)a.prefix_len + 31) / 32;
+  // a prefix is taken along by every sequence where the blocks of both are few: two launches less
+  // (8 sequences behind 1500 tokens FOLD_FIG)
+  p.fold = pre > 0 && pre + longest <= 64 && items <= 512;
+  p.direct = p.fold ? std::max(4, direct_of(items, pre + longest)) : direct_of(items, longest);
   p.grid = (int)std::min<int64_t>(256 * cu_holds(a.qmax == 0, p.frags * dim), std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront
-  if (a.prefix_len) {
+  if (a.prefix_len && !p.fold) {
     const int64_t prows = (int64_t)a.batch * rows;
     p.pre_frags = prows <= 64 || dim == 256 ? 1 : 2;
     const int64_t wgs = ((prows + 64 * p.pre_frags - 1) / (64 * p.pre_frags)) * a.kv_heads;
@@ -1003,7 +1019,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   size_t o = 0;
   p.starts = o; o = align(o + (p.direct ? 0 : 4 * ((size_t)a.batch + 2)));
   p.part = o; o = align(o + (p.direct ? 0 : 2) * (size_t)p.grid * std::min(rows, 16 * p.frags) * rs);
-  p.own = o; o = align(o + (a.prefix_len ? (size_t)all * rs : 0));
+  p.own = o; o = align(o + (a.prefix_len && !p.fold ? (size_t)all * rs : 0));
   p.pre = o; o = align(o + (size_t)p.shares * all * rs);
   p.total = o;
   return p;
@@ -1034,7 +1050,7 @@ template <int KIND, int D, int MF> hipError_t go_prefix(const AttnArgs& a, hipSt
 }
 template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipStream_t s) {
   hipError_t e = hipSuccess;
-  if (a.prefix_len) {
+  if (a.prefix_len && !p.fold) {
     if constexpr (D <= 128)
       if (p.pre_frags == 2) e = go_prefix<KIND, D, 2>(a, s);
     if (p.pre_frags == 1) e = go_prefix<KIND, D, 1>(a, s);
@@ -1043,7 +1059,7 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
   if constexpr (D <= 128)
     if (p.frags == 2) e = go_own<KIND, D, 2>(a, p, s);
   if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
-  if (e != hipSuccess || (p.direct && !a.prefix_len)) return e;
+  if (e != hipSuccess || (p.direct && (!a.prefix_len || p.fold))) return e;
   const unsigned all = (unsigned)(a.batch * a.n_q * a.q_heads);
   if (p.pieces <= 8)
     hipLaunchKernelGGL((attention_join_kernel<D, 1>), dim3((all * (D / 4) + 255) / 256), dim3(256), 0, s, a);
@@ -1072,6 +1088,7 @@ hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s) {
   a.row_blocks = p.row_blocks;
   a.shares = p.shares;
   a.direct = p.direct;
+  a.fold = p.fold;
   if (a.qmax == kQmaxF8) return by_dim<C_F8>(a, p, dim, s);
   if (a.qmax) return by_dim<C_I8>(a, p, dim, s);
   return a.act == MXMOE_BF16 ? by_dim<C_BF16>(a, p, dim, s) : by_dim<C_F16>(a, p, dim, s);

@@ -61,13 +61,15 @@ template <int ACT> LANES_INL void widened(u32x4 w, float (&v)[8]) {
 }
 LANES_INL u32x4 row_piece(const void* p, int64_t at) { return *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const uint16_t*>(p) + at); }
 
-// The slots of 32 tokens of a call from t0 on: whether they are one block of the cache, from its first
-// slot on (every wavefront finds out for itself)
+// The slots of 32 tokens of a call from t0 on (of those that there are): the first slot of the block of the
+// cache that they are side by side in, each at its place, or -1.  Every wavefront finds out for itself.
 LANES_INL int block_of(const int32_t* slots, int t0, int tokens, int n_slots) {
   const int l = threadIdx.x & 31, t = t0 + l;
-  const int slot = t >= 0 && t < tokens ? slots[t] : -1, first = __builtin_amdgcn_readfirstlane(slot);
-  const bool in = first >= 0 && first < n_slots && first % 32 == 0 && slot == first + l;
-  return __ballot(!in) ? -1 : first;
+  const bool live = t >= 0 && t < tokens;
+  const int at = live ? slots[t] - l : 0;
+  const uint64_t all = __ballot(live);
+  const int base = __builtin_amdgcn_readlane(at, __builtin_ctzll(all));  // (t0 < tokens: there is one)
+  return base >= 0 && base < n_slots && base % 32 == 0 && __ballot(live && at != base) == 0 ? base : -1;
 }
 
 // Pieces of values in LDS: 256 bytes of (dim tile, q), 16 bytes further apart than in the cache, so that
@@ -113,9 +115,30 @@ template <int D, int ES, int ACT> LANES_INL void append_values(const KvAppendArg
   if (first < 0) return;
   __syncthreads();
   uint8_t* base = reinterpret_cast<uint8_t*>(a.cv) + (rec0 + (first & page)) * (D * ES);
+  const int lo = max(0, -t0), hi = min(32, a.tokens - t0);  // tokens of the block that are the call's
+  for (int o = tid; o < 2 * D * ES; o += 256) {
+    const uint8_t* piece = lds + (o >> 4) * kTile + (o & 15) * 16;
+    uint8_t* to = base + 16 * o;
+    if (lo == 0 && hi == 32) {
+      *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(piece);
+      continue;
+    }
+    const int q = (o >> 4) & 3;
 #pragma unroll
-  for (int o = tid; o < 2 * D * ES; o += 256)
-    *reinterpret_cast<u32x4*>(base + 16 * o) = *reinterpret_cast<const u32x4*>(lds + (o >> 4) * kTile + (o & 15) * 16);
+    for (int g = 0; g < 4; ++g) {  // 4 bytes: 2 or 4 tokens of an element
+      const int t = 4 * q + (ES == 2 ? 2 * (g & 1) + 16 * (g >> 1) : 16 * (g & 1));
+      if (t >= lo && t + 4 / ES <= hi) {
+        *reinterpret_cast<uint32_t*>(to + 4 * g) = *reinterpret_cast<const uint32_t*>(piece + 4 * g);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4 / ES; ++e)
+          if (t + e >= lo && t + e < hi) {
+            if (ES == 2) *reinterpret_cast<uint16_t*>(to + 4 * g + 2 * e) = *reinterpret_cast<const uint16_t*>(piece + 4 * g + 2 * e);
+            else to[4 * g + e] = piece[4 * g + e];
+          }
+      }
+    }
+  }
 }
 
 // The first `value_jobs` workgroups take 32 tokens' values of one head each.  The others take `tb`
@@ -314,7 +337,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += RP) {
       const int i = r0 + tid / GL;
-      if (i >= 32) break;
+      if (i >= 32 || t0 + i < 0 || t0 + i >= a.tokens) continue;
       uint16_t* out = to + ((int64_t)(t0 + i) * a.kv_heads + h) * D + 8 * c;
       if constexpr (ES == 2) {
         u32x4 v;

@@ -620,10 +620,10 @@ struct AttnArgs {
   float scale, softcap;
   int32_t batch, n_q, q_heads, kv_heads, width, prefix_len, n_pages, page_log2, act, qmax;
   // set by the launch: parts of the workspace, fragments of 16 rows to a wavefront, row blocks
-  // of an item, shares of the prefix, wavefronts to an item (0: the list of blocks is shared)
+  // of an item, shares of the prefix, wavefronts to an item (0: the list of costs is shared), 1 if items take the prefix along
   uint32_t* starts;         // [batch + 2]: first block of a sequence, all blocks, blocks of a workgroup
   float *part, *own, *pre;  // rows of dim + 4: sums, reference, sum of weights
-  int32_t frags, row_blocks, shares, direct;
+  int32_t frags, row_blocks, shares, direct, fold;
 };
 size_t attention_workspace(const AttnArgs& a, int dim);
 hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s);

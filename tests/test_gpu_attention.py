@@ -596,6 +596,118 @@ def test_binding_refusals():
             M.kv_read(c.cache, bad)
 
 
+# Every form of the attention: items to a workgroup (4 or 8 wavefronts), the shared list, the prefix taken along or through
+# LDS; one and two fragments of rows.
+@pytest.mark.parametrize("act", ["bf16", "fp16"])
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("hq", [4, 40])
+def test_attention_forms(hq, dim, qmax, act):
+    for lengths, n_q in (([70, 3, 200], 1), ([2200, 0, 31, 640], 1), ([33] * 130, 2)):
+        c = Case(hq + dim, lengths, n_q=n_q, hq=hq, kv=2, dim=dim, qmax=qmax, act=act, page=64)
+        c.check(c.run(), only=range(min(4, len(lengths))), where=f"{lengths[:4]}")
+    # behind a long prefix, which ends inside a block; sequences that end inside it
+    lengths = [2150, 0, 1, 2101, 2100, 1500, 2133, 2099, 2300]
+    c = Case(hq + dim + 1, lengths, hq=hq, kv=2, dim=dim, qmax=qmax, act=act, page=64, prefix=2100)
+    c.check(c.run(), where="prefix")
+    c.softcap = 20.0
+    c.check(c.run(), where="prefix, cap")
+
+
+@pytest.mark.parametrize("qmax,dim", [(0, 64), (0, 128), (0, 256), (127, 128), (448, 64), (448, 128), (448, 256)])
+def test_long_prefix_odd_rows(qmax, dim):
+    """A long prefix whose rows past its end, and inside it past a sequence's end, are not finite; and
+    a value that is not finite where some rows see it; pages that are not the cache's."""
+    torch = torch_mod()
+    lengths = [2150, 700, 2100, 2101, 0, 64, 1999, 2080]
+    make = lambda: Case(19, lengths, n_q=2, hq=12, kv=2, dim=dim, qmax=qmax, page=64, prefix=2090)  # noqa: E731
+    c = make()
+    clean = c.run()
+    c.check(clean)
+    ends = np.arange(2090 % 64, 64) + 64 * int(c.prefix[-1])          # behind the prefix in its last page
+    for what in (float("nan"), float("inf")):
+        c = make()
+        poison(c, ends, what)
+        assert torch.equal(c.run().view(torch.int16), clean.view(torch.int16))
+        for at in (1000, 2085, 63):
+            c = make()
+            poison(c, c.slots(0)[at:at + 1], what)
+            got = c.run()
+            for b, n in enumerate(lengths):
+                for j in range(2):
+                    r = 2 * b + j
+                    if n - 1 + j > at:
+                        assert not torch.isfinite(got[r]).any(), (what, at, b, j)
+                    else:
+                        assert torch.equal(got[r].view(torch.int16), clean[r].view(torch.int16)), (what, at, b, j)
+    if qmax == 0:   # one element: that element alone
+        c = make()
+        slot = c.slots(0)[1000:1001]
+        k, v = M.kv_read(c.cache, i32(slot))
+        v[0, 1, 5] = float("inf")
+        M.kv_append(c.cache, k, v, i32(slot))
+        got = c.run()
+        odd = torch.zeros_like(clean, dtype=torch.bool)
+        for b, n in enumerate(lengths):
+            for j in range(2):
+                if n - 1 + j > 1000:
+                    odd[2 * b + j, 6:, 5] = True
+        assert not torch.isfinite(got[odd]).any()
+        assert torch.equal(got[~odd].view(torch.int16), clean[~odd].view(torch.int16))
+    c = make()
+    c.prefix[20] = c.cache.n_pages
+    got = c.run()
+    for b, n in enumerate(lengths):
+        for j in range(2):
+            r = 2 * b + j
+            if n - 1 + j > 20 * 64:
+                assert torch.isnan(got[r]).all()
+            else:
+                assert torch.equal(got[r].view(torch.int16), clean[r].view(torch.int16))
+
+
+def test_least_and_largest_lengths():
+    torch = torch_mod()
+    for prefix in (0, 40, 3000):
+        c = Case(44, [prefix + 50] * 4, qmax=127, prefix=prefix)
+        clean = c.run()
+        n = c.lengths.astype(np.int64)
+        n[[0, 2]] = (-2 ** 31, 2 ** 31 - 1)
+        got = M.attention_decode(c.cache, up(c.q, c.act), i32(c.table), i32(n), prefix=i32(c.prefix) if prefix else None,
+                                 prefix_len=prefix)
+        assert not got[0].any() and torch.isnan(got[2]).all()
+        assert torch.equal(got[[1, 3]].view(torch.int16), clean[[1, 3]].view(torch.int16))
+
+
+@pytest.mark.parametrize("qmax,dim,act", [(0, 64, "bf16"), (0, 128, "fp16"), (0, 256, "bf16"), (127, 64, "bf16"), (127, 128, "fp16"),
+                                          (448, 128, "bf16"), (448, 256, "fp16")])
+def test_runs_of_slots(qmax, dim, act):
+    """Calls whose tokens fill blocks of the cache in part: runs that begin and end anywhere, two runs
+    that meet inside a block of the call, a run broken by one token."""
+    torch = torch_mod()
+    rng = np.random.default_rng(dim)
+    kv, page, n_pages = 2, 64, 8
+    for slots in (np.arange(5, 100), np.arange(64, 64 + 33), np.arange(37, 37 + 40), np.arange(95, 127),
+                  np.concatenate([np.arange(70, 110), np.arange(200, 260)]), np.concatenate([np.arange(0, 17), np.arange(400, 440)]),
+                  np.concatenate([np.arange(32, 50), [300], np.arange(51, 96)]), np.arange(150, 100, -1),
+                  np.concatenate([[-1] * 3, np.arange(131, 190), [10 ** 9]]), np.arange(480, 512), np.arange(0, 512)):
+        n = len(slots)
+        cache, other = (M.KVCache(n_pages, kv, dim, page_size=page, act=act, qmax=qmax) for _ in range(2))
+        for t in (*cache.buffers(), *other.buffers()):
+            if t is not None:
+                t.view(torch.uint8).fill_(0x33)
+        x, y = rows(rng, (n, kv, dim), act), rows(rng, (n, kv, dim), act)
+        M.kv_append(cache, up(x, act), up(y, act), i32(slots))
+        for i in range(n):                                      # token by token
+            M.kv_append(other, up(x[i:i + 1], act), up(y[i:i + 1], act), i32(slots[i:i + 1]))
+        for a, b in zip(all_bytes(cache), all_bytes(other)):
+            assert torch.equal(a, b), slots
+        kept = (slots >= 0) & (slots < n_pages * page)
+        gk, gv = M.kv_read(cache, i32(slots))
+        assert np.array_equal(down(gk)[kept], exact_read(x, qmax, act)[kept]) and not down(gk)[~kept].any()
+        assert np.array_equal(down(gv)[kept], exact_read(y, qmax, act)[kept]) and not down(gv)[~kept].any()
+
+
 # ------------------------------------------------------------------ together
 def test_streams_and_graph():
     """A decode loop captured once: append and attention replayed with new tokens, slots and lengths, against the
