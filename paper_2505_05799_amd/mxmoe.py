@@ -548,6 +548,7 @@ class KVCache:
         self.t.k, self.t.v = self.k.data_ptr(), self.v.data_ptr()
         if qmax:
             self.t.k_scales, self.t.v_scales = self.k_scales.data_ptr(), self.v_scales.data_ptr()
+        self._ref = C.byref(self.t)
         self._dev = self.k.get_device()
         if self._dev < 0:
             raise ValueError(f"device {device}: a cache on a GPU is expected")
@@ -559,10 +560,10 @@ class KVCache:
 def _heads(t, name, dtype, rows, heads, dim, dev):
     """Raise ValueError unless t is [rows, heads, dim] of the dtype on GPU `dev`, a
     token's heads side by side; returns its address and the tokens' stride."""
-    if t.dtype is not dtype or tuple(t.shape) != (rows, heads, dim) or t.get_device() != dev:
+    if t.dtype is not dtype or t.shape != (rows, heads, dim) or t.get_device() != dev:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {dtype} {(rows, heads, dim)} on GPU {dev}")
     ld, hs, one = t.stride()
-    if rows and (one != 1 or (hs != dim and heads > 1) or (ld < heads * dim and rows > 1)):
+    if (one != 1 or (hs != dim and heads > 1) or (ld < heads * dim and rows > 1)) and rows:
         raise ValueError(f"{name}: strides {t.stride()}; a token's heads side by side, tokens apart from each other, are expected")
     return t.data_ptr(), (ld if rows > 1 else heads * dim)
 
@@ -580,13 +581,13 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None,
     rotation.  A slot must not come twice in a call."""
     torch = _torch()
     lib = _lib or load_library()
-    dev, dt, kv, dim = cache._dev, cache.dtype, cache.heads, cache.dim
+    dev, dt, kv, dim, i32 = cache._dev, cache.dtype, cache.heads, cache.dim, (torch.int32,)
     if k.dim() != 3:
         raise ValueError(f"k: shape {tuple(k.shape)}, expected [tokens, heads, dim]")
     n = k.shape[0]
     kp, ldk = _heads(k, "k", dt, n, kv, dim, dev)
     vp, ldv = _heads(v, "v", dt, n, kv, dim, dev)
-    sp = _dense(slots, "slots", (torch.int32,), (n,), dev)
+    sp = _dense(slots, "slots", i32, (n,), dev)
     qp, ldq, hq, op, ldo = None, 0, 0, None, 0
     if q is None:
         if q_weight is not None or q_out is not None:
@@ -599,15 +600,15 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None,
         ldo = hq * dim
         if q_out is not None:
             op, ldo = _heads(q_out, "q_out", dt, n, hq, dim, dev)
-    qw, kw = (None if w is None else _dense(w, name, (dt,), (dim,), dev)
-              for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+    qw = None if q_weight is None else _dense(q_weight, "q_weight", (dt,), (dim,), dev)
+    kw = None if k_weight is None else _dense(k_weight, "k_weight", (dt,), (dim,), dev)
     if (positions is None) != (freqs is None):
         raise ValueError("positions and freqs: a rotation needs both")
     pp = fp = None
     rot = 0
     if freqs is not None:
         rot = 2 * freqs.numel()
-        pp = _dense(positions, "positions", (torch.int32,), (n,), dev)
+        pp = _dense(positions, "positions", i32, (n,), dev)
         fp = _dense(freqs, "freqs", (torch.float64,), (rot // 2,), dev)
         if rot == 0:
             pp = fp = None
@@ -617,13 +618,13 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None,
         if q is not None and o is None:
             o = torch.empty(n, hq, dim, dtype=dt, device=q.device)
             p = o.data_ptr()
-        st = lib.mxmoe_kv_append(C.byref(cache.t), n, qp, ldq, hq, kp, ldk, vp, ldv, qw, kw, eps, pp, fp, rot,
+        st = lib.mxmoe_kv_append(cache._ref, n, qp, ldq, hq, kp, ldk, vp, ldv, qw, kw, eps, pp, fp, rot,
                                  1 if interleaved else 0, sp, p, ldo, s)
         if st:
             raise MxmoeError(st, "mxmoe_kv_append")
         return o
 
-    return _run_on(dev, stream, body, (q, k, v, slots, q_weight, k_weight, positions, freqs, q_out, *cache.buffers()))
+    return _run_on(dev, stream, body, stream and (q, k, v, slots, q_weight, k_weight, positions, freqs, q_out, *cache.buffers()))
 
 
 def kv_read(cache: KVCache, slots, stream=None):
@@ -638,13 +639,14 @@ def kv_read(cache: KVCache, slots, stream=None):
     sp = _dense(slots, "slots", (torch.int32,), (n,), dev)
 
     def body(s):
-        k, v = (torch.empty(n, cache.heads, cache.dim, dtype=cache.dtype, device=cache.k.device) for _ in range(2))
-        st = lib.mxmoe_kv_read(C.byref(cache.t), n, sp, k.data_ptr(), v.data_ptr(), s)
+        k = torch.empty(n, cache.heads, cache.dim, dtype=cache.dtype, device=slots.device)
+        v = torch.empty_like(k)
+        st = lib.mxmoe_kv_read(cache._ref, n, sp, k.data_ptr(), v.data_ptr(), s)
         if st:
             raise MxmoeError(st, "mxmoe_kv_read")
         return k, v
 
-    return _run_on(dev, stream, body, (slots, *cache.buffers()))
+    return _run_on(dev, stream, body, stream and (slots, *cache.buffers()))
 
 
 def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len: int = 0, scale: Optional[float] = None,
@@ -668,19 +670,20 @@ def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len:
     if rows != batch * n_q or (batch and n_q == 0):
         raise ValueError(f"q: {rows} tokens for {batch} sequences")
     qp, ldq = _heads(q, "q", dt, rows, hq, dim, dev)
-    tp = _dense(table, "table", (torch.int32,), (batch, width), dev)
-    lp = _dense(lengths, "lengths", (torch.int32,), (batch,), dev)
+    i32 = (torch.int32,)
+    tp = _dense(table, "table", i32, (batch, width), dev)
+    lp = _dense(lengths, "lengths", i32, (batch,), dev)
     pp = None
     if prefix is None:
         if prefix_len:
             raise ValueError(f"prefix_len {prefix_len} without prefix")
     else:
-        pp = _dense(prefix, "prefix", (torch.int32,), (-(-prefix_len // cache.page_size),), dev)
+        pp = _dense(prefix, "prefix", i32, (-(-prefix_len // cache.page_size),), dev)
         pp = pp if prefix_len else None
     op, ldo = (None, hq * dim) if out is None else _heads(out, "out", dt, rows, hq, dim, dev)
     if scale is None:
         scale = dim ** -0.5
-    wsb = lib.mxmoe_attention_workspace_bytes(C.byref(cache.t), batch, n_q, hq, width, prefix_len)
+    wsb = lib.mxmoe_attention_workspace_bytes(cache._ref, batch, n_q, hq, width, prefix_len)
 
     def body(s):
         o, p = out, op
@@ -688,13 +691,13 @@ def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len:
             o = torch.empty(rows, hq, dim, dtype=dt, device=q.device)
             p = o.data_ptr()
         ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
-        st = lib.mxmoe_attention_decode(C.byref(cache.t), qp, ldq, batch, n_q, hq, tp if width else None, width, lp, pp,
+        st = lib.mxmoe_attention_decode(cache._ref, qp, ldq, batch, n_q, hq, tp if width else None, width, lp, pp,
                                         prefix_len, scale, softcap, p, ldo, ws.data_ptr() if wsb else None, wsb, s)
         if st:
             raise MxmoeError(st, "mxmoe_attention_decode")
         return o
 
-    return _run_on(dev, stream, body, (q, table, lengths, prefix, out, *cache.buffers()))
+    return _run_on(dev, stream, body, stream and (q, table, lengths, prefix, out, *cache.buffers()))
 
 
 # --------------------------------------------------------------- routing
