@@ -173,8 +173,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
   };
   u32x4 next = live && h < a.heads ? row_of(h) : u32x4{0u, 0u, 0u, 0u};
   const int slot = live ? a.slots[t] : -1;
-  // Row element i becomes (x own[i] + partner turned[i]) times the row's factor: weight times cosine,
-  // partner's weight times sine (with its sign), of queries first, of keys when they come.
+  // Row element i, times the row's factor, becomes x own[i] + partner turned[i]: weight times cosine,
+  // partner's weight times sine (with its sign), of queries first, of keys when they come.  (The factor
+  // first: a large row's products with its weight may pass the largest value.)
   float own[8], turned[8];
   int kind = -1;
   const int hc = a.rot / 16;
@@ -259,8 +260,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
     if (what < 2 && (norm || a.rot)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = v[i] * own[i];
-        v[i] = (in ? __builtin_fmaf(o[i], turned[i], y) : y) * f;
+        const float y = v[i] * f * own[i];
+        v[i] = in ? __builtin_fmaf(o[i] * f, turned[i], y) : y;
       }
     }
     if (what == 0) {

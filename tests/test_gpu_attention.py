@@ -226,6 +226,27 @@ def test_append_special_rows(act):
 
 
 @pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+def test_append_large_rows_and_weights(qmax, inter):
+    """Rows whose products with the norm's weight pass the largest value, though the normalized rows are ordinary;
+    and small ones."""
+    torch = torch_mod()
+    rng = np.random.default_rng(17)
+    T, hq, kv, dim = 40, 2, 2, 128
+    x = rows(rng, (T, hq + kv, dim), "bf16") * np.where(np.arange(T) % 2, 2.0 ** 122, 2.0 ** -60)[:, None, None]
+    qw, kw = (O.round_to_act(rows(rng, dim, "bf16", 8.0) + 64, "bf16") for _ in range(2))
+    pos, freqs = rng.integers(0, 5000, T), 1e4 ** (-np.arange(32) / 32)
+    cache = M.KVCache(2, kv, dim, page_size=32, act="bf16", qmax=qmax)
+    v = up(rows(rng, (T, kv, dim), "bf16"), "bf16")
+    got = M.kv_append(cache, up(x[:, hq:], "bf16"), v, i32(np.arange(T)), q=up(x[:, :hq], "bf16"), q_weight=up(qw, "bf16"),
+                      k_weight=up(kw, "bf16"), positions=i32(pos), freqs=torch.from_numpy(freqs).cuda(), interleaved=inter)
+    y, e = head_error(x[:, :hq], qw, pos, freqs, inter)
+    assert np.all(np.abs(down(got) - y) <= TL.slot_bound(y, e, "bf16"))
+    y, e = head_error(x[:, hq:], kw, pos, freqs, inter)
+    check_cached(down(M.kv_read(cache, i32(np.arange(T)))[0]), y, e, qmax, "bf16")
+
+
+@pytest.mark.parametrize("inter", [False, True])
 def test_append_in_place_and_far_positions(inter):
     torch = torch_mod()
     rng = np.random.default_rng(4)
