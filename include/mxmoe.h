@@ -355,8 +355,8 @@ MXMOE_API size_t mxmoe_kv_scale_bytes(const mxmoe_kv_cache* cache);
  *              q_out is written).  A slot given twice in a call holds either token's
  *              bytes or some of both: what is read from it is undefined, other slots are not
  *              affected.
- * `act` is the cache's.  rot: a multiple of 16 up to dim, n_tokens <= 2^24 (UNSUPPORTED
- * otherwise).
+ * `act` is the cache's.  rot: a multiple of 16 up to dim, n_tokens <= 2^24, n_tokens * heads
+ * <= 2^27 (UNSUPPORTED otherwise).
  * 2-byte aligned rows, 4-byte positions and slots, 8-byte freqs.  Outputs share no
  * byte with inputs (but q_out with q) or each other.  1e-30 <= eps <= 1e30 where there is a
  * weight; q_heads <= 65536.
@@ -370,8 +370,9 @@ MXMOE_API mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_to
 
 /* Rows of the cache back: k_out, v_out `act` [n_tokens, heads, dim] dense, code * scale
  * rounded once (16-bit rows as they are); slots int32 [n_tokens], zeros for a slot outside the
- * cache.  n_tokens <= 2^24 (UNSUPPORTED beyond).  Outputs 2-byte aligned; they share no byte with the cache, slots or each
- * other.  Errors: INVALID_ARG, UNSUPPORTED, HIP.                             */
+ * cache.  n_tokens <= 2^24, n_tokens * heads <= 2^27 (UNSUPPORTED beyond).  Outputs 2-byte aligned;
+ * they share no byte with the cache, slots or each other.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP.                                     */
 MXMOE_API mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const int32_t* slots,
                            void* k_out, void* v_out, hipStream_t stream);
 
@@ -391,7 +392,7 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  *            them: query j sees the first lengths[b] - n_q + 1 + j.  A query that sees none
  *            (padding: length 0, or shorter than n_q) gets zeros.
  *   table  : int32 [batch, width]: pages of the positions from prefix_len on, page_size to a
- *            page.  Entries past a sequence's length are not read.
+ *            page.  Entries past a sequence's length are not used.
  *   prefix : int32 [ceil(prefix_len / page_size)]: pages of the first prefix_len positions, the
  *            same for every sequence and read once for all; NULL with prefix_len 0.  The
  *            result is that of a table in which they come first.
@@ -403,9 +404,9 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  * parts with a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
  * value's scale is in them (scales below 2^-80 count for less).
  * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
- * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^26,
- * batch * heads * ceil(n_q * q_heads / heads / 16) * (width * page_size + 1024) < 2^36 (UNSUPPORTED beyond).  scale finite, 0 <= softcap finite.  q and out 2-byte
- * aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
+ * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^24,
+ * batch * heads * ceil(n_q * q_heads / heads / 16) * (width * page_size + 1024) < 2^36
+ * (UNSUPPORTED beyond).  scale finite, softcap 0 or from 0 on, finite.  q and out 2-byte aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
  * each other or the inputs.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.  */
 MXMOE_API mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, int64_t ldq, int32_t batch,
                                     int32_t n_q, int32_t q_heads, const int32_t* table, int32_t width,

@@ -683,7 +683,9 @@ mxmoe_status check_cache(const mxmoe_kv_cache* c, bool buffers) {
   if (!aligned(c->k_scales, 16) || !aligned(c->v_scales, 16)) return MXMOE_ERR_INVALID_ARG;
   return MXMOE_OK;
 }
-constexpr int32_t kMaxKvTokens = 1 << 24;  // of a call
+// Tokens of a call: a launch has fewer than 2^32 threads, 256 to 32 tokens' keys or values of a head
+// and, with dim 256, to 8 tokens at the least.
+bool kv_tokens_ok(const mxmoe_kv_cache& c, int32_t n) { return n <= 1 << 24 && (int64_t)n * c.heads <= 1 << 27; }
 int64_t cache_bytes(const mxmoe_kv_cache& c) { return (int64_t)c.n_pages * c.heads * c.page_size * c.dim * (c.qmax ? 1 : 2); }
 int64_t scale_bytes(const mxmoe_kv_cache& c) { return c.qmax ? (int64_t)c.n_pages * c.heads * c.page_size * 4 : 0; }
 Rows whole(const void* p, int64_t bytes) { return Rows{p, bytes, bytes, p && bytes > 0 ? 1 : 0}; }
@@ -720,7 +722,7 @@ mxmoe_status mxmoe_kv_append(const mxmoe_kv_cache* cache, int32_t n_tokens, cons
   if (st != MXMOE_OK) return st;
   const mxmoe_kv_cache& c = *cache;
   if (n_tokens < 0 || q_heads < 0 || q_heads > 65536 || (interleaved != 0 && interleaved != 1)) return MXMOE_ERR_INVALID_ARG;
-  if (rot < 0 || rot > c.dim || rot % 16 || n_tokens > kMaxKvTokens) return MXMOE_ERR_UNSUPPORTED;
+  if (rot < 0 || rot > c.dim || rot % 16 || !kv_tokens_ok(c, n_tokens)) return MXMOE_ERR_UNSUPPORTED;
   if ((q_weight || k_weight) && (!(eps >= 1e-30) || !(eps <= 1e30))) return MXMOE_ERR_INVALID_ARG;
   if (n_tokens == 0) return MXMOE_OK;
   if (!k || !v || !slots || (q_heads > 0) != (q != nullptr) || (q_heads > 0) != (q_out != nullptr) || (q_weight && !q))
@@ -778,7 +780,7 @@ mxmoe_status mxmoe_kv_read(const mxmoe_kv_cache* cache, int32_t n_tokens, const 
   if (st != MXMOE_OK) return st;
   const mxmoe_kv_cache& c = *cache;
   if (n_tokens < 0) return MXMOE_ERR_INVALID_ARG;
-  if (n_tokens > kMaxKvTokens) return MXMOE_ERR_UNSUPPORTED;
+  if (!kv_tokens_ok(c, n_tokens)) return MXMOE_ERR_UNSUPPORTED;
   if (n_tokens == 0) return MXMOE_OK;
   if (!slots || !k_out || !v_out || !aligned(slots, 4) || !aligned(k_out, 2) || !aligned(v_out, 2)) return MXMOE_ERR_INVALID_ARG;
   const int64_t ob = 2 * (int64_t)n_tokens * c.heads * c.dim;
@@ -807,7 +809,7 @@ namespace {
 mxmoe_status check_attention(const mxmoe_kv_cache& c, int32_t batch, int32_t n_q, int32_t q_heads, int32_t width,
                              int32_t prefix_len) {
   if (batch < 0 || n_q <= 0 || q_heads <= 0 || q_heads % c.heads || width < 0 || prefix_len < 0) return MXMOE_ERR_INVALID_ARG;
-  if (n_q > MXMOE_ATTENTION_QUERIES || batch > 65535 || q_heads > 65536 || (int64_t)batch * n_q * q_heads >= (1 << 26) ||
+  if (n_q > MXMOE_ATTENTION_QUERIES || batch > 65535 || q_heads > 65536 || (int64_t)batch * n_q * q_heads >= (1 << 24) ||  // (a launch has fewer than 2^32 threads)
       (int64_t)width * c.page_size + prefix_len > (1 << 30))
     return MXMOE_ERR_UNSUPPORTED;
   // the kernels number blocks of 32 tokens (and some more for each 16 query rows of a kv head) with 32 bits

@@ -203,6 +203,18 @@ def test_attention_refuses_caches_and_unsupported(lib):
     assert attend(lib, batch=0, q=None, table=None, lengths=None, prefix=None, out=None, ws=None) == M.OK
 
 
+def test_calls_past_a_launch_are_refused(lib):
+    """A launch has fewer than 2^32 threads; these would need more."""
+    big = lambda heads, dim=64: cache(n_pages=1, heads=heads, dim=dim, k=at(1 << 19), v=at(1 << 19 | 1 << 18), ks=at(3), vs=at(4))  # noqa: E731
+    n = 1 << 24
+    assert read(lib, big(16), n=n) == M.ERR_UNSUPPORTED and append(lib, big(16), n=n, ldk=1024, ldv=1024) == M.ERR_UNSUPPORTED
+    assert read(lib, big(1024), n=(1 << 17) + 1) == M.ERR_UNSUPPORTED
+    c = big(1024)
+    assert attend(lib, c, batch=32768, n_q=1, hq=1024, ldq=1 << 16, ldo=1 << 16, width=1, plen=0, prefix=None) == M.ERR_UNSUPPORTED
+    assert lib.mxmoe_attention_workspace_bytes(C.byref(c), 16384, 1, 1024, 1, 0) == 0
+    assert lib.mxmoe_attention_workspace_bytes(C.byref(cache(heads=1)), 16384, 1, 1023, 100, 0) > 0
+
+
 def test_attention_workspace(lib):
     need = lib.mxmoe_attention_workspace_bytes(C.byref(cache()), 3, 2, 4, 500, 4000)
     if need:
