@@ -400,13 +400,13 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  * length past prefix_len + width * page_size those of its sequence.  What lies in
  * the cache past a query's last token does not reach it, whatever it is.  A query with
  * NaN or inf, and a seen key or value row that is not finite, may make the outputs that depend
- * on it NaN or inf.  Scores, weights and sums are fp32; weights are rounded to fp16 (two bf16
+ * on it NaN or inf, and so may a score past 2^125 in magnitude.  Scores, weights and sums are fp32; weights are rounded to fp16 (two bf16
  * parts with a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
  * value's scale is in them (scales below 2^-80 count for less).
  * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
  * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^24,
  * batch * heads * ceil(n_q * q_heads / heads / 16) * (width * page_size + 1024) < 2^36
- * (UNSUPPORTED beyond).  scale finite, softcap 0 or from 0 on, finite.  q and out 2-byte aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
+ * (UNSUPPORTED beyond).  scale finite, softcap 0 or 1e-30 .. 1e30.  q and out 2-byte aligned, workspace 256-byte (NULL where none is needed); out and workspace share no byte with
  * each other or the inputs.  Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP.  */
 MXMOE_API mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, int64_t ldq, int32_t batch,
                                     int32_t n_q, int32_t q_heads, const int32_t* table, int32_t width,

@@ -849,7 +849,7 @@ mxmoe_status mxmoe_attention_decode(const mxmoe_kv_cache* cache, const void* q, 
   const mxmoe_kv_cache& c = *cache;
   st = check_attention(c, batch, n_q, q_heads, width, prefix_len);
   if (st != MXMOE_OK) return st;
-  if (!(scale - scale == 0.f) || !(softcap >= 0.f) || !(softcap - softcap == 0.f)) return MXMOE_ERR_INVALID_ARG;
+  if (!(scale - scale == 0.f) || !(softcap == 0.f || (softcap >= 1e-30f && softcap <= 1e30f))) return MXMOE_ERR_INVALID_ARG;
   if (batch == 0) return MXMOE_OK;
   if (!q || !out || !lengths || (width > 0) != (table != nullptr) || (prefix_len > 0) != (prefix != nullptr))
     return MXMOE_ERR_INVALID_ARG;

@@ -68,6 +68,17 @@ template <int KIND> LANES_INL u32x4 widen8(uint32_t lo, uint32_t hi) {
   return u32x4{a[0], a[1], b[0], b[1]};
 }
 
+// tanh y = 1 - 2 / (1 + e^(2 y)) for y > 0; below 1/4, where the difference takes the value's own
+// digits (scores far below a cap), four terms more of the series.
+LANES_INL float tanh_of(float y) {
+  const float z = y * y;
+  const float big = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(fabsf(y) * (2.f * kLog2e)));
+  float s = __builtin_fmaf(z, 62.f / 2835.f, -17.f / 315.f);
+  s = __builtin_fmaf(z, s, 2.f / 15.f);
+  s = __builtin_fmaf(z, s, -1.f / 3.f);
+  return fabsf(y) < 0.25f ? __builtin_fmaf(y * z, s, y) : __builtin_copysignf(big, y);
+}
+
 LANES_INL float quarters_max(float v) {  // over the four lanes of a query row
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
@@ -153,7 +164,8 @@ template <int KIND, int D, int MF> struct Rows16 {
       for (int s = 0; s < D / 32; ++s) q[f][s] = u32x4{turned(q[f][s][0]), turned(q[f][s][1]), turned(q[f][s][2]), turned(q[f][s][3])};
       m = __builtin_ldexpf(m, -up);
     }
-    mul[f] = a.softcap > 0.f ? m / a.softcap : m * kLog2e;
+    // (finite: 0 times it is 0)
+    mul[f] = fminf(fmaxf(a.softcap > 0.f ? m / a.softcap : m * kLog2e, -0x1.fffffep127f), 0x1.fffffep127f);
   }
 
   // products of the rows and 32 keys: 16 keys of a tile, 32 elements of a step at a time
@@ -178,28 +190,31 @@ template <int KIND, int D, int MF> struct Rows16 {
   // weights of the 32 tokens, sums and references; ks, vs: the tokens' scales, limit: how many of
   // the tokens a row sees
   LANES_INL void weigh(const AttnArgs& a, const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Sight& g, const int (&limit)[MF], int lane) {
+    // A score is x k m, (k m) first: x k may pass the largest value where the score does not.
     float x[MF][8], p[MF][8], m[MF];
+    f32x4 k[2] = {f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{1.f, 1.f, 1.f, 1.f}};
+    if constexpr (ES == 1) { k[0] = ks[0]; k[1] = ks[1]; }
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
       m[f] = mul[f];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[f][i] = ES == 1 ? w[f][i] * ks[i >> 2][i & 3] : w[f][i];
+      for (int i = 0; i < 8; ++i) x[f][i] = w[f][i];
     }
     if (a.softcap > 0.f) {
-      const float c = a.softcap * kLog2e;
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)  // tanh y = 1 - 2 / (1 + e^(2 y))
-          x[f][i] = c - 2.f * c * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[f][i] * m[f] * (2.f * kLog2e)));
+        for (int i = 0; i < 8; ++i) x[f][i] = a.softcap * kLog2e * tanh_of(x[f][i] * (ES == 1 ? k[i >> 2][i & 3] * m[f] : m[f]));
         m[f] = 1.f;
       }
+      k[0] = k[1] = f32x4{1.f, 1.f, 1.f, 1.f};
     }
+    auto factor = [&](int f, int i) { return ES == 1 ? k[i >> 2][i & 3] * m[f] : m[f]; };
     auto sees = [&](int f, int i) { return 4 * (lane >> 4) + (i & 3) + 16 * (i >> 2) < limit[f]; };
     auto weights = [&](int f) {
       const float off = kBase - ref[f];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[f][i] = __builtin_fmaf(x[f][i], m[f], off);
+      for (int i = 0; i < 8; ++i) p[f][i] = __builtin_fmaf(x[f][i], factor(f, i), off);
       if (g.some) {  // (after the same arithmetic: a row's result does not hang on what others see)
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[f][i] = sees(f, i) ? (g.bad ? __builtin_nanf("") : p[f][i]) : -__builtin_inff();
@@ -234,7 +249,7 @@ template <int KIND, int D, int MF> struct Rows16 {
         float r = kNoReference;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (!g.some || sees(f, i)) r = fmaxf(r, x[f][i] * m[f] + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i >> 2][i & 3], kLeastScale)) : 0.f));
+          if (!g.some || sees(f, i)) r = fmaxf(r, x[f][i] * factor(f, i) + (ES == 1 ? __builtin_amdgcn_logf(fmaxf(vs[i >> 2][i & 3], kLeastScale)) : 0.f));
         r = quarters_max(r);
         const float next = t > kMost ? fmaxf(ref[f], r) : ref[f], d = t > kMost ? __builtin_amdgcn_exp2f(ref[f] - next) : 1.f;
         ref[f] = next;

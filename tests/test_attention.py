@@ -215,6 +215,11 @@ def test_calls_past_a_launch_are_refused(lib):
     assert lib.mxmoe_attention_workspace_bytes(C.byref(cache(heads=1)), 16384, 1, 1023, 100, 0) > 0
 
 
+@pytest.mark.parametrize("cap", [1e-31, 1e31, 1e-45])
+def test_caps_out_of_range_are_refused(lib, cap):
+    assert attend(lib, cap=cap) == M.ERR_INVALID_ARG
+
+
 def test_attention_workspace(lib):
     need = lib.mxmoe_attention_workspace_bytes(C.byref(cache()), 3, 2, 4, 500, 4000)
     if need:

@@ -6,7 +6,10 @@ over the cache within the error model below.
 Error model of the attention.  With the cached values as given, a weight w_t is off by
   d = ACC16_EPS * scale * sum |q||k|  (fp32 sums of exact products, tests/tolerance.py)
       + 8 * 2^-24 * (1 + |x|_max)     (products by scales, the reference's difference, exp2)
-      + cap * 2^-20 with a cap        (1 / (1 + e^2y) and e^2y to 2^-22 each, twice the cap)
+      + min(cap * 2^-20, |x|_max * 2^-19) with a cap (tanh y = 1 - 2 / (1 + e^2y) for y > 0: the quotient
+                                       and e^2y to 2^-22 each, twice the cap.  From y = 1/4 on, where
+                                       2 / (1 + e^2y) <= 0.76 and tanh y >= 0.24, that is 2^-19 of tanh y;
+                                       below, four terms more of its series leave out 2^-26 of it)
 relative to itself, in the numerator and in the normalizer; the numerator's weights are rounded
 once more, by at most u = eps / 2 of the dtype of the product (2^-8 bf16, 2^-11 fp16), and both
 sums are fp32 (ACC16_EPS each).  So |out - ref| <= (2 d + u + 2 ACC16_EPS) * sum p|v|, and half a
@@ -325,7 +328,7 @@ class Case:
             else:
                 qk = np.zeros((self.n_q, self.hq))
             x = abs(self.scale) * qk
-            d = TL.ACC16_EPS * x + 8 * TL.U32 * (1 + x) + (self.softcap * 2.0 ** -20 if self.softcap else 0)
+            d = TL.ACC16_EPS * x + 8 * TL.U32 * (1 + x) + (np.minimum(self.softcap * 2.0 ** -20, x * 2.0 ** -19) if self.softcap else 0)
             bound = TL.slot_bound(ref, (2 * d[..., None] + u + 2 * TL.ACC16_EPS) * mass, self.act)
             for j in range(self.n_q):
                 if seen[j] <= 0:
@@ -373,6 +376,26 @@ def test_attention_softcap(qmax, cap):
     c.check(c.run())
     c.scale = -0.05
     c.check(c.run())
+
+
+@pytest.mark.parametrize("cap", [1e-30, 1e-3, 300.0, 1e5, 1e9, 1e30])
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+def test_attention_caps_of_any_size(qmax, cap):
+    """Caps far above the scores, which hardly change them, and far below, which leave all tokens alike."""
+    c = Case(12, [1, 50, 333, 2100], n_q=2, qmax=qmax)
+    c.softcap = cap
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+def test_attention_sizes_that_meet(qmax, act="bf16"):
+    """Small queries and large keys, and the other way round: the scores are ordinary."""
+    for size in (2.0 ** 110, 2.0 ** -105):
+        for cap in (0.0, 20.0):
+            c = Case(13, [1, 70, 500], qmax=qmax, act=act, kscale=size)
+            c.q = O.round_to_act(c.q / size * 2, act)
+            c.softcap = cap
+            c.check(c.run(), where=f"{size} {cap}")
 
 
 @pytest.mark.parametrize("prefix", [1, 31, 32, 40, 64, 100, 777])
