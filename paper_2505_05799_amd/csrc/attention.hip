@@ -993,8 +993,9 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
   store4(a.out, tok * a.ldo + (int64_t)head * D + d, v * (past ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l), a.act);
 }
 
-
-// Fragments of 16 rows that a wavefront takes
+// Fragments of 16 rows that a wavefront takes.  us with 1 and 2 (32 heads of 128, 8 kv heads): 16 sequences up to 4000
+// tokens, 20 rows int8 32.4, 31.8, bf16 48.5, 39.3; 64 of 1000, 32 rows int8 37.9, 31.4, bf16 52, 55.  (40 rows: 28.1,
+// 32.5, bf16 38.0, 38.1)
 int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : 2; }
 
 // Wavefronts to an item, or 0 where the list of costs is shared.  An item to a workgroup is one launch
@@ -1016,14 +1017,17 @@ Plan plan_of(const AttnArgs& a, int dim) {
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_blocks, longest = ((int64_t)a.width << a.page_log2) / 32, most = items * longest;
   const int64_t pre = ((int64_t)a.prefix_len + 31) / 32;
-  // a prefix is taken along by every sequence where the blocks of both are few: two launches less
-  // (8 sequences behind 1500 tokens 18 -> 13.5 us)
-  p.fold = pre > 0 && pre + longest <= 64 && items <= 512;
-  p.direct = p.fold ? std::max(4, direct_of(items, pre + longest)) : direct_of(items, longest);
+  // A prefix is taken along by every item where that costs less than two launches more: few blocks to
+  // read again (by its bytes), and items not much longer.  us, taken along or apart (int8, dim 128, 4 rows): 8 sequences
+  // behind 1500 tokens 14.4, 18.0; 64 24.5, 33.6; 128 39.7, 45.9; 256 69, 63; 512 behind 300 60, 70; 64 behind 2500 35, 38;
+  // 4 19.5, 17.6; dim 256, 128 behind 300 28.8, 41, behind 1500 66, 58
+  p.fold = pre > 0 && (pre + longest <= 64 || (items >= 64 && pre <= 80 && longest <= 64)) && pre * items * dim <= 50000 * 128;
+  p.direct = p.fold ? direct_of(items, std::min<int64_t>(pre + longest, 48)) : direct_of(items, longest);
   p.grid = (int)std::min<int64_t>(256 * cu_holds(a.qmax == 0, p.frags * dim), std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront
   if (a.prefix_len && !p.fold) {
     const int64_t prows = (int64_t)a.batch * rows;
-    p.pre_frags = prows <= 64 || dim == 256 ? 1 : 2;
+    // (us with 1 and 2 behind 16000 int8 tokens: 128 rows a kv head 39.2, 42.2, 256 56.3, 55.6, 512 94, 82)
+    p.pre_frags = prows <= 128 || dim == 256 ? 1 : 2;
     const int64_t wgs = ((prows + 64 * p.pre_frags - 1) / (64 * p.pre_frags)) * a.kv_heads;
     const int64_t blocks = ((int64_t)a.prefix_len + 31) / 32;
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((blocks + 3) / 4, 64), 512 / wgs));
@@ -1076,9 +1080,12 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
   if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
   if (e != hipSuccess || (p.direct && (!a.prefix_len || p.fold))) return e;
   const unsigned all = (unsigned)(a.batch * a.n_q * a.q_heads);
-  if (p.pieces <= 8)
+  // groups to a row: all pieces of few rows at once, many rows without a meeting.  us with 1, 1024 / dim, 32 (behind 16000
+  // int8 tokens, 32 heads of 128): 4 sequences, 64 pieces 42.8, 27.2, 26.3; 32, 64 pieces 55, 42.3, 44.3; 64, 33 pieces 57.7,
+  // 55.6, 64.4; 128, 17 pieces 79.8, 81.9, 98
+  if (p.pieces <= 8 || (p.pieces <= 32 && all >= 4096))
     hipLaunchKernelGGL((attention_join_kernel<D, 1>), dim3((all * (D / 4) + 255) / 256), dim3(256), 0, s, a);
-  else if (p.pieces <= 32 || D == 256)
+  else if (p.pieces <= 32 || all > 512 || D == 256)
     hipLaunchKernelGGL((attention_join_kernel<D, 1024 / D>), dim3(all), dim3(256), 0, s, a);
   else if constexpr (D < 256)
     hipLaunchKernelGGL((attention_join_kernel<D, 32>), dim3(all), dim3(8 * D), 0, s, a);

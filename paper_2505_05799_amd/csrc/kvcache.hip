@@ -406,12 +406,15 @@ __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
 
 template <int D, int ACT> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
   constexpr int RP = 2048 / D;
-  // 32 tokens and more: values by blocks
+  // 32 tokens and more: values by blocks (us of a run of 256 slots, 4 heads of 128, int8: 4.8, without
+  // 6.9; 16384: 68, 73; below, a call is its launch, and 31 slots of dim 256 would take 5.3 for 3.9)
   const int blocks = a.tokens >= 32 ? (a.tokens + 31) / 32 + 1 : 0;  // (they may begin anywhere in one)
   a.value_jobs = blocks * a.kv_heads;
   a.heads = a.q_heads + (blocks ? 1 : 2) * a.kv_heads;
-  // tokens to a workgroup: one pair of angles to a thread, more where there are many tokens
-  a.tb = a.tokens >= 4096 ? RP : a.tokens >= 4 ? (RP < 4 ? RP : 4) : 1;
+  // tokens to a workgroup: more of them share angles and weights, fewer fill the CUs.  us with 1, 4, 8 (28 + 4
+  // heads of 128, int8): 16 tokens 3.9, 4.2, 4.5, 1024 10.4, 8.6, 9.1, 8192 -, 37.3, 33.2, 16384 102, 72, 68; 16 tokens of
+  // dim 256 3.8, 4.8, 4.9
+  a.tb = a.tokens >= 8192 ? 8 : a.tokens >= 32 ? 4 : 1;
   const int teams = (a.tokens + a.tb - 1) / a.tb, per = RP / a.tb;
   const int most = (a.heads + per - 1) / per, want = (512 + teams - 1) / teams;
   a.parts = want < most ? want : most;

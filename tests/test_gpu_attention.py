@@ -710,6 +710,42 @@ def test_long_prefix_odd_rows(qmax, dim):
                 assert torch.equal(got[r].view(torch.int16), clean[r].view(torch.int16))
 
 
+@pytest.mark.parametrize("B,hq,kv,prefix,longest", [
+    (40, 16, 8, 2100, 300), (10, 16, 8, 2500, 90), (130, 8, 8, 300, 200),    # taken along by 320, 80 and 1040 items
+    (40, 16, 8, 2600, 40), (3, 8, 2, 2100, 40),                              # too long for that
+    (40, 16, 1, 8200, 40), (128, 32, 2, 2700, 20), (9, 2, 1, 8200, 30)])     # many rows of many pieces, of some; few of many
+@pytest.mark.parametrize("qmax", [0, 127])
+def test_prefix_forms(B, hq, kv, prefix, longest, qmax):
+    rng = np.random.default_rng(B + prefix)
+    lengths = prefix + rng.integers(-40, longest, B)
+    lengths[:3] = (0, prefix // 2, prefix + longest)
+    c = Case(B, lengths, hq=hq, kv=kv, dim=64, qmax=qmax, prefix=prefix, page=64)
+    c.check(c.run(), only=range(min(B, 12)))
+    if B > 12:
+        c.check(c.run(), only=range(B - 4, B))
+
+
+@pytest.mark.parametrize("T", [31, 32, 8192])
+def test_append_tokens_of_a_workgroup(T):
+    """The same rows, each by itself and in a call of many."""
+    torch = torch_mod()
+    rng = np.random.default_rng(T)
+    kv, dim = 1, 64
+    x = up(rows(rng, (T, 3 * kv, dim), "bf16"), "bf16")
+    w = up(O.round_to_act(rows(rng, dim, "bf16", 0.2) + 1, "bf16"), "bf16")
+    pos, freqs = i32(rng.integers(0, 9000, T)), torch.from_numpy(1e4 ** (-np.arange(32) / 32)).cuda()
+    a, b = (M.KVCache(-(-T // 64), kv, dim, page_size=64, act="bf16", qmax=127) for _ in range(2))
+    slots = i32(np.arange(T))
+    args = lambda s: dict(q=x[s, :1], q_weight=w, k_weight=w, positions=pos[s], freqs=freqs)  # noqa: E731
+    got = M.kv_append(a, x[:, 1:2], x[:, 2:], slots, **args(slice(0, T)))
+    for t in range(0, T, 1 if T < 100 else 1111):
+        s = slice(t, t + 1)
+        one = M.kv_append(b, x[s, 1:2], x[s, 2:], slots[s], **args(s))
+        assert torch.equal(one, got[s])
+        for g, h in zip(M.kv_read(a, slots[s]), M.kv_read(b, slots[s])):
+            assert torch.equal(g, h)
+
+
 def test_least_and_largest_lengths():
     torch = torch_mod()
     for prefix in (0, 40, 3000):
