@@ -451,6 +451,8 @@ LANES_INL uint32_t item_cost(int blocks) { return blocks ? blocks + kItemCost : 
 // 2 g + 1 for one that begins one.  A wavefront asks for its next block's keys when this one's
 // have made their scores, for its values when this one's are added, in the same registers, also
 // into the next item, so that they are on their way while the wavefronts meet.
+// Bound by memory: 64 sequences up to 8192 fp8 tokens of 8 heads of 128, 555 MB, 108 us with the join, 5.1 TB/s
+// (a copy reaches 5.15, reading alone 6.0); 2 of 131072 int8 tokens 52 us, and 6 for the join of 64 pieces a row.
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attention_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
@@ -631,6 +633,8 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
 // Items of few blocks: a workgroup of W wavefronts takes an item, its wavefronts every Wth
 // block, and they meet in LDS: one launch, nothing in the workspace.  A short prefix is taken along
 // (a.fold), block by block in front of the item's own; beside a long one the sums go to the workspace.
+// Bound by latency: one sequence of 300 int8 tokens, 8 heads, 6.7 us, of which a launch is 2.3 and the rest the chain
+// length, page, keys, scores, weights, meeting; 8 sequences behind 1500 tokens 14.5 (seven blocks to a wavefront).
 template <int KIND, int D, int MF, int W>
 __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) attention_item_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
@@ -728,6 +732,10 @@ template <int KIND, int D> struct Stage {
 // wavefronts 16 MF rows each; keys and values go through LDS, two stages of them, where they come
 // once for all wavefronts and codes are widened once.  Workgroups with the same blocks, for other
 // rows, have indexes 8 apart: one XCD's, so that its L2 has them.
+// 128 sequences of 4 rows a kv head behind 32768 fp8 tokens, 8 heads of 128: 120 us for 69 GFLOP, 0.58 PFLOP/s (a bf16 product
+// of 8192^3: 1.16).  Neither memory (71 MB) nor the matrix cores (27% busy) bound it: a score takes some 8 vector
+// instructions, one of them a quarter-rate exponential, and two wavefronts a SIMD, as many as the
+// registers allow, wait for one another's results 43% of the time.
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
   using S = Stage<KIND, D>;
@@ -911,7 +919,7 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
 
 // Pieces of a query row joined: of the prefix's shares, of the workgroups that shared its
 // item.  D / 4 lanes hold a row; GP groups of them take the pieces of one row in turn, four at
-// a time, and meet in LDS.
+// a time, and meet in LDS.  Bound by memory where rows are many: 17 pieces of 4096 rows, 37 MB, 9.2 us.
 template <int D, int GP>
 __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_kernel(AttnArgs a) {
   constexpr int RS = D + 4, L = D / 4, T = GP == 32 ? 32 * L : 256, R = T / (L * GP);  // rows of a workgroup

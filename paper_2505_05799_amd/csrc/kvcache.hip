@@ -9,6 +9,8 @@
 // row consists of.  A value's elements lie 16 bytes apart there, next to those of other tokens:
 // 32 tokens whose slots are one block of the cache go through LDS and leave as whole pieces (and come
 // back that way), others element by element.
+#include <algorithm>
+
 #include "kvcache.h"
 #include "lanes.h"
 
@@ -146,6 +148,9 @@ template <int D, int ES, int ACT> LANES_INL void append_values(const KvAppendArg
 // their own): the groups of dim / 8 lanes share the tokens and take heads in turn, the next
 // row on its way meanwhile.  The rotations' cosines and sines go through LDS, one pair of a
 // token to a thread, into the registers of the lanes that need them for all heads.
+// Bound by memory where there are many tokens: 28 + 2 x 4 heads of 128 of 16384 tokens, bf16 in, int8 out,
+// 68.2 us, 4.9 TB/s (a copy of as much: 5.15); by its launch and three memory latencies (slot and row,
+// positions and frequencies, weights) where there are few: one token 3.7 us.
 template <int D, int ACT>
 __global__ void __launch_bounds__(256) kv_append_kernel(KvAppendArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL;
@@ -303,7 +308,8 @@ LANES_INL void decoded(u32x2 q, float s, int qmax, float (&v)[8]) {
 }
 
 // Rows at slots back in 16 bits.  32 tokens' keys or values of one head to a workgroup: whole pieces
-// where their slots are one block, else piece by piece and element by element.
+// where their slots are one block, else piece by piece and element by element.  65536 tokens of 8 int8
+// heads of 128: 89 us, 4.6 TB/s (copy 5.15; 177 without LDS); 1237 of one bf16 head of 256, 80 workgroups, 4.3 us: latency.
 template <int D, int ES, int ACT>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL, kRow = D * ES + 16;  // (rows of keys 16 bytes apart)
@@ -411,10 +417,10 @@ template <int D, int ACT> hipError_t go_append(KvAppendArgs a, hipStream_t s) {
   const int blocks = a.tokens >= 32 ? (a.tokens + 31) / 32 + 1 : 0;  // (they may begin anywhere in one)
   a.value_jobs = blocks * a.kv_heads;
   a.heads = a.q_heads + (blocks ? 1 : 2) * a.kv_heads;
-  // tokens to a workgroup: more of them share angles and weights, fewer fill the CUs.  us with 1, 4, 8 (28 + 4
-  // heads of 128, int8): 16 tokens 3.9, 4.2, 4.5, 1024 10.4, 8.6, 9.1, 8192 -, 37.3, 33.2, 16384 102, 72, 68; 16 tokens of
-  // dim 256 3.8, 4.8, 4.9
-  a.tb = a.tokens >= 8192 ? 8 : a.tokens >= 32 ? 4 : 1;
+  // tokens to a workgroup: more of them share angles and weights, fewer fill the CUs.  us with 1, 4, 8, 16 (28 + 4 heads
+  // of 128, int8): 16 tokens 3.9, 4.2, 4.5, 5.0, 1024 10.4, 8.6, 9.1, 9.8, 8192 -, 37.3, 33.2, 45.1, 16384 102, 72.4, 67.7, 68.2; 262144
+  // tokens of 4 keys and values alone -, -, 293, 264; 16384 of dim 64 -, 43.7, 37.4, 33.8
+  a.tb = a.tokens >= 16384 ? std::min(RP, 16) : a.tokens >= 8192 ? 8 : a.tokens >= 32 ? 4 : 1;
   const int teams = (a.tokens + a.tb - 1) / a.tb, per = RP / a.tb;
   const int most = (a.heads + per - 1) / per, want = (512 + teams - 1) / teams;
   a.parts = want < most ? want : most;
