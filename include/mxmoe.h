@@ -402,7 +402,8 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  * NaN or inf, and a seen key or value row that is not finite, may make the outputs that depend
  * on it NaN or inf, and so may a score past 2^125 in magnitude.  Scores, weights and sums are fp32; weights are rounded to fp16 (two bf16
  * parts with a 16-bit bf16 cache) for the product with v, with an 8-bit cache after the
- * value's scale is in them (scales below 2^-80 count for less).
+ * value's scale is in them.  Where tokens whose values are zeros, or have scales below 2^-80, have weights more than
+ * 2^90 times the other tokens', these count with fewer digits.
  * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
  * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^24,
  * batch * heads * ceil(n_q * q_heads / heads / 16) * (width * page_size + 1024) < 2^36

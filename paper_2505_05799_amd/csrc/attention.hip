@@ -13,7 +13,7 @@
 // fewer bits than fp16; what falls under fp16's least is under 2^-38 of the largest).  A
 // key's scale multiplies its score.  A value's scale multiplies its weight, and the reference
 // is that of the products, so that they keep 11 bits whatever the scales are; scales
-// under 2^-80 do not move it.  The sum of the weights is of fp32 values, before any rounding.
+// under 2^-80 move it no further than one of 2^-80 would.  The sum of the weights is of fp32 values, before any rounding.
 // 16-bit rows: fp16 weights are rounded once (11 bits), a bf16 weight enters as two, the rounded
 // one and what it lacks (with one, 8 bits, the output's error was 1.4 times its own rounding's;
 // the second product costs 0.5% where memory bounds a call, 5% where it does not).
@@ -40,6 +40,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kBase = 8.f;              // weights are 2^8 at the reference ..
 constexpr uint32_t kMostF16 = 0x7800u, kMostBf16 = 0x4700u;  // .. and move it past 2^15 (fp16 ends at 2^16)
 constexpr float kLeastScale = 0x1p-80f;
+constexpr float kMostSum = 0x1p96f;  // of a lane's weights of a block, without their values' scales, likewise
 constexpr float kNoReference = -0x1p126f;  // of a row that has seen nothing: below any, and against it every weight is inf
 
 template <int KIND> LANES_INL f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -87,6 +88,8 @@ LANES_INL float quarters_sum(float v) {
   v += __shfl_xor(v, 16, 64);
   return v + __shfl_xor(v, 32, 64);
 }
+
+LANES_INL float sum8(const float (&p)[8]) { return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])); }
 
 // Keys (or values) of 32 tokens as a lane holds them, and their scales.
 template <int KIND, int D> struct Frag {
@@ -191,7 +194,7 @@ template <int KIND, int D, int MF> struct Rows16 {
   // the tokens a row sees
   LANES_INL void weigh(const AttnArgs& a, const f32x4 (&ks)[2], const f32x4 (&vs)[2], const Sight& g, const int (&limit)[MF], int lane) {
     // A score is x k m, (k m) first: x k may pass the largest value where the score does not.
-    float x[MF][8], p[MF][8], m[MF];
+    float x[MF][8], p[MF][8], m[MF], total[ES == 1 ? MF : 1];
     f32x4 k[2] = {f32x4{1.f, 1.f, 1.f, 1.f}, f32x4{1.f, 1.f, 1.f, 1.f}};
     if constexpr (ES == 1) { k[0] = ks[0]; k[1] = ks[1]; }
 #pragma unroll
@@ -231,7 +234,16 @@ template <int KIND, int D, int MF> struct Rows16 {
       constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
       const u32x4 o = {pack2<P>(w[f][0], w[f][1]), pack2<P>(w[f][2], w[f][3]), pack2<P>(w[f][4], w[f][5]), pack2<P>(w[f][6], w[f][7])};
       pw[f] = o;
-      return max2(max2(o[0], o[1]), max2(o[2], o[3]));
+      uint32_t t = max2(max2(o[0], o[1]), max2(o[2], o[3]));
+      // Weights of values that are zeros, or whose scale is small, pass no limit with their scale in
+      // them: their sum is looked at too, so that the row's stays finite (2^27 times 2^96).  Past the
+      // limit a weight is 2^93 or more, its score at least 5 over what a scale of 2^-80 puts the
+      // reference to: it moves, and a lane's sum is 2^91 then at the most.
+      if constexpr (ES == 1) {
+        total[f] = sum8(p[f]);
+        if (total[f] > kMostSum) t = 0xffffffffu;
+      }
+      return t;
     };
     // (weights are not negative: the order of their bits is theirs, and inf and NaN come last; a
     // row without a reference has inf for its first tokens)
@@ -260,8 +272,7 @@ template <int KIND, int D, int MF> struct Rows16 {
       }
     }
 #pragma unroll
-    for (int f = 0; f < MF; ++f)
-      sum[f] += ((p[f][0] + p[f][1]) + (p[f][2] + p[f][3])) + ((p[f][4] + p[f][5]) + (p[f][6] + p[f][7]));
+    for (int f = 0; f < MF; ++f) sum[f] += ES == 1 ? total[ES == 1 ? f : 0] : sum8(p[f]);
   }
 
   // `what` in the 16-bit halves of the lane's tokens that come before a limit
