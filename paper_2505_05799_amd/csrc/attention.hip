@@ -12,11 +12,13 @@
 // fp16: queries in bf16 get a power of 2 a row that brings the largest to 2^14 (bf16 has
 // fewer bits than fp16; what falls under fp16's least is under 2^-38 of the largest).  A
 // key's scale multiplies its score.  A value's scale multiplies its weight, and the reference
-// is that of the products, so that they keep 11 bits whatever the scales are; scales
+// is that of the products, so that they keep their bits whatever the scales are; scales
 // under 2^-80 move it no further than one of 2^-80 would.  The sum of the weights is of fp32 values, before any rounding.
-// 16-bit rows: fp16 weights are rounded once (11 bits), a bf16 weight enters as two, the rounded
-// one and what it lacks (with one, 8 bits, the output's error was 1.4 times its own rounding's;
-// the second product costs 0.5% where memory bounds a call, 5% where it does not).
+//
+// A weight enters its product as two, the rounded one and what it lacks (bf16 16 bits, fp16 22), or,
+// where codes meet bf16 outputs, as one of fp16: its 11 bits lie under the output's 8 (errors grow by less
+// than 1%).  With one part 16-bit bf16 rows were off by 1.4 times the output's own rounding, fp16 outputs by 1.3 times.
+// The second product costs 0.5 to 1% where memory bounds a call, 5 to 11% where it does not.
 //
 // Tokens past a row's last are left out by selection, whatever they hold: their scores
 // become -inf, their values zeros.  Where rows of a tile see different tokens and a value
@@ -35,7 +37,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Workgroups of 4 wavefronts that a CU holds (registers)
 constexpr int cu_holds(bool wide, int mf_dim) { return wide && mf_dim >= 256 ? 1 : 2; }
-enum CacheKind { C_BF16, C_F16, C_I8, C_F8 };
+enum CacheKind { C_BF16, C_F16, C_I8, C_F8, C_I8_F16, C_F8_F16 };  // (codes by the activations' type, bf16 first)
+constexpr bool is_i8(int kind) { return kind == C_I8 || kind == C_I8_F16; }
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kBase = 8.f;              // weights are 2^8 at the reference ..
 constexpr uint32_t kMostF16 = 0x7800u, kMostBf16 = 0x4700u;  // .. and move it past 2^15 (fp16 ends at 2^16)
@@ -52,7 +55,7 @@ template <int KIND> LANES_INL f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 
 // 4 codes -> 4 fp16 values
 template <int KIND> LANES_INL u32x2 widen(uint32_t w) {
-  if constexpr (KIND == C_I8) {  // 1024 + 128 + q, less 1152
+  if constexpr (is_i8(KIND)) {  // 1024 + 128 + q, less 1152
     w ^= 0x80808080u;
     const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
     const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - off;
@@ -125,12 +128,14 @@ struct Sight { int some, bad, most, least; };
 // MF times 16 query rows of a wavefront: row 16 f + lane % 16.
 template <int KIND, int D, int MF> struct Rows16 {
   static constexpr int ES = KIND <= C_F16 ? 2 : 1;
+  static constexpr bool BOTH = KIND != C_I8 && KIND != C_F8;  // both parts of a weight
   u32x4 q[MF][D / 32];
   f32x4 acc[MF][D / 16];   // elements 16 i + 4 (lane / 16) + (0..3)
   float ref[MF], sum[MF];  // the row's reference, the sum of its weights (this lane's tokens)
   float mul[MF];           // from a product of codes to a score: in powers of 2, or (with a cap) parts of the cap
   float w[MF][8];          // products, then weights of the block in hand
   u32x4 pw[MF];            // weights as the second product takes them
+  static constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
 
   LANES_INL void clear() {
 #pragma unroll
@@ -149,7 +154,7 @@ template <int KIND, int D, int MF> struct Rows16 {
       const int c = ES == 2 ? 4 * s + qd : 8 * (s >> 1) + 2 * qd + (s & 1);
       q[f][s] = row ? (u32x4) * reinterpret_cast<const u32x4_any*>(row + 8 * c) : u32x4{0u, 0u, 0u, 0u};
     }
-    if (ES == 1 && a.act == MXMOE_BF16) {
+    if constexpr (KIND == C_I8 || KIND == C_F8) {
       uint32_t b = 0u;
 #pragma unroll
       for (int s = 0; s < D / 32; ++s)
@@ -231,7 +236,6 @@ template <int KIND, int D, int MF> struct Rows16 {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[f][i] = sees(f, i) ? w[f][i] : 0.f;
       }
-      constexpr int P = KIND == C_BF16 ? MXMOE_BF16 : MXMOE_F16;
       const u32x4 o = {pack2<P>(w[f][0], w[f][1]), pack2<P>(w[f][2], w[f][3]), pack2<P>(w[f][4], w[f][5]), pack2<P>(w[f][6], w[f][7])};
       pw[f] = o;
       uint32_t t = max2(max2(o[0], o[1]), max2(o[2], o[3]));
@@ -313,7 +317,7 @@ template <int KIND, int D, int MF> struct Rows16 {
   // becomes zero, and rows become NaN where a product of ones counts such values among
   // the tokens they see.
   LANES_INL void sift(Frag<KIND, D>& v, const Sight& g, const int (&limit)[MF], int lane) {
-    if constexpr (KIND == C_I8) return;  // (every code is finite, the weights of what is not seen are 0)
+    if constexpr (is_i8(KIND)) return;  // (every code is finite, the weights of what is not seen are 0)
     const u32x4 any = kept(g.most, lane);
     uint32_t odd = 0u;
 #pragma unroll
@@ -346,13 +350,13 @@ template <int KIND, int D, int MF> struct Rows16 {
 
   // weights times values, 16 elements of a tile at a time
   template <class V> LANES_INL void add(V value) {
-    u32x4 rest[KIND == C_BF16 ? MF : 1];
-    if constexpr (KIND == C_BF16) {
+    u32x4 rest[BOTH ? MF : 1];  // what the rounded weights lack
+    if constexpr (BOTH) {
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         auto lack = [&](int i) {
-          const f32x2 r = unpack2<MXMOE_BF16>(pw[f][i]);
-          return pack2<MXMOE_BF16>(w[f][2 * i] - r[0], w[f][2 * i + 1] - r[1]);
+          const f32x2 r = unpack2<P>(pw[f][i]);
+          return pack2<P>(w[f][2 * i] - r[0], w[f][2 * i + 1] - r[1]);
         };
         rest[f] = u32x4{lack(0), lack(1), lack(2), lack(3)};
       }
@@ -363,7 +367,7 @@ template <int KIND, int D, int MF> struct Rows16 {
 #pragma unroll
       for (int f = 0; f < MF; ++f) {
         acc[f][i] = mfma<KIND>(b, pw[f], acc[f][i]);
-        if constexpr (KIND == C_BF16) acc[f][i] = mfma<KIND>(b, rest[f], acc[f][i]);
+        if constexpr (BOTH) acc[f][i] = mfma<KIND>(b, rest[f], acc[f][i]);
       }
     }
   }
@@ -817,7 +821,7 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
   // Values enter LDS as finite ones, tokens past the prefix as zeros: rows that do not see a token
   // then need no more than a weight of 0.
   auto put = [&](S& to, int i0) {
-    if constexpr (KIND != C_I8) {
+    if constexpr (!is_i8(KIND)) {
       uint32_t seen16 = 0u, any = 0u;
       if (32 * (i0 + NB) > a.prefix_len) {
 #pragma unroll
@@ -897,7 +901,7 @@ __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
     if (i0 + NB < last) put(stage[at ^ 1], i0 + NB);
     __syncthreads();
   }
-  if (KIND != C_I8 && odd_values) {  // (rare: the values once more, as memory has them)
+  if (!is_i8(KIND) && odd_values) {  // (rare: the values once more, as memory has them)
     for (int i = first; i < min(last, (most + 31) >> 5); ++i) {
       const int64_t t = token_of(i, id_of(i));
       const u32x4 any = R::kept(a.prefix_len - 32 * i, lane);
@@ -1013,9 +1017,15 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
 }
 
 // Fragments of 16 rows that a wavefront takes.  us with 1 and 2 (32 heads of 128, 8 kv heads): 16 sequences up to 4000
-// tokens, 20 rows int8 32.4, 31.8, bf16 48.5, 39.3; 64 of 1000, 32 rows int8 37.9, 31.4, bf16 52, 55.  (40 rows: 28.1,
-// 32.5, bf16 38.0, 38.1)
-int frags_of(int64_t rows, int dim) { return rows <= 16 || dim == 256 ? 1 : 2; }
+// tokens, 20 rows int8 32.2, 31.6, bf16 48.2, 39.3; 64 of 1000, 32 rows int8 35.5, 31.0, bf16 52, 55.  (40 rows, which fill
+// three of one and four of two: 27.9, 32.5, bf16 38.3, 38.4)  FP8 codes with both parts of fp16 weights fit the
+// registers with one alone at dim 128: 20 rows 30.9, 98; 32 rows 35.6, 138.
+constexpr bool two_frags(int kind, int dim) { return dim == 64 || (dim == 128 && kind != C_F8_F16); }
+int kind_of(const AttnArgs& a) {
+  const bool bf16 = a.act == MXMOE_BF16;
+  return a.qmax == kQmaxF8 ? (bf16 ? C_F8 : C_F8_F16) : a.qmax ? (bf16 ? C_I8 : C_I8_F16) : bf16 ? C_BF16 : C_F16;
+}
+int frags_of(int64_t rows, int kind, int dim) { return rows > 16 && two_frags(kind, dim) ? 2 : 1; }
 
 // Wavefronts to an item, or 0 where the list of costs is shared.  An item to a workgroup is one launch
 // and needs no search for its place; from 64 blocks on its length is what the launch waits for, and
@@ -1032,7 +1042,7 @@ Plan plan_of(const AttnArgs& a, int dim) {
   Plan p = {};
   const int group = a.q_heads / a.kv_heads, rows = a.n_q * group;
   const int64_t rs = 4 * (int64_t)(dim + 4), all = (int64_t)a.batch * a.n_q * a.q_heads;
-  p.frags = frags_of(rows, dim);
+  p.frags = frags_of(rows, kind_of(a), dim);
   p.row_blocks = (rows + 16 * p.frags - 1) / (16 * p.frags);
   const int64_t items = (int64_t)a.batch * a.kv_heads * p.row_blocks, longest = ((int64_t)a.width << a.page_log2) / 32, most = items * longest;
   const int64_t pre = ((int64_t)a.prefix_len + 31) / 32;
@@ -1094,7 +1104,7 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
     if (p.pre_frags == 1) e = go_prefix<KIND, D, 1>(a, s);
     if (e != hipSuccess) return e;
   }
-  if constexpr (D <= 128)
+  if constexpr (two_frags(KIND, D))
     if (p.frags == 2) e = go_own<KIND, D, 2>(a, p, s);
   if (p.frags == 1) e = go_own<KIND, D, 1>(a, p, s);
   if (e != hipSuccess || (p.direct && (!a.prefix_len || p.fold))) return e;
@@ -1130,9 +1140,14 @@ hipError_t launch_attention(AttnArgs a, int dim, hipStream_t s) {
   a.shares = p.shares;
   a.direct = p.direct;
   a.fold = p.fold;
-  if (a.qmax == kQmaxF8) return by_dim<C_F8>(a, p, dim, s);
-  if (a.qmax) return by_dim<C_I8>(a, p, dim, s);
-  return a.act == MXMOE_BF16 ? by_dim<C_BF16>(a, p, dim, s) : by_dim<C_F16>(a, p, dim, s);
+  switch (kind_of(a)) {
+    case C_BF16: return by_dim<C_BF16>(a, p, dim, s);
+    case C_F16: return by_dim<C_F16>(a, p, dim, s);
+    case C_I8: return by_dim<C_I8>(a, p, dim, s);
+    case C_F8: return by_dim<C_F8>(a, p, dim, s);
+    case C_I8_F16: return by_dim<C_I8_F16>(a, p, dim, s);
+    default: return by_dim<C_F8_F16>(a, p, dim, s);
+  }
 }
 
 }  // namespace mxmoe
