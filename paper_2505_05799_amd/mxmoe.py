@@ -528,7 +528,8 @@ class KVCache:
     activation dtype, 127 int8 codes and 448 FP8 e4m3 with an fp32 scale per token
     and head.  k, v [n_pages, heads, page_size * dim] and k_scales, v_scales [n_pages, heads,
     page_size] start as zeros; rows are in an order of their own inside a page
-    (kv_append writes them, kv_read reads them), pages may be copied whole."""
+    (kv_append writes them, kv_read reads them), pages may be copied whole.  The calls use the
+    buffers' addresses: contents change in place, attributes are not set again."""
 
     def __init__(self, n_pages: int, heads: int, dim: int, page_size: int = 64, act: str = "bf16", qmax: int = 0,
                  device="cuda"):
@@ -552,6 +553,11 @@ class KVCache:
         self._dev = self.k.get_device()
         if self._dev < 0:
             raise ValueError(f"device {device}: a cache on a GPU is expected")
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{name}: a cache keeps its buffers and sizes; copy into the buffers")
+        super().__setattr__(name, value)
 
     def buffers(self):
         return self.k, self.v, self.k_scales, self.v_scales

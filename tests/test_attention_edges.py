@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 from oracle import mxmoe_oracle as O
+from paper_2505_05799_amd import mxmoe as M
 from paper_2505_05799_amd import workloads as W
 from tests import tolerance as TL
 
@@ -68,3 +69,15 @@ def test_the_bound_tells_one_part_of_a_weight_from_two(qmax, act):
                 worst = max(worst, float((np.abs(rounded(out, act) - ref[0, h]) / weight_bound(mass, ref, qmax, dim, act)[0, h]).max()))
         ratio[parts] = worst
     assert ratio[1] > 2 and ratio[2] < 1, ratio
+
+
+# ------------------------------------------------------------------ binding
+@pytest.mark.parametrize("name", ["k", "v", "k_scales", "v_scales", "t", "n_pages", "page_size", "qmax", "dtype"])
+def test_a_cache_keeps_its_buffers(name):
+    """The calls use the addresses that the descriptor was given: another tensor in a buffer's place would not be
+    the one that they write, and the one that they write might be freed."""
+    c = M.KVCache.__new__(M.KVCache)
+    setattr(c, name, 1)
+    with pytest.raises(AttributeError):
+        setattr(c, name, 2)
+    assert getattr(c, name) == 1
