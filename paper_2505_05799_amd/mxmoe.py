@@ -538,7 +538,8 @@ class KVCache:
         self.n_pages, self.heads, self.dim, self.page_size, self.act, self.qmax = n_pages, heads, dim, page_size, act, qmax
         self.dtype = {"bf16": torch.bfloat16, "fp16": torch.float16}[act]
         self.t = KVCache_t(n_pages, heads, dim, page_size, act_code(act), qmax)
-        if lib.mxmoe_kv_cache_bytes(C.byref(self.t)) == 0:
+        # (the descriptor's fields would take larger numbers modulo 2^32)
+        if max(n_pages, heads, dim, page_size, qmax) >> 31 > 0 or lib.mxmoe_kv_cache_bytes(C.byref(self.t)) == 0:
             raise MxmoeError(ERR_UNSUPPORTED, f"kv_cache({n_pages} pages of {page_size}, {heads} heads of {dim}, qmax {qmax})")
         rows = torch.int8 if qmax else self.dtype
         self.k, self.v = (torch.zeros(n_pages, heads, page_size * dim, dtype=rows, device=device) for _ in range(2))
@@ -675,6 +676,8 @@ def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len:
     n_q = rows // batch if batch else 1
     if rows != batch * n_q or (batch and n_q == 0):
         raise ValueError(f"q: {rows} tokens for {batch} sequences")
+    if max(width, prefix_len) >> 31 > 0:  # (the call would take them modulo 2^32)
+        raise MxmoeError(ERR_UNSUPPORTED, f"attention_decode(width {width}, prefix_len {prefix_len})")
     qp, ldq = _heads(q, "q", dt, rows, hq, dim, dev)
     i32 = (torch.int32,)
     tp = _dense(table, "table", i32, (batch, width), dev)

@@ -1,6 +1,8 @@
 """Edges of the attention of a decode step, on the CPU: that the bounds of test_gpu_attention_edges tell
 what they are for."""
 
+from types import SimpleNamespace
+
 import numpy as np
 import pytest
 
@@ -81,3 +83,23 @@ def test_a_cache_keeps_its_buffers(name):
     with pytest.raises(AttributeError):
         setattr(c, name, 2)
     assert getattr(c, name) == 1
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Not taken modulo 2^32."""
+    import torch
+    for k, size in enumerate((4, 2, 64, 64)):
+        for by in (1 << 31, 1 << 32, 1 << 40):
+            sizes = [4, 2, 64, 64]
+            sizes[k] = size + by
+            with pytest.raises(M.MxmoeError):
+                M.KVCache(*sizes, device="cpu")
+    with pytest.raises(M.MxmoeError):
+        M.KVCache(4, 2, 64, qmax=127 + (1 << 32), device="cpu")
+    cache = SimpleNamespace(_dev=0, dtype=torch.bfloat16, dim=64, page_size=64)
+    q, n = torch.empty(1, 2, 64, dtype=torch.bfloat16, device="meta"), torch.empty(1, dtype=torch.int32, device="meta")
+    pages = lambda *s: torch.empty(*s, dtype=torch.int32, device="meta")  # noqa: E731
+    with pytest.raises(M.MxmoeError):
+        M.attention_decode(cache, q, pages(1, (1 << 32) + 2), n)
+    with pytest.raises(M.MxmoeError):
+        M.attention_decode(cache, q, pages(1, 2), n, prefix=pages((1 << 26) + 1), prefix_len=(1 << 32) + 64)
