@@ -543,10 +543,8 @@ class KVCache:
             raise MxmoeError(ERR_UNSUPPORTED, f"kv_cache({n_pages} pages of {page_size}, {heads} heads of {dim}, qmax {qmax})")
         rows = torch.int8 if qmax else self.dtype
         self.k, self.v = (torch.zeros(n_pages, heads, page_size * dim, dtype=rows, device=device) for _ in range(2))
-        self.k_scales = self.v_scales = None
-        if qmax:
-            self.k_scales, self.v_scales = (torch.zeros(n_pages, heads, page_size, dtype=torch.float32, device=device)
-                                            for _ in range(2))
+        self.k_scales, self.v_scales = (torch.zeros(n_pages, heads, page_size, dtype=torch.float32, device=device) if qmax else None
+                                        for _ in range(2))
         self.t.k, self.t.v = self.k.data_ptr(), self.v.data_ptr()
         if qmax:
             self.t.k_scales, self.t.v_scales = self.k_scales.data_ptr(), self.v_scales.data_ptr()

@@ -74,6 +74,16 @@ def test_the_bound_tells_one_part_of_a_weight_from_two(qmax, act):
 
 
 # ------------------------------------------------------------------ binding
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+def test_a_cache_is_made(qmax, monkeypatch):
+    """All of it but the GPU: the constructor's steps on memory that is none."""
+    import torch
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    c = M.KVCache(4, 2, 64, page_size=32, qmax=qmax, device="meta")
+    assert c.k.shape == c.v.shape == (4, 2, 2048) and c.t.qmax == qmax and c._dev == 0
+    assert [t is not None for t in c.buffers()] == [True, True, qmax > 0, qmax > 0]
+
+
 @pytest.mark.parametrize("name", ["k", "v", "k_scales", "v_scales", "t", "n_pages", "page_size", "qmax", "dtype"])
 def test_a_cache_keeps_its_buffers(name):
     """The calls use the addresses that the descriptor was given: another tensor in a buffer's place would not be
