@@ -7,7 +7,7 @@ import pytest
 from oracle import mxmoe_oracle as O
 from paper_2505_05799_amd import mxmoe as M
 from tests.gpuhelp import torch_mod
-from tests.test_attention_edges import opposite_values, weight_bound
+from tests.test_attention_edges import opposite_values, rounded, weight_bound
 from tests.test_gpu_attention import Case, down, i32, up
 
 pytestmark = pytest.mark.gpu
@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 # items, a long one goes through LDS.  More than 16 rows (128 in LDS) make two fragments.
 FORMS = {"item8": (3, 2, 4, 1500, 0), "item8, two": (3, 2, 20, 1500, 0), "item4": (150, 2, 4, 1500, 0),
          "item4, two": (150, 2, 20, 1500, 0), "list": (64, 2, 4, 3000, 0), "list, two": (64, 2, 20, 3000, 0),
-         "fold": (8, 2, 4, 40, 1500), "lds": (20, 8, 4, 40, 6400), "lds, two": (128, 8, 4, 40, 6400)}
+         "fold": (8, 2, 4, 40, 1500), "lds": (20, 2, 4, 40, 2700), "lds, two": (70, 2, 4, 40, 2700)}
 
 
 def steep(qmax, dim, form, period, gap, last, small):
@@ -79,3 +79,121 @@ def test_both_parts_of_a_weight(form, dim, qmax, act):
         ref, mass = O.attention(c.q[b:b + 1], c.k[at], c.v[at], [n], c.scale)
         err, bound = np.abs(got[b] - ref[0]), weight_bound(mass, ref, qmax, dim, act)[0]
         assert np.all(err <= bound), (b, float((err / bound).max()))
+
+
+# ------------------------------------------------------------------ what is masked, in every form
+def spread(form, dim, qmax, act, seed=5):
+    """Sequences of every length from half the form's own tokens on, two query tokens each, over the same pages (so
+    that a token is past the end of some and seen by others), some that end inside the prefix; a table wider by a page."""
+    B, kv, group, own, prefix = FORMS[form]
+    c = Case(seed, [prefix + own], n_q=2, hq=max(1, group // 2) * kv, kv=kv, dim=dim, qmax=qmax, act=act, page=64, prefix=prefix)
+    rng = np.random.default_rng(seed)
+    c.q = c.q[:1] * rng.uniform(0.5, 1.5, (2 * B, 1, 1))
+    c.q = rounded(c.q, act)
+    c.table = np.repeat(c.table, B, axis=0)
+    c.lengths = prefix + own - rng.integers(0, own // 2, B)
+    c.lengths[0] = prefix + own
+    if prefix:
+        c.lengths[2:6] = prefix // 2 + 5, prefix // 2 + 6, prefix - 1, prefix
+    return c
+
+
+def poisoned(c, slots, what):
+    torch = torch_mod()
+    bad = torch.full((len(slots), c.kv, c.dim), what, dtype=c.cache.dtype, device="cuda")
+    M.kv_append(c.cache, bad, bad, i32(slots))
+
+
+def same_bits(a, b):
+    torch = torch_mod()
+    return bool(torch.equal(a.view(torch.int16), b.view(torch.int16)))
+
+
+def compare(c, got, clean, hit, where):
+    """Rows of tokens: those that `hit` names are not finite anywhere, the others as before, bit for bit."""
+    torch = torch_mod()
+    hit = torch.from_numpy(np.asarray(hit)).cuda()
+    assert not torch.isfinite(got[hit]).any(), where
+    assert same_bits(got[~hit], clean[~hit]), where
+
+
+def seeing(c, at):
+    """Whether each query token sees position `at`."""
+    return (np.repeat(c.lengths, 2) - 2 + np.tile([0, 1], len(c.lengths))) >= at
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp16"])
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_odd_values_in_every_form(form, dim, qmax, act):
+    """Keys and values that are not finite, e4m3 NaN codes, pages outside the cache and lengths past the table: NaN or
+    inf for the queries that see them, nothing for the others."""
+    torch = torch_mod()
+    c = spread(form, dim, qmax, act)
+    n, prefix = int(c.lengths[0]), c.prefix_len
+    slots = c.slots(0)
+    clean = c.run()
+    assert bool(torch.isfinite(clean).all())
+    keep = [None if t is None else t.clone() for t in c.cache.buffers()]
+
+    def restore():
+        for t, k in zip(c.cache.buffers(), keep):
+            if t is not None:
+                t.copy_(k)
+
+    ends = np.sort(c.lengths)
+    places = [n - 1, int(ends[len(ends) // 2]) - 1, int(ends[0]) - 1, prefix + 13] + ([prefix // 2 + 5, prefix - 1] if prefix else [])
+    for what in (float("nan"), float("inf")):
+        for at in places:
+            poisoned(c, slots[at:at + 1], what)
+            compare(c, c.run(), clean, seeing(c, at), (what, at))
+            restore()
+        tail = np.setdiff1d(np.arange(c.cache.n_pages * c.page), slots)          # what no sequence has
+        poisoned(c, tail, what)
+        assert same_bits(c.run(), clean), what
+        restore()
+    if qmax == 448:                                # codes that kv_append does not write, from the eighth token of a page on
+        first = prefix + (n - prefix) // c.page * c.page
+        page, some = int(slots[first]) // c.page, i32(slots[first:first + 7])
+        k, v = M.kv_read(c.cache, some)            # (rounded, and coded again)
+        M.kv_append(c.cache, k, v, some)
+        again = c.run()
+        for t in c.cache.buffers():
+            t[page].view(torch.uint8).fill_(0x7f)
+        M.kv_append(c.cache, k, v, some)
+        compare(c, c.run(), again, seeing(c, first + 7), "codes")
+        restore()
+    # a page outside the cache, for every second sequence
+    at, table = (n - prefix) * 3 // 4 // c.page, c.table.copy()
+    for id_ in (-1, c.cache.n_pages, 2 ** 31 - 1):
+        c.table[::2, at] = id_
+        hit = seeing(c, prefix + at * c.page) & np.repeat(np.arange(len(c.lengths)) % 2 == 0, 2)
+        compare(c, c.run(), clean, hit, id_)
+    c.table = table
+    if prefix:
+        pages = c.prefix.copy()
+        c.prefix[len(pages) // 2] = c.cache.n_pages
+        compare(c, c.run(), clean, seeing(c, len(pages) // 2 * c.page), "prefix")
+        c.prefix = pages
+    # lengths past the table: as empty places for all others (which decide where the shared list is cut)
+    lengths = c.lengths.copy()
+    c.lengths[1::3] = 0
+    empty = c.run()
+    assert not empty.reshape(len(lengths), 2, -1)[1::3].any()
+    c.lengths[1::3] = prefix + c.table.shape[1] * c.page + 1 + np.arange(len(c.lengths[1::3])) % 2 * 10 ** 9
+    past = np.zeros(len(lengths), bool)
+    past[1::3] = True
+    compare(c, c.run(), empty, np.repeat(past, 2), "past the table")
+
+
+@pytest.mark.parametrize("act", ["bf16", "fp16"])
+@pytest.mark.parametrize("qmax", [0, 127, 448])
+def test_lengths_of_neighbours(qmax, act):
+    """Where sequences share one list, the cuts between workgroups go by all lengths: a row may differ in rounding
+    when a neighbour's length changes, and stays within its bound."""
+    c = Case(23, [3000, 2500, 640, 0, 1], hq=4, kv=2, dim=64, qmax=qmax, act=act)
+    c.check(c.run())
+    for n in (1, 70, 2300):
+        c.lengths = np.array([3000, n, 640, 0, 1])
+        c.check(c.run(), where=f"{n}")
