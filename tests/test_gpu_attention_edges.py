@@ -8,7 +8,7 @@ from oracle import mxmoe_oracle as O
 from paper_2505_05799_amd import mxmoe as M
 from tests.gpuhelp import torch_mod
 from tests.test_attention_edges import opposite_values, rounded, weight_bound
-from tests.test_gpu_attention import Case, down, i32, up
+from tests.test_gpu_attention import Case, down, exact_read, i32, up
 
 pytestmark = pytest.mark.gpu
 
@@ -197,3 +197,62 @@ def test_lengths_of_neighbours(qmax, act):
     for n in (1, 70, 2300):
         c.lengths = np.array([3000, n, 640, 0, 1])
         c.check(c.run(), where=f"{n}")
+
+
+# ------------------------------------------------------------------ append
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("T,dim,qmax,rot", [(8192 + 5, 64, 448, 64), (8192 + 7, 128, 127, 128), (8192 + 3, 256, 0, 256),
+                                            (16384 + 13, 64, 127, 32), (16384 + 9, 128, 448, 128), (16384 + 5, 256, 127, 128),
+                                            (16384 + 15, 128, 0, 64)])
+def test_append_workgroups_of_many_tokens(T, dim, qmax, rot, inter):
+    """8 and 16 tokens to a workgroup, the last one filled in part: rows, codes and scales of single-token calls."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    hq, kv = 5, 2
+    make = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    x, w = make(T, hq + 2 * kv, dim), [make(dim) for _ in range(2)]
+    pos = torch.randint(0, 90000, (T,), generator=g, device="cuda").to(torch.int32)
+    freqs = torch.from_numpy(1e4 ** (-np.arange(rot // 2) / (rot // 2))).cuda()
+    pages = -(-T // 64) + 1
+    a, b = (M.KVCache(pages, kv, dim, page_size=64, act="bf16", qmax=qmax) for _ in range(2))
+    slots = torch.arange(3, T + 3, device="cuda").to(torch.int32)
+
+    def call(cache, s):
+        return M.kv_append(cache, x[s, hq:hq + kv], x[s, hq + kv:], slots[s], q=x[s, :hq], q_weight=w[0], k_weight=w[1],
+                           positions=pos[s], freqs=freqs, interleaved=inter)
+
+    got = call(a, slice(0, T))
+    some = sorted({*range(0, T, 997), *range(0, 17), *range(8180, 8193), *range(T - 33, T)})
+    for t in some:
+        assert same_bits(call(b, slice(t, t + 1))[0], got[t]), t
+    at = slots[torch.tensor(some, device="cuda")]
+    for g, h in zip(M.kv_read(a, at), M.kv_read(b, at)):
+        assert same_bits(g, h)
+
+
+@pytest.mark.parametrize("qmax", [0, 127])
+@pytest.mark.parametrize("first", [-1, 64])
+def test_runs_of_several_sequences(first, qmax):
+    """A call that writes and reads several prompts, each from the beginning of a page on: runs that the call's blocks of
+    32 tokens do not meet in step."""
+    torch = torch_mod()
+    rng = np.random.default_rng(8)
+    kv, dim, page = 2, 128, 64
+    lengths = [77, 1, 200, 33, 64, 130]
+    at, slots = 1, []
+    for n in lengths:
+        slots.append(at * page + np.arange(n))
+        at += -(-n // page)
+    slots = np.concatenate(slots)
+    slots[0] = first
+    n = len(slots)
+    cache = M.KVCache(at + 1, kv, dim, page_size=page, act="bf16", qmax=qmax)
+    x, y = (rounded(rng.standard_normal((n, kv, dim)), "bf16") for _ in range(2))
+    M.kv_append(cache, up(x, "bf16"), up(y, "bf16"), i32(slots))
+    keep = slots >= 0
+    for got, want in zip(M.kv_read(cache, i32(slots)), (x, y)):
+        assert np.array_equal(down(got)[keep], exact_read(want, qmax, "bf16")[keep])
+        assert not down(got)[~keep].any()
+    others = np.setdiff1d(np.arange(cache.n_pages * page), slots)
+    for got in M.kv_read(cache, i32(others)):
+        assert not torch.any(got)
