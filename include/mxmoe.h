@@ -354,7 +354,7 @@ MXMOE_API size_t mxmoe_kv_scale_bytes(const mxmoe_kv_cache* cache);
  *   slots    : int32 [n_tokens]; a token whose slot is outside the cache is not kept (its
  *              q_out is written).  A slot given twice in a call holds either token's
  *              bytes or some of both: what is read from it is undefined, other slots are not
- *              affected.
+ *              affected.  Fastest where the tokens are one sequence's: a run of slots.
  * `act` is the cache's.  rot: a multiple of 16 up to dim, n_tokens <= 2^24, n_tokens * heads
  * <= 2^27 (UNSUPPORTED otherwise).
  * 2-byte aligned rows, 4-byte positions and slots, 8-byte freqs.  Outputs share no
@@ -400,9 +400,10 @@ MXMOE_API size_t mxmoe_attention_workspace_bytes(const mxmoe_kv_cache* cache, in
  * length past prefix_len + width * page_size those of its sequence.  What lies in
  * the cache past a query's last token does not reach it, whatever it is.  A query with
  * NaN or inf, and a seen key or value row that is not finite, may make the outputs that depend
- * on it NaN or inf, and so may a score past 2^125 in magnitude.  Scores, weights and sums are fp32; weights enter the product
- * with v as two rounded parts (fp16, or bf16 with a 16-bit bf16 cache), or as one of fp16 where an 8-bit cache
- * meets bf16 outputs; with an 8-bit cache the value's scale is in what is rounded.  Where tokens whose values are zeros, or have scales below 2^-80, have weights more than
+ * on it NaN or inf, and so may a score past 2^125 or a value past 2^80 in magnitude.  Scores, weights and
+ * sums are fp32; weights enter the product with v as two rounded parts (fp16, or bf16 with a 16-bit bf16
+ * cache), or as one of fp16 where an 8-bit cache meets bf16 outputs; with an 8-bit cache the value's scale is in
+ * what is rounded.  Where tokens whose values are zeros, or have scales below 2^-80, have weights more than
  * 2^90 times the other tokens', these count with fewer digits.
  * Limits: n_q <= MXMOE_ATTENTION_QUERIES, q_heads a multiple of heads, batch <= 65535,
  * q_heads <= 65536, prefix_len + width * page_size <= 2^30, batch * n_q * q_heads < 2^24,

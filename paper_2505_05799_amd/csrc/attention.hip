@@ -289,8 +289,8 @@ template <int KIND, int D, int MF> struct Rows16 {
     return m;
   }
   static constexpr uint32_t kInf = KIND == C_BF16 ? 0x7f80u : 0x7c00u, kOne = KIND == C_BF16 ? 0x3f80u : 0x3c00u;
-  // ones in the halves that are not finite.  (Fragments are changed whole: element by element, hipcc
-  // (clang 22, ROCm 7.2) has given a part of one's registers to other values while it was in use.)
+  // ones in the halves that are not finite.  (Fragments are changed whole: written element by element, results
+  // were wrong for bf16, dim 64, 32 rows, by hipcc of ROCm 7.2, for a reason that was not found.)
   static LANES_INL uint32_t odd_half(uint32_t w) {
     return ((w & kInf) == kInf ? 0xffffu : 0u) | ((w & (kInf << 16)) == kInf << 16 ? 0xffff0000u : 0u);
   }
@@ -454,8 +454,8 @@ LANES_INL void meet(const Rows16<KIND, D, MF>& x, int f, int live, bool has, flo
 }
 
 // What an item costs a workgroup beside its blocks (its queries, the wavefronts' meeting), in blocks.
-// us with 4, 8, 16: 64 sequences up to 8192 tokens fp8 110.6, 109.3, 110.0, 16 up to 4000 with 40
-// rows a kv head 37.7, 31.8, 28.1, one of 2000 12.8, 12.4, 14.0 (without: 123, 68, 13.0)
+// us with 4, 8, 16: 64 sequences up to 8192 tokens fp8 110.0, 108.5, 109.5, 16 up to 4000 with 40
+// rows a kv head 38.3, 32.6, 30.5, one of 2000 12.7, 12.1, 13.8 (without: 123, 68, 13.0)
 constexpr uint32_t kItemCost = 8;
 LANES_INL uint32_t item_cost(int blocks) { return blocks ? blocks + kItemCost : 0u; }
 
@@ -467,7 +467,7 @@ LANES_INL uint32_t item_cost(int blocks) { return blocks ? blocks + kItemCost : 
 // have made their scores, for its values when this one's are added, in the same registers, also
 // into the next item, so that they are on their way while the wavefronts meet.
 // Bound by memory: 64 sequences up to 8192 fp8 tokens of 8 heads of 128, 555 MB, 108 us with the join, 5.1 TB/s
-// (a copy reaches 5.15, reading alone 6.0); 2 of 131072 int8 tokens 52 us, and 6 for the join of 64 pieces a row.
+// (a copy reaches 5.15, reading alone 6.0); 2 of 131072 int8 tokens in fp16 54 us, and 6 for the join of 64 pieces a row.
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attention_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
@@ -648,8 +648,9 @@ __global__ void __launch_bounds__(256, cu_holds(KIND <= C_F16, MF * D)) attentio
 // Items of few blocks: a workgroup of W wavefronts takes an item, its wavefronts every Wth
 // block, and they meet in LDS: one launch, nothing in the workspace.  A short prefix is taken along
 // (a.fold), block by block in front of the item's own; beside a long one the sums go to the workspace.
-// Bound by latency: one sequence of 300 int8 tokens, 8 heads, 6.7 us, of which a launch is 2.3 and the rest the chain
-// length, page, keys, scores, weights, meeting; 8 sequences behind 1500 tokens 14.5 (seven blocks to a wavefront).
+// Bound by latency: one sequence of 300 int8 tokens, 8 heads, 6.6 us, of which a launch is 2.3 and the rest the chain
+// length, page, keys, scores, weights, meeting; 8 sequences behind 1500 tokens 13.9 (32 workgroups, seven blocks to a
+// wavefront).
 template <int KIND, int D, int MF, int W>
 __global__ void __launch_bounds__(64 * W, cu_holds(KIND <= C_F16, MF * D)) attention_item_kernel(AttnArgs a) {
   constexpr int RS = D + 4;
@@ -747,10 +748,11 @@ template <int KIND, int D> struct Stage {
 // wavefronts 16 MF rows each; keys and values go through LDS, two stages of them, where they come
 // once for all wavefronts and codes are widened once.  Workgroups with the same blocks, for other
 // rows, have indexes 8 apart: one XCD's, so that its L2 has them.
-// 128 sequences of 4 rows a kv head behind 32768 fp8 tokens, 8 heads of 128: 120 us for 69 GFLOP, 0.58 PFLOP/s (a bf16 product
-// of 8192^3: 1.16).  Neither memory (71 MB) nor the matrix cores (27% busy) bound it: a score takes some 8 vector
-// instructions, one of them a quarter-rate exponential, and two wavefronts a SIMD, as many as the
-// registers allow, wait for one another's results 43% of the time.
+// 128 sequences of 4 rows a kv head behind 32768 fp8 tokens, 8 heads of 128, bf16: 115 us for 69 GFLOP, 0.60 PFLOP/s (a bf16
+// product of 8192^3: 1.16).  Neither memory (71 MB) nor the matrix cores (29% busy) are its limit, but the order of its
+// work: scores, weights (some 8 vector instructions and a quarter-rate exponential a score) and products follow one
+// another in each of two wavefronts a SIMD (the registers hold no third), which wait 33% of the time, together at a
+// barrier each 64 tokens.
 template <int KIND, int D, int MF>
 __global__ void __launch_bounds__(256, 2) attention_prefix_kernel(AttnArgs a) {
   using S = Stage<KIND, D>;
@@ -1017,8 +1019,8 @@ __global__ void __launch_bounds__(GP == 32 ? 32 * D / 4 : 256) attention_join_ke
 }
 
 // Fragments of 16 rows that a wavefront takes.  us with 1 and 2 (32 heads of 128, 8 kv heads): 16 sequences up to 4000
-// tokens, 20 rows int8 32.2, 31.6, bf16 48.2, 39.3; 64 of 1000, 32 rows int8 35.5, 31.0, bf16 52, 55.  (40 rows, which fill
-// three of one and four of two: 27.9, 32.5, bf16 38.3, 38.4)  FP8 codes with both parts of fp16 weights fit the
+// tokens, 20 rows int8 32.4, 31.3, bf16 48.1, 39.3; 64 of 1000, 32 rows int8 36.6, 31.2, bf16 52, 55.  (40 rows, which fill
+// three of one and four of two: 28.0, 32.6, bf16 38.1, 38.1: for them one would be the better.)  FP8 codes with both parts of fp16 weights fit the
 // registers with one alone at dim 128: 20 rows 30.9, 98; 32 rows 35.6, 138.
 constexpr bool two_frags(int kind, int dim) { return dim == 64 || (dim == 128 && kind != C_F8_F16); }
 int kind_of(const AttnArgs& a) {
@@ -1030,8 +1032,9 @@ int frags_of(int64_t rows, int kind, int dim) { return rows > 16 && two_frags(ki
 // Wavefronts to an item, or 0 where the list of costs is shared.  An item to a workgroup is one launch
 // and needs no search for its place; from 64 blocks on its length is what the launch waits for, and
 // few long items leave CUs idle.  us with 4 wavefronts to an item, 8, shared (int8, dim 128, 4 rows; sequences of
-// 3/4 to all of the length): 8 items of 4 blocks 4.6, 4.4, 9.0; 8 of 63 16.1, 13.7, 11.6; 128 of 63 19.4, 15.9,
-// 21.0; 512 of 4 6.8, 8.9, 13.0; 512 of 63 46.4, 47.6, 56.3; 2048 of 16 50.6, 62.8, 65.0
+// 3/4 to all of the length): 8 items of 4 blocks 4.9, 5.0, 8.2; 8 of 63 17.5, 14.7, 12.1; 128 of 63 20.4, 16.7,
+// 20.1; 512 of 4 7.6, 10.2, 14.4; 512 of 63 47.3, 49.0, 54.3; 2048 of 16 51.0, 67.1, 62.9.  (By the table's
+// width, all that the host knows: short sequences behind a wide table take the shared list.)
 int direct_of(int64_t items, int64_t longest) {
   if (longest > 64 || (longest > 48 && items < 16)) return 0;
   return items <= 256 ? 8 : 4;
@@ -1048,14 +1051,14 @@ Plan plan_of(const AttnArgs& a, int dim) {
   const int64_t pre = ((int64_t)a.prefix_len + 31) / 32;
   // A prefix is taken along by every item where that costs less than two launches more: few blocks to
   // read again (by its bytes), and items not much longer.  us, taken along or apart (int8, dim 128, 4 rows): 8 sequences
-  // behind 1500 tokens 14.4, 18.0; 64 24.5, 33.6; 128 39.7, 45.9; 256 69, 63; 512 behind 300 60, 70; 64 behind 2500 35, 38;
-  // 4 19.5, 17.6; dim 256, 128 behind 300 28.8, 41, behind 1500 66, 58
+  // behind 1500 tokens 13.6, 17.7; 64 22.7, 33.3; 128 38.1, 42.0; 256 66, 54; 512 behind 300 58, 68; 64 behind 2500 32, 38;
+  // 4 18.6, 17.3; dim 256, 128 behind 300 27.7, 39, behind 1500 63, 51
   p.fold = pre > 0 && (pre + longest <= 64 || (items >= 64 && pre <= 80 && longest <= 64)) && pre * items * dim <= 50000 * 128;
   p.direct = p.fold ? direct_of(items, std::min<int64_t>(pre + longest, 48)) : direct_of(items, longest);
   p.grid = (int)std::min<int64_t>(256 * cu_holds(a.qmax == 0, p.frags * dim), std::max<int64_t>(1, (most + 3) / 4));  // a block to a wavefront
   if (a.prefix_len && !p.fold) {
     const int64_t prows = (int64_t)a.batch * rows;
-    // (us with 1 and 2 behind 16000 int8 tokens: 128 rows a kv head 39.2, 42.2, 256 56.3, 55.6, 512 94, 82)
+    // (us with 1 and 2 behind 16000 int8 tokens: 128 rows a kv head 37.9, 41.1, 256 54.0, 54.3, 512 85, 77)
     p.pre_frags = prows <= 128 || dim == 256 ? 1 : 2;
     const int64_t wgs = ((prows + 64 * p.pre_frags - 1) / (64 * p.pre_frags)) * a.kv_heads;
     const int64_t blocks = ((int64_t)a.prefix_len + 31) / 32;
@@ -1110,8 +1113,8 @@ template <int KIND, int D> hipError_t go(const AttnArgs& a, const Plan& p, hipSt
   if (e != hipSuccess || (p.direct && (!a.prefix_len || p.fold))) return e;
   const unsigned all = (unsigned)(a.batch * a.n_q * a.q_heads);
   // groups to a row: all pieces of few rows at once, many rows without a meeting.  us with 1, 1024 / dim, 32 (behind 16000
-  // int8 tokens, 32 heads of 128): 4 sequences, 64 pieces 42.8, 27.2, 26.3; 32, 64 pieces 55, 42.3, 44.3; 64, 33 pieces 57.7,
-  // 55.6, 64.4; 128, 17 pieces 79.8, 81.9, 98
+  // int8 tokens, 32 heads of 128): 4 sequences, 64 pieces 41.7, 26.1, 25.1; 32, 64 pieces 44, 37.8, 42.4; 64, 33 pieces 56.2,
+  // 54.4, 63.1; 128, 17 pieces 77.4, 79.6, 96
   if (p.pieces <= 8 || (p.pieces <= 32 && all >= 4096))
     hipLaunchKernelGGL((attention_join_kernel<D, 1>), dim3((all * (D / 4) + 255) / 256), dim3(256), 0, s, a);
   else if (p.pieces <= 32 || all > 512 || D == 256)

@@ -8,7 +8,10 @@
 // dim / 8 lanes hold a head's row, 8 elements each.  Keys are written in the 16-byte pieces that a
 // row consists of.  A value's elements lie 16 bytes apart there, next to those of other tokens:
 // 32 tokens whose slots are one block of the cache go through LDS and leave as whole pieces (and come
-// back that way), others element by element.
+// back that way), others element by element.  The tokens are counted off by 32 from where the call's first slot
+// says, so that one sequence's tokens fall into blocks; where a call holds several, those after the first
+// do as a rule not.  65536 tokens of 8 int8 heads of 128 in one sequence and in 16: in 119 and 182 us, back 85 and
+// 224; 16-bit rows in 129 and 249, back 94 and 222 (a call to a sequence has each fall into blocks).
 #include <algorithm>
 
 #include "kvcache.h"
@@ -309,7 +312,7 @@ LANES_INL void decoded(u32x2 q, float s, int qmax, float (&v)[8]) {
 
 // Rows at slots back in 16 bits.  32 tokens' keys or values of one head to a workgroup: whole pieces
 // where their slots are one block, else piece by piece and element by element.  65536 tokens of 8 int8
-// heads of 128: 89 us, 4.6 TB/s (copy 5.15; 177 without LDS); 1237 of one bf16 head of 256, 80 workgroups, 4.3 us: latency.
+// heads of 128: 85-89 us, 4.6-4.8 TB/s (copy 5.15; 177 without LDS), bf16 94, 5.7; 1237 of one bf16 head of 256, 80 workgroups, 4.3 us: latency.
 template <int D, int ES, int ACT>
 __global__ void __launch_bounds__(256) kv_read_kernel(KvReadArgs a) {
   constexpr int GL = D / 8, RP = 256 / GL, kRow = D * ES + 16;  // (rows of keys 16 bytes apart)

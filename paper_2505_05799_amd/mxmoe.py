@@ -583,7 +583,8 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None,
     stride (views of a joint projection); slots int32 [tokens], page * page_size + place
     (outside the cache: not kept); q_weight, k_weight [dim] or None for no norm;
     positions int32 [tokens] and freqs float64 [rot / 2], radians a position, or None for no
-    rotation.  A slot must not come twice in a call."""
+    rotation.  A slot must not come twice in a call.  32 and more tokens are fastest a sequence to a
+    call (a run of slots).  The queries have no autograd graph, also where inputs have one."""
     torch = _torch()
     lib = _lib or load_library()
     dev, dt, kv, dim, i32 = cache._dev, cache.dtype, cache.heads, cache.dim, (torch.int32,)
@@ -634,7 +635,7 @@ def kv_append(cache: KVCache, k, v, slots, q=None, q_weight=None, k_weight=None,
 
 def kv_read(cache: KVCache, slots, stream=None):
     """Rows of the cache back in its activation dtype (mxmoe_kv_read): (k, v), each [tokens,
-    heads, dim]; slots int32 [tokens], zeros for one outside the cache."""
+    heads, dim]; slots int32 [tokens], zeros for one outside the cache.  Without autograd graph."""
     torch = _torch()
     lib = _lib or load_library()
     dev = cache._dev
@@ -663,7 +664,8 @@ def attention_decode(cache: KVCache, q, table, lengths, prefix=None, prefix_len:
     table int32 [batch, width], pages of the positions from prefix_len on; lengths int32
     [batch], all tokens of a sequence (prefix and queries among them), 0 for padding; prefix
     int32 [ceil(prefix_len / page_size)], pages that every sequence begins with.  scale:
-    1 / sqrt(dim) by default; softcap > 0 caps the scores."""
+    1 / sqrt(dim) by default; softcap > 0 caps the scores.  The result has no autograd graph, also
+    where q has one."""
     torch = _torch()
     lib = _lib or load_library()
     dev, dt, dim = cache._dev, cache.dtype, cache.dim
